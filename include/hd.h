@@ -293,6 +293,135 @@ const char *hd_bundle_kernel(int64_t N, int64_t F, int64_t D, int64_t K, hd_dtyp
  */
 const char *hd_infer_kernel(int64_t N, int64_t F, int64_t D, int64_t K, hd_dtype dt, int packed);
 
+/*
+ * ---- Operators behind answers and learning ---------------------------------
+ *
+ * These calls keep the conventions above (device pointers owned by the caller,
+ * nothing allocated, work enqueued on `stream`, arguments checked on the host
+ * before anything is enqueued, N == 0 a no-op) with one addition: matrices of
+ * rows carry a row stride in elements (ld..., at least the row's length), so
+ * that a part of a wider matrix can be passed. Their dtypes are HD_F32 and
+ * HD_BF16 (HD_I8 gives HD_ERR_UNSUPPORTED). Results do not depend on the order of
+ * execution: the same inputs give the same bits. Rows are independent: what
+ * a row holds, NaN included, reaches no other row.
+ *
+ * Weights in 4 bits with group scales. A weight matrix of `outer` outputs and
+ * `inner` inputs stands for
+ *   w[o][i] = scale[o][i / group] * (code[o][i] - zero[o][i / group]),
+ * code and zero in 0..15, zero = 8 where there are no zero points, scale in
+ * bfloat16, group 32, 64 or 128 (the last group of a row may be shorter).
+ * Both matrices of a model are of this kind: the base hypervectors with
+ * outer = D, inner = F (B read column-major), the class hypervectors with
+ * outer = K, inner = D. Unlike the scales of an int8 model, group scales do not
+ * leave HardSign unchanged, so they are part of the product.
+ *
+ * hd_nibble_pack lays given codes out once (hd_nibble_bytes bytes, 256-byte
+ * aligned, opaque): codes [outer][ceil(inner/2)], input 2j in the low and 2j+1
+ * in the high half of byte j; scales [outer][ceil(inner/group)] bfloat16 bits;
+ * zeros the same shape, a byte each, or NULL.
+ * hd_nibble_quantize takes a matrix of numbers instead: W[outer][inner], or with
+ * inner_rows != 0 W[inner][outer] (B as it is); rows of stride ldw. Each group's
+ * scale is max |w| / 7, or with zeros != 0 (max - min) / 15 over the group and
+ * 0, rounded to bfloat16; codes are rounded to nearest (even). A group
+ * that holds an infinity or NaN stands for NaN throughout.
+ * hd_nibble_unpack writes the weights an image stands for, [outer][inner] fp32.
+ *
+ * hd_nibble_product: Y[n][o] = act( sum_i X[n][i] w[o][i] ), X[N][inner] of x_dt,
+ * Y[N][outer] of y_dt, sums in fp32 (products of codes and X exact), one
+ * rounding to y_dt. An X of fp32 is used in full. `zeros` says whether the
+ * image was made with zero points. Made for few rows (a single reading, a
+ * request batch): up to 64 rows read the weights once.
+ * Limits: outer, inner <= 2^30, ceil(outer/16) * ceil(inner/128) <= 2^24,
+ * N <= 2^20.
+ */
+size_t hd_nibble_bytes(int64_t outer, int64_t inner, int64_t group);
+hd_status hd_nibble_pack(const uint8_t *codes, const uint16_t *scales, const uint8_t *zeros,
+                         int64_t outer, int64_t inner, int64_t group, void *image,
+                         size_t image_bytes, hipStream_t stream);
+hd_status hd_nibble_quantize(const void *W, int64_t ldw, int inner_rows, int zeros, int64_t outer,
+                             int64_t inner, int64_t group, hd_dtype dt, void *image,
+                             size_t image_bytes, hipStream_t stream);
+hd_status hd_nibble_unpack(const void *image, int zeros, float *W, int64_t outer, int64_t inner,
+                           int64_t group, hipStream_t stream);
+hd_status hd_nibble_product(const void *X, int64_t ldx, const void *image, int zeros, void *Y,
+                            int64_t ldy, int64_t N, int64_t outer, int64_t inner, int64_t group,
+                            hd_dtype x_dt, hd_dtype y_dt, hd_act act, hipStream_t stream);
+
+/*
+ * Log probabilities of given classes, with the entropy and the best
+ * alternatives, from scores[N][K] (row stride ld):
+ *   m = max_k s_k,  L = log sum_k exp(scale (s_k - m)),
+ *   t_k = scale (s_k - m) - L                (the log probability of class k),
+ *   logp = t_y,  entropy = -sum_k exp(t_k) t_k,  stats = {m, L},
+ *   ids, top_logp: the `top` classes of largest score, largest first, ties to the
+ *   lowest class, with their t (0 <= top <= 32).
+ * scale > 0 is an inverse temperature. mask, if not NULL, is [N][K] bytes of row
+ * stride ldm (0: one row for all): classes whose byte is 0 take no part, and what their
+ * scores hold is not looked at. A score of -inf takes no part either; one of the
+ * type's lowest finite value is a number like others.
+ *   - y[n] outside [0, K): no class is asked for, logp = 0. y may be NULL (then
+ *     logp is not written and may be NULL).
+ *   - a class that takes no part has logp = -inf; alternatives that are not there
+ *     (top > classes that take part) have id -1 and log probability -inf.
+ *   - a row in which nothing takes part: logp = -inf (0 where no class is asked
+ *     for), entropy = 0, stats = {-inf, 0}, no alternatives.
+ *   - a row with NaN or +inf in a class that takes part: entropy, stats and
+ *     log probabilities NaN, ids -1 (logp 0 where no class is asked for).
+ * Sums are fp32. workspace: hd_logprobs_workspace_bytes(...) bytes (0 is possible),
+ * zeroed before its first use and left zeroed by every call.
+ * Limits: N, K <= 2^30.
+ */
+size_t hd_logprobs_workspace_bytes(int64_t N, int64_t K, hd_dtype dt);
+hd_status hd_logprobs(const void *scores, int64_t ld, const uint8_t *mask, int64_t ldm,
+                      const int32_t *y, float scale, float *logp, float *entropy, float *stats,
+                      int32_t *ids, float *top_logp, int64_t N, int64_t K, int64_t top,
+                      hd_dtype dt, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The gradient with respect to the scores of
+ *   sum_n g_logp[n] logp[n] + g_entropy[n] entropy[n]:
+ *   dscores[n][k] = scale ( g_logp (1[k = y] - p_k) - g_entropy p_k (t_k + entropy) ),
+ * p_k = exp(t_k), from the scores, mask, y and scale of hd_logprobs and its stats and
+ * entropy. Classes that take no part get 0 (NaN in a row whose stats are NaN);
+ * g_logp is read as 0 where no class is asked for. g_logp, g_entropy and y may be
+ * NULL (0, 0, none). dscores has the scores' dtype and row stride ldd; it may be
+ * the scores' own memory (same stride).
+ */
+hd_status hd_logprobs_grad(const void *scores, int64_t ld, const uint8_t *mask, int64_t ldm,
+                           const int32_t *y, float scale, const float *stats,
+                           const float *entropy, const float *g_logp, const float *g_entropy,
+                           void *dscores, int64_t ldd, int64_t N, int64_t K, hd_dtype dt,
+                           hipStream_t stream);
+
+/*
+ * Activations kept in 8 bits for the backward pass (encodings H[N][D], or any
+ * layer's inputs). 64 consecutive rows of one column share a scale:
+ *   s = max |x| * fl(1/127),  q = rint(x * fl(1/s)) in -127..127, kept as q * s
+ * (s in fp32; columns, since activations differ in size by channel). A group that
+ * holds an infinity or NaN is kept as NaN throughout; one whose largest value is
+ * below about 2^-121 is kept as 0.
+ * hd_ckpt_store writes the image (hd_ckpt_bytes bytes, 256-byte aligned, opaque);
+ * hd_ckpt_load gives the rows back as q * s, rounded once to dt.
+ *
+ * hd_ckpt_class_grad: the gradient of scores S = H C^T with respect to the class
+ * vectors, from the scores' gradient dS[N][K] (row stride lds) and the
+ * checkpoint of H:
+ *   dC[k][d] = sum_n dS[n][k] * (q s)[n][d]      fp32 [K][D], contiguous;
+ * accumulate != 0 adds to what dC holds. Products are exact, sums fp32.
+ * workspace: hd_ckpt_class_grad_workspace_bytes(...) bytes, contents irrelevant
+ * before and undefined after the call.
+ * Limits: N <= 65535 * 64, D <= 2^30, K <= 2^20, and ceil(N/64) * ceil(K/32) < 2^23.
+ */
+size_t hd_ckpt_bytes(int64_t N, int64_t D);
+hd_status hd_ckpt_store(const void *H, int64_t ldh, int64_t N, int64_t D, hd_dtype dt, void *image,
+                        size_t image_bytes, hipStream_t stream);
+hd_status hd_ckpt_load(const void *image, void *H, int64_t ldh, int64_t N, int64_t D, hd_dtype dt,
+                       hipStream_t stream);
+size_t hd_ckpt_class_grad_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
+hd_status hd_ckpt_class_grad(const void *dS, int64_t lds, const void *image, float *dC, int64_t N,
+                             int64_t D, int64_t K, hd_dtype dt, int accumulate, void *workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,11 @@ library is missing, importing a function raises.
 Operation (ScalableHD, Alg. 1): H = HardSign(X B) (Eq. 7, Eq. 1),
 S = H C^T (Eq. 8), labels = argmax_k S (Eq. 9). Single-pass training
 (Sec. II-C): C = HardSign of the per-class sums of HardSign(X B).
+
+Behind an answer: products with 4-bit weights (``nibble_*``) and log
+probabilities with entropy and alternatives (``logprobs``). Behind learning:
+their gradient (``logprobs_grad``) and encodings kept in 8 bits, from which the
+class vectors' gradient is read (``ckpt_*``).
 """
 from __future__ import annotations
 
@@ -15,6 +20,7 @@ import ctypes
 import functools
 import os
 import threading
+from typing import NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libhd.so")
@@ -43,6 +49,19 @@ SYMBOLS = (
     "hd_class_hardsign",
     "hd_bundle_classes_packed",
     "hd_bundle_kernel",
+    "hd_nibble_bytes",
+    "hd_nibble_pack",
+    "hd_nibble_quantize",
+    "hd_nibble_unpack",
+    "hd_nibble_product",
+    "hd_logprobs_workspace_bytes",
+    "hd_logprobs",
+    "hd_logprobs_grad",
+    "hd_ckpt_bytes",
+    "hd_ckpt_store",
+    "hd_ckpt_load",
+    "hd_ckpt_class_grad_workspace_bytes",
+    "hd_ckpt_class_grad",
 )
 
 _lib = None
@@ -107,6 +126,36 @@ def lib():
         L.hd_bundle_classes_packed.restype = i32
         L.hd_bundle_kernel.argtypes = [i64, i64, i64, i64, i32, i32]
         L.hd_bundle_kernel.restype = ctypes.c_char_p
+        f32 = ctypes.c_float
+        L.hd_nibble_bytes.argtypes = [i64, i64, i64]
+        L.hd_nibble_bytes.restype = sz
+        L.hd_nibble_pack.argtypes = [vp, vp, vp, i64, i64, i64, vp, sz, vp]
+        L.hd_nibble_pack.restype = i32
+        L.hd_nibble_quantize.argtypes = [vp, i64, i32, i32, i64, i64, i64, i32, vp, sz, vp]
+        L.hd_nibble_quantize.restype = i32
+        L.hd_nibble_unpack.argtypes = [vp, i32, vp, i64, i64, i64, vp]
+        L.hd_nibble_unpack.restype = i32
+        L.hd_nibble_product.argtypes = [vp, i64, vp, i32, vp, i64, i64, i64, i64, i64, i32, i32,
+                                        i32, vp]
+        L.hd_nibble_product.restype = i32
+        L.hd_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
+        L.hd_logprobs_workspace_bytes.restype = sz
+        L.hd_logprobs.argtypes = [vp, i64, vp, i64, vp, f32, vp, vp, vp, vp, vp, i64, i64, i64,
+                                  i32, vp, sz, vp]
+        L.hd_logprobs.restype = i32
+        L.hd_logprobs_grad.argtypes = [vp, i64, vp, i64, vp, f32, vp, vp, vp, vp, vp, i64, i64,
+                                       i64, i32, vp]
+        L.hd_logprobs_grad.restype = i32
+        L.hd_ckpt_bytes.argtypes = [i64, i64]
+        L.hd_ckpt_bytes.restype = sz
+        L.hd_ckpt_store.argtypes = [vp, i64, i64, i64, i32, vp, sz, vp]
+        L.hd_ckpt_store.restype = i32
+        L.hd_ckpt_load.argtypes = [vp, vp, i64, i64, i64, i32, vp]
+        L.hd_ckpt_load.restype = i32
+        L.hd_ckpt_class_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.hd_ckpt_class_grad_workspace_bytes.restype = sz
+        L.hd_ckpt_class_grad.argtypes = [vp, i64, vp, vp, i64, i64, i64, i32, i32, vp, sz, vp]
+        L.hd_ckpt_class_grad.restype = i32
         _lib = L
         return L
 
@@ -477,3 +526,299 @@ def train(X, B, y, K: int):
     """Single-pass training in one call: M [K, D] float32 = class_hardsign(
     bundle_classes(X, B, y, K))."""
     return class_hardsign(bundle_classes(X, B, y, K))
+
+
+# ---- Operators behind answers and learning ------------------------------------------------
+
+
+def _check_rows(t, name: str, dtypes):
+    """A matrix on the GPU whose rows are contiguous; returns its row stride."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    # (the stride of a single row or of none is not used, and may be anything)
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name} must not have overlapping rows")
+    return ld
+
+
+def _check_vec(t, name: str, dtype, n: int, device):
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n}")
+
+
+def _floats():
+    torch = _torch()
+    return (torch.float32, torch.bfloat16)
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+class NibbleWeights:
+    """A matrix in 4 bits with group scales, laid out once (opaque device image)."""
+
+    def __init__(self, image, outer: int, inner: int, group: int, zeros: bool):
+        self.image, self.outer, self.inner = image, outer, inner
+        self.group, self.zeros = group, zeros
+
+
+def _nibble_image(outer: int, inner: int, group: int, device):
+    torch = _torch()
+    nbytes = int(lib().hd_nibble_bytes(outer, inner, group))
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def nibble_pack(codes, scales, zeros=None, inner: int = 0, group: int = 64) -> NibbleWeights:
+    """4-bit weights from given codes: ``codes`` [outer, ceil(inner/2)] uint8 (input
+    2j in the low half of byte j), ``scales`` [outer, ceil(inner/group)] bfloat16,
+    ``zeros`` the same shape uint8 (0..15) or None (8 everywhere). ``inner`` 0
+    stands for twice the bytes of a row."""
+    torch = _torch()
+    _check_dev(codes, scales)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
+        raise TypeError("codes must be uint8 and scales bfloat16")
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError("codes and scales must be matrices")
+    outer, half = codes.shape
+    inner = inner or 2 * half
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    groups = -(-inner // group)
+    if half != -(-inner // 2) or tuple(scales.shape) != (outer, groups):
+        raise ValueError("shape mismatch")
+    if zeros is not None:
+        _check_dev(zeros)
+        if zeros.dtype != torch.uint8:
+            raise TypeError("zeros must be uint8")
+        if tuple(zeros.shape) != (outer, groups):
+            raise ValueError("shape mismatch")
+    image, nbytes = _nibble_image(outer, inner, group, codes.device)
+    st = lib().hd_nibble_pack(codes.data_ptr(), scales.data_ptr(), _ptr(zeros), outer, inner,
+                              group, image.data_ptr(), nbytes, _stream_ptr(codes.device))
+    _raise(st, "hd_nibble_pack")
+    return NibbleWeights(image, outer, inner, group, zeros is not None)
+
+
+def nibble_quantize(W, group: int = 64, inner_rows: bool = False,
+                    zeros: bool = False) -> NibbleWeights:
+    """4-bit weights from numbers: ``W`` [outer, inner] (class hypervectors), or with
+    ``inner_rows`` [inner, outer] (base hypervectors B[F, D]); float32 or bfloat16.
+    ``zeros``: min-max codes with zero points instead of symmetric ones."""
+    ld = _check_rows(W, "W", _floats())
+    outer, inner = (W.shape[1], W.shape[0]) if inner_rows else W.shape
+    image, nbytes = _nibble_image(outer, inner, group, W.device)
+    st = lib().hd_nibble_quantize(W.data_ptr(), ld, int(inner_rows), int(zeros), outer, inner,
+                                  group, _dt(W), image.data_ptr(), nbytes, _stream_ptr(W.device))
+    _raise(st, "hd_nibble_quantize")
+    return NibbleWeights(image, outer, inner, group, bool(zeros))
+
+
+def nibble_unpack(w: NibbleWeights):
+    """The weights that ``w`` stands for: [outer, inner] float32."""
+    torch = _torch()
+    W = torch.empty((w.outer, w.inner), dtype=torch.float32, device=w.image.device)
+    st = lib().hd_nibble_unpack(w.image.data_ptr(), int(w.zeros), W.data_ptr(), w.outer, w.inner,
+                                w.group, _stream_ptr(w.image.device))
+    _raise(st, "hd_nibble_unpack")
+    return W
+
+
+def nibble_product(X, w: NibbleWeights, act: str = "identity", dtype=None, out=None):
+    """Y[N, outer] = act(X w^T) for X [N, inner] float32 or bfloat16; ``dtype`` of Y
+    defaults to X's. ``act`` "hardsign" encodes (Stage I on 4-bit base vectors)."""
+    torch = _torch()
+    ldx = _check_rows(X, "X", _floats())
+    N, inner = X.shape
+    if inner != w.inner:
+        raise ValueError("shape mismatch")
+    if X.device != w.image.device:
+        raise ValueError("X and the weights must be on one device")
+    if out is None:
+        out = torch.empty((N, w.outer), dtype=dtype or X.dtype, device=X.device)
+    elif out.device != X.device or tuple(out.shape) != (N, w.outer):
+        raise ValueError("out must be [N, outer] on X's device")
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError("out has another dtype")
+    ldy = _check_rows(out, "out", _floats())
+    st = lib().hd_nibble_product(X.data_ptr(), ldx, w.image.data_ptr(), int(w.zeros),
+                                 out.data_ptr(), ldy, N, w.outer, inner, w.group, _dt(X),
+                                 _dt(out), ACTS[act], _stream_ptr(X.device))
+    _raise(st, "hd_nibble_product")
+    return out
+
+
+class LogProbs(NamedTuple):
+    """What ``logprobs`` gives for N rows: ``logp`` [N] (None without ``y``),
+    ``entropy`` [N], ``stats`` [N, 2] (the largest score m, and log sum exp
+    scale (s - m)), ``ids`` and ``top_logp`` [N, top] (None for top 0)."""
+    logp: object
+    entropy: object
+    stats: object
+    ids: object
+    top_logp: object
+
+
+def _mask_arg(mask, N: int, K: int, device):
+    """Pointer and row stride of a mask [K] or [N, K] (bool or uint8)."""
+    torch = _torch()
+    if mask is None:
+        return None, 0
+    if mask.device != device:
+        raise ValueError("mask must be on the scores' device")
+    if mask.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("mask must be bool or uint8")
+    if tuple(mask.shape) == (K,) and (K == 1 or mask.stride(0) == 1):
+        return mask.data_ptr(), 0
+    if tuple(mask.shape) != (N, K):
+        raise ValueError("mask must be [K] or [N, K]")
+    if N > 1 and mask.stride(0) == 0 and (K == 1 or mask.stride(1) == 1):
+        return mask.data_ptr(), 0  # one row, expanded
+    return mask.data_ptr(), _check_rows(mask, "mask", (torch.bool, torch.uint8))
+
+
+def logprobs_workspace_bytes(N: int, K: int, dtype) -> int:
+    return int(lib().hd_logprobs_workspace_bytes(N, K, _dt_of(dtype)))
+
+
+def logprobs(scores, y=None, top: int = 0, scale: float = 1.0, mask=None,
+             workspace=None) -> LogProbs:
+    """Log probabilities of the classes ``y`` [N] int32 (outside [0, K): none asked
+    for) under softmax(scale * scores), scores [N, K] float32 or bfloat16, with
+    the entropy and the ``top`` (up to 32) best alternatives. ``mask`` [K] or [N, K]:
+    classes that are False take no part. ``workspace`` may be a zeroed uint8
+    device tensor of ``logprobs_workspace_bytes(...)`` bytes."""
+    torch = _torch()
+    ld = _check_rows(scores, "scores", _floats())
+    N, K = scores.shape
+    device = scores.device
+    if y is not None:
+        _check_vec(y, "y", torch.int32, N, device)
+    mptr, ldm = _mask_arg(mask, N, K, device)
+    dt = _dt(scores)
+    # logp, entropy and stats, and the alternatives, in one allocation each
+    f = torch.empty(4 * N, dtype=torch.float32, device=device)
+    entropy, stats = f[2 * N:3 * N], f[:2 * N].view(N, 2)
+    logp = f[3 * N:] if y is not None else None
+    ids = torch.empty((N, top), dtype=torch.int32, device=device) if top > 0 else None
+    best = torch.empty((N, top), dtype=torch.float32, device=device) if top > 0 else None
+    need = _need("hd_logprobs_workspace_bytes", device.index, N, K, dt)
+    ws = workspace if workspace is not None else _workspace(device, need, ("logprobs", N, K, dt))
+    st = lib().hd_logprobs(scores.data_ptr(), ld, mptr, ldm, _ptr(y), scale, _ptr(logp),
+                           entropy.data_ptr(), stats.data_ptr(), _ptr(ids), _ptr(best), N, K, top,
+                           dt, _ptr(ws), ws.numel() if ws is not None else 0,
+                           _stream_ptr(device))
+    _raise(st, "hd_logprobs")
+    return LogProbs(logp, entropy, stats, ids, best)
+
+
+def logprobs_grad(scores, y, lp: LogProbs, g_logp=None, g_entropy=None, scale: float = 1.0,
+                  mask=None, out=None):
+    """The gradient of sum(g_logp * logp + g_entropy * entropy) with respect to the
+    scores, [N, K] of their dtype; ``lp`` is what ``logprobs`` gave for the same
+    scores, scale and mask. ``out`` may be the scores themselves."""
+    torch = _torch()
+    ld = _check_rows(scores, "scores", _floats())
+    N, K = scores.shape
+    device = scores.device
+    if y is not None:
+        _check_vec(y, "y", torch.int32, N, device)
+    for t, name in ((g_logp, "g_logp"), (g_entropy, "g_entropy"), (lp.entropy, "entropy")):
+        if t is not None:
+            _check_vec(t, name, torch.float32, N, device)
+    if (tuple(lp.stats.shape) != (N, 2) or lp.stats.dtype != torch.float32
+            or not lp.stats.is_contiguous() or lp.stats.device != device):
+        raise ValueError("stats must be float32 [N, 2] on the scores' device")
+    mptr, ldm = _mask_arg(mask, N, K, device)
+    if out is None:
+        out = torch.empty((N, K), dtype=scores.dtype, device=device)
+    elif tuple(out.shape) != (N, K) or out.dtype != scores.dtype or out.device != device:
+        raise ValueError("out must have the scores' shape, dtype and device")
+    ldd = _check_rows(out, "out", _floats())
+    st = lib().hd_logprobs_grad(scores.data_ptr(), ld, mptr, ldm, _ptr(y), scale,
+                                lp.stats.data_ptr(), lp.entropy.data_ptr(), _ptr(g_logp),
+                                _ptr(g_entropy), out.data_ptr(), ldd, N, K, _dt(scores),
+                                _stream_ptr(device))
+    _raise(st, "hd_logprobs_grad")
+    return out
+
+
+class Checkpoint:
+    """Activations [N, D] kept in 8 bits (opaque device image)."""
+
+    def __init__(self, image, N: int, D: int):
+        self.image, self.N, self.D = image, N, D
+
+
+def ckpt_store(H, out=None) -> Checkpoint:
+    """Keeps activations ``H`` [N, D] (float32 or bfloat16) in 8 bits, 64 rows of a
+    column sharing a scale. ``out``: a Checkpoint of the same sizes to overwrite."""
+    torch = _torch()
+    ld = _check_rows(H, "H", _floats())
+    N, D = H.shape
+    if out is None:
+        out = Checkpoint(torch.empty(int(lib().hd_ckpt_bytes(N, D)), dtype=torch.uint8,
+                                     device=H.device), N, D)
+    elif (out.N, out.D) != (N, D) or out.image.device != H.device:
+        raise ValueError("out must be a checkpoint of H's sizes on its device")
+    st = lib().hd_ckpt_store(H.data_ptr(), ld, N, D, _dt(H), out.image.data_ptr(),
+                             out.image.numel(), _stream_ptr(H.device))
+    _raise(st, "hd_ckpt_store")
+    return out
+
+
+def ckpt_load(kept: Checkpoint, dtype=None, out=None):
+    """The activations a checkpoint stands for, [N, D] (float32 unless ``dtype`` or
+    ``out`` says bfloat16)."""
+    torch = _torch()
+    N, D = kept.N, kept.D
+    if out is None:
+        out = torch.empty((N, D), dtype=dtype or torch.float32, device=kept.image.device)
+    elif tuple(out.shape) != (N, D) or out.device != kept.image.device:
+        raise ValueError("out must be [N, D] on the checkpoint's device")
+    ld = _check_rows(out, "out", _floats())
+    st = lib().hd_ckpt_load(kept.image.data_ptr(), out.data_ptr(), ld, N, D, _dt(out),
+                            _stream_ptr(out.device))
+    _raise(st, "hd_ckpt_load")
+    return out
+
+
+def ckpt_class_grad(dS, kept: Checkpoint, out=None, accumulate: bool = False):
+    """The class vectors' gradient dC[K, D] float32 = dS^T H from the scores' gradient
+    ``dS`` [N, K] (float32 or bfloat16) and the checkpoint of the encodings H.
+    ``out`` receives it, or with ``accumulate`` has it added."""
+    torch = _torch()
+    ld = _check_rows(dS, "dS", _floats())
+    N, K = dS.shape
+    D = kept.D
+    if N != kept.N:
+        raise ValueError("shape mismatch")
+    if dS.device != kept.image.device:
+        raise ValueError("dS and the checkpoint must be on one device")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((K, D), dtype=torch.float32, device=dS.device)
+    else:
+        _check_dev(out)
+        if out.dtype != torch.float32 or tuple(out.shape) != (K, D) or out.device != dS.device:
+            raise ValueError("out must be float32 [K, D] on dS's device")
+    need = _need("hd_ckpt_class_grad_workspace_bytes", dS.device.index, N, D, K, _dt(dS))
+    ws = torch.empty(need, dtype=torch.uint8, device=dS.device)
+    st = lib().hd_ckpt_class_grad(dS.data_ptr(), ld, kept.image.data_ptr(), out.data_ptr(), N, D,
+                                  K, _dt(dS), int(accumulate), ws.data_ptr(), ws.numel(),
+                                  _stream_ptr(dS.device))
+    _raise(st, "hd_ckpt_class_grad")
+    return out

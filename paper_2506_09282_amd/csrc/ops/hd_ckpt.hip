@@ -1,0 +1,423 @@
+// Activations kept in 8 bits, and the class vectors' gradient read from them.
+//
+// A group is kCkptRows rows of one column d:
+//   s = max |x| / 127 (times the fp32 nearest to 1/127),  q = rint(x * (1/s)) in -127..127,
+// and a kept value stands for q * s. Columns, not rows, share a scale, because
+// activations differ in size from channel to channel. A group that holds an
+// infinity or NaN is kept as NaN.
+//
+//   dC[k,d] = sum over groups b of s[b,d] * sum_{n in b} dS[n,k] q[n,d]
+//
+// The column scale leaves the product's reduction (over n) alone: q goes to the
+// bf16 matrix instruction as it is (8 bits, exact), bf16 dS too, and fp32 dS as
+// the exact sum of three bf16 values; s multiplies the finished group in fp32. What bounds
+// it is reading q once, N*D bytes, while K is small.
+//
+// Layout: [group of rows][16 rows of the group][column][16 bytes], then the scales
+// [group][column]. A lane's 16-byte load is 16 rows of a column, half an operand pair of
+// v_mfma_f32_32x32x16_bf16, neighbouring lanes are neighbouring columns, and
+// storing is coalesced too. dS is first cut and laid out as the other
+// operand (a small launch), so that the product's loop holds no transposition.
+#include "hd_ops.hpp"
+
+namespace hd {
+namespace ops {
+
+namespace {
+
+constexpr int kRows = kCkptRows;
+constexpr float kInv127 = 1.0f / 127.0f;
+
+__host__ __device__ inline int64_t groups_of(int64_t N) { return cdiv(N, kRows); }
+__host__ __device__ inline int64_t scales_at(int64_t N, int64_t D) {
+  return (groups_of(N) * kRows * D + 255) / 256 * 256;
+}
+
+// ---- store and load --------------------------------------------------------------
+
+// COLS columns to a thread (2: bf16 pairs, 4-byte loads).
+template <typename T, int COLS>
+__global__ __launch_bounds__(256) void ckpt_store_kernel(const T* __restrict__ H, int64_t ldh,
+                                                         int64_t N, int64_t D, u32x4* out,
+                                                         float* out_s) {
+  const int64_t d = ((int64_t)blockIdx.x * 256 + threadIdx.x) * COLS;
+  if (d >= D) return;
+  const int64_t b = blockIdx.y, n0 = b * kRows;
+  const bool pair = COLS == 2 && d + 1 < D;
+  float v[COLS][kRows];
+  const T* p = H + n0 * ldh + d;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const bool in = n0 + r < N;
+    if constexpr (COLS == 2) {
+      uint32_t w = 0;
+      if (in) w = pair ? *reinterpret_cast<const uint32_t*>(p + r * ldh) : p[r * ldh];
+      v[0][r] = __uint_as_float(w << 16);
+      v[1][r] = __uint_as_float(w & 0xffff0000u);
+    } else {
+      v[0][r] = in ? load_elem(p, r * ldh) : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) {
+    if (c == 1 && !pair) break;
+    uint32_t top = 0;  // as bits, an infinity and NaN are larger than any number
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const uint32_t a = __float_as_uint(v[c][r]) & 0x7fffffffu;
+      top = a > top ? a : top;
+    }
+    const bool bad = top >= 0x7f800000u;
+    const float s = __uint_as_float(top) * kInv127;
+    float inv = 1.0f / s;
+    if (bad || !(inv < INFINITY)) inv = 0.0f;  // 0, or too small for its inverse: kept as 0
+#pragma unroll
+    for (int ch = 0; ch < kRows / 16; ++ch) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float q = rintf((bad ? 0.0f : v[c][ch * 16 + 4 * i + e]) * inv);
+          w[i] |= ((uint32_t)(int)fminf(fmaxf(q, -127.0f), 127.0f) & 255u) << (8 * e);
+        }
+      }
+      out[(b * 4 + ch) * D + d + c] = w;
+    }
+    out_s[b * D + d + c] = bad ? NAN : s;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void ckpt_load_kernel(const u32x4* __restrict__ q,
+                                                        const float* __restrict__ scale, T* H,
+                                                        int64_t ldh, int64_t N, int64_t D) {
+  const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (d >= D) return;
+  const int64_t b = blockIdx.y;
+  const float s = scale[b * D + d];
+  u32x4 w[kRows / 16];
+#pragma unroll
+  for (int ch = 0; ch < kRows / 16; ++ch) w[ch] = q[(b * 4 + ch) * D + d];
+#pragma unroll
+  for (int ch = 0; ch < kRows / 16; ++ch)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int64_t n = b * kRows + ch * 16 + e;
+      if (n < N) store_elem(H, n * ldh + d, (float)(int8_t)(w[ch][e / 4] >> (8 * (e % 4))) * s);
+    }
+}
+
+// ---- the other operand --------------------------------------------------------------
+
+// dS as operand fragments: [group][tile of 32 classes][8 rows of half a wave: p, j]
+// [part][lane][16 bytes]; lane l holds class l % 32, rows 32 p + 16 (l / 32) + 8 j + e.
+template <typename T>
+struct DsParts;
+template <>
+struct DsParts<float> {
+  static constexpr int kParts = 3;
+};
+template <>
+struct DsParts<bf16raw> {
+  static constexpr int kParts = 1;
+};
+constexpr int kSteps = kRows / 16;  // matrix steps of a group
+
+template <typename T>
+__global__ __launch_bounds__(256) void ckpt_grad_operand_kernel(const T* __restrict__ dS,
+                                                                int64_t lds, int64_t N, int K,
+                                                                int ktiles, int64_t total,
+                                                                u32x4* out) {
+  constexpr int P = DsParts<T>::kParts;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  const int lane = (int)(at & 63), step = (int)(at >> 6) % kSteps;
+  const int64_t bt = (at >> 6) / kSteps;
+  const int kt = (int)(bt % ktiles);
+  const int64_t b = bt / ktiles;
+  const int k = 32 * kt + lane % 32;
+  const int64_t n0 = b * kRows + 32 * (step / 2) + 16 * (lane / 32) + 8 * (step % 2);
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    v[e] = (k < K && n0 + e < N) ? load_elem(dS, (n0 + e) * lds + k) : 0.0f;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t a = __float_as_uint(v[2 * e]), c = __float_as_uint(v[2 * e + 1]);
+      w[e] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+      // what is left; nothing of an infinity or NaN, whose first part says all
+      v[2 * e] = (a & 0x7f800000u) == 0x7f800000u ? 0.0f
+                                                  : v[2 * e] - __uint_as_float(a & 0xffff0000u);
+      v[2 * e + 1] = (c & 0x7f800000u) == 0x7f800000u
+                         ? 0.0f
+                         : v[2 * e + 1] - __uint_as_float(c & 0xffff0000u);
+      // (a NaN whose upper half alone would read as an infinity)
+      if (P == 3 && p == 0) {
+        if ((a & 0x7fffffffu) > 0x7f800000u) w[e] |= 0x00000040u;
+        if ((c & 0x7fffffffu) > 0x7f800000u) w[e] |= 0x00400000u;
+      }
+    }
+    out[((bt * kSteps + step) * P + p) * 64 + lane] = w;
+  }
+}
+
+// ---- the gradient -----------------------------------------------------------------
+
+__device__ __forceinline__ bf16x8 bytes_bf16(uint32_t a, uint32_t b) {
+  u32x4 v;
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = (float)(int8_t)(a >> (8 * e));
+    f[4 + e] = (float)(int8_t)(b >> (8 * e));
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    v[e] = __builtin_amdgcn_perm(__float_as_uint(f[2 * e + 1]), __float_as_uint(f[2 * e]),
+                                 0x07060302u);
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// Four waves; each takes DT tiles of 32 columns and KT tiles of 32 classes over a
+// slice of the groups. The waves share the dS operand through LDS.
+template <int P, int KT, int DT>
+__global__ __launch_bounds__(256) void ckpt_class_grad_kernel(
+    const u32x4* __restrict__ q, const float* __restrict__ scale, const u32x4* __restrict__ ds,
+    float* __restrict__ out, int64_t D, int K, int ktiles, int64_t groups, int64_t per_slice,
+    int64_t slice_stride, int accumulate) {
+  constexpr int OPS = KT * kSteps * P;  // operand fragments of a group
+  __shared__ u32x4 op[2][OPS * 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 31, half = lane >> 5;
+  const int64_t d0 = ((int64_t)blockIdx.x * 4 + wave) * (32 * DT);
+  const int kt0 = blockIdx.y * KT;
+  const int64_t b0 = (int64_t)blockIdx.z * per_slice;
+  const int64_t b1 = b0 + per_slice < groups ? b0 + per_slice : groups;
+  int64_t dcol[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) {
+    const int64_t d = d0 + 32 * t + col;
+    dcol[t] = d < D ? d : D - 1;  // columns past D: any, never written
+  }
+  f32x16 acc[KT][DT];
+#pragma unroll
+  for (int k = 0; k < KT; ++k)
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[k][t][r] = 0.0f;
+
+  // class tiles past the last repeat it (their results are not written)
+  auto operand_at = [&](int64_t b, int i) {
+    const int k = i / (kSteps * P * 64);
+    const int kt = kt0 + k < ktiles ? kt0 + k : ktiles - 1;
+    return ((b * ktiles + kt) * kSteps * P) * 64 + i % (kSteps * P * 64);
+  };
+  constexpr int PER = (OPS * 64 + 255) / 256;
+  u32x4 stage[PER];
+  auto fetch = [&](int64_t b) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      if (OPS * 64 % 256 == 0 || at < OPS * 64) stage[i] = ds[operand_at(b, at)];
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      if (OPS * 64 % 256 == 0 || at < OPS * 64) op[buf][at] = stage[i];
+    }
+  };
+  if (b0 < b1) {
+    fetch(b0);
+    put(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int64_t b = b0; b < b1; ++b, buf ^= 1) {
+    u32x4 w[DT][2];
+    float s[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) w[t][p] = q[(b * 4 + 2 * p + half) * D + dcol[t]];
+      s[t] = scale[b * D + dcol[t]];
+    }
+    if (b + 1 < b1) fetch(b + 1);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      bf16x8 qb[kSteps];
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+        qb[i] = bytes_bf16(w[t][i / 2][2 * (i % 2)], w[t][i / 2][2 * (i % 2) + 1]);
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        f32x16 g;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g[r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+            g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8, op[buf][((k * kSteps + i) * P + p) * 64 + lane]), qb[i],
+                g, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[k][t][r] = fmaf(s[t], g[r], acc[k][t][r]);
+      }
+    }
+    if (b + 1 < b1) put(buf ^ 1);
+    __syncthreads();
+  }
+  float* dst = out + (int64_t)blockIdx.z * slice_stride;
+#pragma unroll
+  for (int k = 0; k < KT; ++k)
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const int64_t d = d0 + 32 * t + col;
+      if (d >= D) continue;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int cls = 32 * (kt0 + k) + 8 * (r / 4) + 4 * half + r % 4;
+        if (cls >= K) continue;
+        float* at = dst + (int64_t)cls * D + d;
+        *at = accumulate ? *at + acc[k][t][r] : acc[k][t][r];
+      }
+    }
+}
+
+__global__ __launch_bounds__(256) void ckpt_grad_join_kernel(const float* __restrict__ part,
+                                                             float* __restrict__ dC,
+                                                             int64_t total, int slices,
+                                                             int accumulate) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= total) return;
+  float v = part[i];
+  for (int s = 1; s < slices; ++s) v += part[s * total + i];
+  dC[i] = accumulate ? dC[i] + v : v;
+}
+
+struct GradPlan {
+  int ktiles, kt, kblocks;  // class tiles, those of a workgroup, workgroups along K
+  int64_t dblocks, per_slice;
+  int slices;
+  size_t operand, total;  // bytes of the dS operand, and with the partial sums
+};
+
+constexpr int kGradDT = 2;
+
+GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
+  GradPlan p;
+  p.ktiles = (int)cdiv(K, 32);
+  p.kt = p.ktiles >= 2 ? 2 : 1;
+  p.kblocks = (int)cdiv(p.ktiles, p.kt);
+  p.dblocks = cdiv(D, 4 * 32 * kGradDT);
+  const int64_t groups = groups_of(N);
+  int64_t slices = cdiv(3 * (int64_t)num_cus(), p.dblocks * p.kblocks);
+  if (slices > groups / 4) slices = groups / 4;
+  if (slices < 1) slices = 1;
+  p.per_slice = cdiv(groups, slices);
+  p.slices = (int)cdiv(groups, p.per_slice);
+  const int parts = dt == 0 ? DsParts<float>::kParts : DsParts<bf16raw>::kParts;
+  p.operand = (size_t)groups * p.ktiles * kSteps * parts * 1024;
+  p.total = p.operand + (p.slices > 1 ? (size_t)p.slices * K * D * 4 : 0);
+  return p;
+}
+
+template <typename T, int KT>
+void launch_grad_kernel(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
+                        float* out, int64_t D, int K, int64_t groups, bool accumulate,
+                        hipStream_t stream) {
+  hipLaunchKernelGGL((ckpt_class_grad_kernel<DsParts<T>::kParts, KT, kGradDT>),
+                     dim3((unsigned)p.dblocks, (unsigned)p.kblocks, (unsigned)p.slices), dim3(256),
+                     0, stream, q, s, ds, out, D, K, p.ktiles, groups, p.per_slice,
+                     (int64_t)K * D, (int)(accumulate && p.slices == 1));
+}
+
+template <typename T>
+hipError_t launch_grad_typed(const void* dS, int64_t lds, const void* image, float* dC, int64_t N,
+                             int64_t D, int64_t K, bool accumulate, const GradPlan& p,
+                             void* workspace, hipStream_t stream) {
+  const int64_t groups = groups_of(N);
+  u32x4* operand = static_cast<u32x4*>(workspace);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.operand);
+  const int64_t total = groups * p.ktiles * kSteps * 64;
+  hipLaunchKernelGGL(ckpt_grad_operand_kernel<T>, dim3((unsigned)cdiv(total, 256)), dim3(256), 0,
+                     stream, static_cast<const T*>(dS), lds, N, (int)K, p.ktiles, total, operand);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const u32x4* q = static_cast<const u32x4*>(image);
+  const float* s =
+      reinterpret_cast<const float*>(static_cast<const char*>(image) + scales_at(N, D));
+  float* out = p.slices > 1 ? part : dC;
+  if (p.kt == 1)
+    launch_grad_kernel<T, 1>(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
+  else
+    launch_grad_kernel<T, 2>(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.slices == 1) return e;
+  hipLaunchKernelGGL(ckpt_grad_join_kernel, dim3((unsigned)cdiv(K * D, 256)), dim3(256), 0, stream,
+                     part, dC, K * D, p.slices, (int)accumulate);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t ckpt_image_bytes(int64_t N, int64_t D) {
+  return (size_t)scales_at(N, D) + (size_t)(groups_of(N) * D) * 4;
+}
+
+hipError_t launch_ckpt_store(const void* H, int64_t ldh, int64_t N, int64_t D, int dt,
+                             void* image, hipStream_t stream) {
+  u32x4* q = static_cast<u32x4*>(image);
+  float* s = reinterpret_cast<float*>(static_cast<char*>(image) + scales_at(N, D));
+  const unsigned groups = (unsigned)groups_of(N);
+  if (dt == 0)
+    hipLaunchKernelGGL((ckpt_store_kernel<float, 1>), dim3((unsigned)cdiv(D, 256), groups),
+                       dim3(256), 0, stream, static_cast<const float*>(H), ldh, N, D, q, s);
+  else if (ldh % 2 == 0 && (uintptr_t)H % 4 == 0)
+    hipLaunchKernelGGL((ckpt_store_kernel<bf16raw, 2>), dim3((unsigned)cdiv(D, 512), groups),
+                       dim3(256), 0, stream, static_cast<const bf16raw*>(H), ldh, N, D, q, s);
+  else
+    hipLaunchKernelGGL((ckpt_store_kernel<bf16raw, 1>), dim3((unsigned)cdiv(D, 256), groups),
+                       dim3(256), 0, stream, static_cast<const bf16raw*>(H), ldh, N, D, q, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_ckpt_load(const void* image, void* H, int64_t ldh, int64_t N, int64_t D, int dt,
+                            hipStream_t stream) {
+  const u32x4* q = static_cast<const u32x4*>(image);
+  const float* s =
+      reinterpret_cast<const float*>(static_cast<const char*>(image) + scales_at(N, D));
+  const dim3 grid((unsigned)cdiv(D, 256), (unsigned)groups_of(N));
+  if (dt == 0)
+    hipLaunchKernelGGL(ckpt_load_kernel<float>, grid, dim3(256), 0, stream, q, s,
+                       static_cast<float*>(H), ldh, N, D);
+  else
+    hipLaunchKernelGGL(ckpt_load_kernel<bf16raw>, grid, dim3(256), 0, stream, q, s,
+                       static_cast<bf16raw*>(H), ldh, N, D);
+  return hipGetLastError();
+}
+
+size_t ckpt_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt) {
+  return grad_plan(N, D, K, dt).total;
+}
+
+hipError_t launch_ckpt_class_grad(const void* dS, int64_t lds, const void* image, float* dC,
+                                  int64_t N, int64_t D, int64_t K, int dt, bool accumulate,
+                                  void* workspace, hipStream_t stream) {
+  const GradPlan p = grad_plan(N, D, K, dt);
+  return dt == 0 ? launch_grad_typed<float>(dS, lds, image, dC, N, D, K, accumulate, p, workspace,
+                                            stream)
+                 : launch_grad_typed<bf16raw>(dS, lds, image, dC, N, D, K, accumulate, p,
+                                              workspace, stream);
+}
+
+}  // namespace ops
+}  // namespace hd

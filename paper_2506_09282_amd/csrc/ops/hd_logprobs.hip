@@ -1,0 +1,625 @@
+// Log probabilities of given classes, with the entropy and the best alternatives:
+//   t_k = scale (s_k - m) - L,  m = max s,  L = log sum_k exp(scale (s_k - m)),
+//   logp = t_y,  entropy = -sum_k exp(t_k) t_k,  the T largest t with their classes
+// and the gradient of g logp + h entropy with respect to s:
+//   scale ( g (1[k=y] - p_k) - h p_k (t_k + entropy) ),  p = exp(t).
+//
+// The scores are read once: each thread keeps a running maximum, the sum of
+// exp and the sum of z exp(z), both rescaled when its maximum grows (all in fp32), so reading
+// the scores is the bound. The two halves m and L are kept apart,
+// because scale * m can be large against the differences that matter.
+//
+// What is masked, and -inf, contributes nothing whatever it holds. NaN or +inf among
+// the rest make the row's floats NaN and its alternatives -1.
+//
+// Alternatives: a score and its class make one 64-bit key, ordered by score and then by
+// lower class, so the choice is exact and does not depend on the order of the
+// work. In a long row each wave keeps a sorted list of keys, one in each lane; a chunk
+// whose largest score does not beat the list's T-th (almost every chunk) costs one
+// comparison.
+//
+// * up to kShortK classes: LPR lanes hold a row in registers.
+// * more: a workgroup walks a row, or a part of it where there are fewer rows than
+//   the chip has room for; the last workgroup to finish joins the parts in order.
+#include "hd_ops.hpp"
+
+namespace hd {
+namespace ops {
+
+namespace {
+
+constexpr int kShortK = 1024;
+constexpr int kLongThreads = 256;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kUnder = -300.0f;  // 2^kUnder is 0: keeps 0 * -inf out of the sums
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Keys: larger is better. 0 stands for no class.
+__device__ __forceinline__ uint64_t key_of(float s, uint32_t k) {
+  uint32_t b = __float_as_uint(s + 0.0f);  // -0 and +0 are one score
+  b ^= (b >> 31) ? 0xffffffffu : 0x80000000u;
+  return (uint64_t)b << 32 | (uint32_t)~k;
+}
+__device__ __forceinline__ float key_score(uint64_t key) {
+  const uint32_t b = (uint32_t)(key >> 32);
+  return __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int off) {
+  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, off, kWave);
+  const uint32_t hi = (uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), off, kWave);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
+
+// The running statistics of a part of a row. m is at least the lowest finite number, so
+// that -inf - m is -inf; the sum is 0 only where nothing was there.
+struct Stats {
+  float m, sum, ez;  // ez: sum of z exp(z), z in powers of two
+};
+__device__ __forceinline__ Stats stats_none() { return Stats{kLowest, 0.0f, 0.0f}; }
+__device__ __forceinline__ void stats_raise(Stats& a, float m, float c) {
+  const float d = fmaxf((a.m - m) * c, kUnder), f = exp2_fast(d);  // d <= 0
+  a.ez = f * fmaf(d, a.sum, a.ez);
+  a.sum *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Stats stats_join(Stats a, Stats b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  stats_raise(a, m, c);
+  stats_raise(b, m, c);
+  return Stats{m, a.sum + b.sum, a.ez + b.ez};
+}
+__device__ __forceinline__ void stats_add(Stats& a, float s, float c) {
+  const float z = (s - a.m) * c, e = exp2_fast(z);
+  a.sum += e;
+  a.ez = fmaf(e, fmaxf(z, kUnder), a.ez);  // (NaN is in e)
+}
+template <int LANES>
+__device__ __forceinline__ Stats stats_across(Stats a, float c) {
+#pragma unroll
+  for (int off = 1; off < LANES; off <<= 1) {
+    Stats b;
+    b.m = __shfl_xor(a.m, off, kWave);
+    b.sum = __shfl_xor(a.sum, off, kWave);
+    b.ez = __shfl_xor(a.ez, off, kWave);
+    // the same order in both lanes: the sums are commutative, so the bits agree
+    a = stats_join(a, b, c);
+  }
+  return a;
+}
+
+struct Row {  // a finished row
+  float m, logsum, entropy;
+  bool none, bad;
+};
+__device__ __forceinline__ Row finish(Stats a) {
+  Row r;
+  r.none = a.sum == 0.0f;
+  r.bad = a.sum != a.sum;
+  r.logsum = r.none ? 0.0f : logf(a.sum);
+  r.m = r.none ? -INFINITY : r.bad ? NAN : a.m;
+  r.entropy = r.none ? 0.0f : r.logsum - (a.ez * kLn2) / a.sum;
+  return r;
+}
+// log probability of a score in a finished row
+__device__ __forceinline__ float logp_of(const Row& r, float s, float scale) {
+  if (r.bad) return NAN;
+  if (r.none || s == -INFINITY) return -INFINITY;
+  return (s - r.m) * scale - r.logsum;
+}
+
+struct Out {
+  float *logp, *entropy, *stats;
+  int32_t* ids;
+  float* top_logp;
+  int top;
+};
+
+template <typename T>
+__device__ __forceinline__ void write_row(const Row& r, const T* row, const uint8_t* mrow,
+                                          const int32_t* y, int64_t n, int64_t K, float scale,
+                                          const Out& o) {
+  if (y) {
+    const int64_t k = y[n];
+    float lp = 0.0f;  // no class asked for
+    if (k >= 0 && k < K) {
+      const bool on = !mrow || mrow[k];
+      lp = logp_of(r, on ? load_elem(row, k) : -INFINITY, scale);
+    }
+    o.logp[n] = lp;
+  }
+  o.entropy[n] = r.bad ? NAN : r.entropy;
+  o.stats[2 * n] = r.m;
+  o.stats[2 * n + 1] = r.bad ? NAN : r.logsum;
+}
+__device__ __forceinline__ void write_top(const Row& r, uint64_t key, int64_t n, int j,
+                                          float scale, const Out& o) {
+  const bool there = key != 0 && !r.bad;
+  o.ids[n * o.top + j] = there ? (int32_t)~(uint32_t)key : -1;
+  o.top_logp[n * o.top + j] =
+      r.bad ? NAN : there ? logp_of(r, key_score(key), scale) : -INFINITY;
+}
+
+// ---- short rows ----------------------------------------------------------------
+
+// LPR lanes to a row, VPL scores in each lane (class lane + LPR j).
+template <typename T, int LPR, int VPL>
+__global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out o) {
+  const int lane = threadIdx.x & (LPR - 1);
+  const int64_t n = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const bool live = n < a.N;
+  const int64_t nn = live ? n : a.N - 1;  // lanes past the end follow along and write nothing
+  const T* row = static_cast<const T*>(a.scores) + nn * a.ld;
+  const uint8_t* mrow = a.mask ? a.mask + nn * a.ldm : nullptr;
+  const int K = (int)a.K;
+  float v[VPL];
+  Stats st = stats_none();
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int k = lane + LPR * j;
+    v[j] = k < K ? load_elem(row, k) : -INFINITY;
+    if (mrow && k < K && !mrow[k]) v[j] = -INFINITY;
+    st.m = fmaxf(st.m, v[j]);
+  }
+#pragma unroll
+  for (int off = 1; off < LPR; off <<= 1) st.m = fmaxf(st.m, __shfl_xor(st.m, off, kWave));
+  const float c = a.scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) stats_add(st, v[j], c);
+#pragma unroll
+  for (int off = 1; off < LPR; off <<= 1) {
+    st.sum += __shfl_xor(st.sum, off, kWave);
+    st.ez += __shfl_xor(st.ez, off, kWave);
+  }
+  const Row r = finish(st);
+  if (live && lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
+  if (o.top == 0) return;
+  uint64_t key[VPL];
+#pragma unroll
+  for (int j = 0; j < VPL; ++j)
+    key[j] = v[j] > -INFINITY ? key_of(v[j], (uint32_t)(lane + LPR * j)) : 0;
+  for (int t = 0; t < o.top; ++t) {
+    uint64_t best = 0;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) best = max64(best, key[j]);
+#pragma unroll
+    for (int off = 1; off < LPR; off <<= 1) best = max64(best, shfl_xor64(best, off));
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) key[j] = key[j] == best ? 0 : key[j];
+    if (live && lane == 0) write_top(r, best, n, t, a.scale, o);
+  }
+}
+
+// ---- long rows -----------------------------------------------------------------
+
+// Sorts one key per lane, largest first.
+__device__ __forceinline__ uint64_t sort64(uint64_t v, int lane) {
+  for (int size = 2; size <= 64; size <<= 1)
+    for (int off = size >> 1; off > 0; off >>= 1) {
+      const uint64_t w = shfl_xor64(v, off);
+      // descending blocks where the lane's `size` bit is clear (64: all of it)
+      const bool keep_max = ((lane & off) == 0) == ((lane & size) == 0 || size == 64);
+      v = keep_max ? max64(v, w) : min64(v, w);
+    }
+  return v;
+}
+// Lanes 0..31 hold a list, largest first, and lanes 32..63 another, smallest
+// first: the 64 keys, largest first.
+__device__ __forceinline__ uint64_t merge64(uint64_t v, int lane) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const uint64_t w = shfl_xor64(v, off);
+    v = (lane & off) == 0 ? max64(v, w) : min64(v, w);
+  }
+  return v;
+}
+
+// A wave's sorted list: lane j holds the (j+1)-th best key seen.
+struct TopList {
+  uint64_t key;
+  float bar;  // a score has to beat this to enter the first `top`
+};
+__device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ float list_bar(uint64_t key, int top) {
+  const uint64_t k = lane_key(key, top - 1);
+  return k ? key_score(k) : -INFINITY;
+}
+// Inserts a key that is the same in all lanes.
+__device__ __forceinline__ uint64_t list_insert(uint64_t list, uint64_t key, int lane) {
+  const int at = __popcll(__ballot(list > key));
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)list, 0x138, 0xf, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(list >> 32), 0x138, 0xf, 0xf, false);
+  const uint64_t up = (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;  // the lane below
+  return lane < at ? list : lane == at ? key : up;
+}
+
+template <typename T>
+struct Chunk {  // 16 bytes of scores
+  static constexpr int kLen = 16 / (int)sizeof(T);
+};
+
+__device__ __forceinline__ void load_chunk(const float* p, float (&v)[4]) {
+  const f32x4 x = *reinterpret_cast<const f32x4_a4*>(p);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = x[e];
+}
+__device__ __forceinline__ void load_chunk(const bf16raw* p, float (&v)[8]) {
+  const u32x4 x = *reinterpret_cast<const u32x4_a2*>(p);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[2 * e] = __uint_as_float(x[e] << 16);
+    v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+  }
+}
+typedef uint32_t u32_a1 __attribute__((aligned(1)));
+template <int LEN>
+__device__ __forceinline__ void mask_chunk(const uint8_t* p, float (&v)[LEN]) {
+#pragma unroll
+  for (int w = 0; w < LEN / 4; ++w) {
+    const uint32_t b = reinterpret_cast<const u32_a1*>(p)[w];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (!(b & (255u << (8 * e)))) v[4 * w + e] = -INFINITY;
+  }
+}
+
+// Joins the waves' statistics and lists of a workgroup; the result is whole in wave 0.
+template <bool TOP>
+__device__ __forceinline__ void join_waves(Stats& st, uint64_t& list, float c, int lane, int wave,
+                                           int waves, Stats* sh_st, uint64_t* sh_key) {
+  if (lane == 0) sh_st[wave] = st;
+  if (TOP && lane < kMaxTop) sh_key[wave * kMaxTop + lane] = list;
+  __syncthreads();
+  if (wave != 0) return;
+  st = sh_st[0];
+  for (int w = 1; w < waves; ++w) st = stats_join(st, sh_st[w], c);
+  if (TOP)
+    for (int w = 1; w < waves; ++w) {
+      const uint64_t other = sh_key[w * kMaxTop + (63 - lane) % kMaxTop];
+      list = merge64(lane < kMaxTop ? list : other, lane);
+    }
+}
+
+// Workspace of a split call: a counter for each row, then for each (row, part)
+// kPartWords words: m, sum, ez, and the list's keys.
+constexpr int kPartWords = 4 + 2 * kMaxTop;
+struct Split {
+  int parts;         // of a row
+  int64_t part_len;  // scores in a part, a multiple of the step of a workgroup
+  uint32_t *tickets, *words;
+};
+
+__device__ __forceinline__ uint32_t take_word(uint32_t* p) {
+  return __hip_atomic_exchange(p, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put_word(uint32_t* p, uint32_t v) {
+  (void)__hip_atomic_exchange(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <typename T, bool TOP, bool MASK>
+__global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArgs a, Out o,
+                                                                     Split sp) {
+  constexpr int LEN = Chunk<T>::kLen, WAVES = kLongThreads / 64;
+  __shared__ Stats sh_st[WAVES];
+  __shared__ uint64_t sh_key[WAVES * kMaxTop];
+  __shared__ uint32_t sh_last;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n = blockIdx.x / sp.parts;
+  const int part = (int)(blockIdx.x % sp.parts);
+  const T* row = static_cast<const T*>(a.scores) + n * a.ld;
+  const uint8_t* mrow = MASK ? a.mask + n * a.ldm : nullptr;
+  const float c = a.scale * kLog2e;
+  const int64_t k_end = (part + 1) * sp.part_len < a.K ? (part + 1) * sp.part_len : a.K;
+
+  Stats st = stats_none();
+  TopList list{0, -INFINITY};
+  bool first = true;
+  constexpr int STEP = kLongThreads * LEN;
+  for (int64_t k0 = part * sp.part_len; k0 < k_end; k0 += STEP) {
+    const int64_t k = k0 + (int64_t)threadIdx.x * LEN;
+    float v[LEN];
+    if (k + LEN <= k_end) {
+      load_chunk(row + k, v);
+      if (MASK) mask_chunk<LEN>(mrow + k, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < LEN; ++e) {
+        v[e] = k + e < k_end ? load_elem(row, k + e) : -INFINITY;
+        if (MASK && k + e < k_end && !mrow[k + e]) v[e] = -INFINITY;
+      }
+    }
+    float m = v[0];
+#pragma unroll
+    for (int e = 1; e < LEN; ++e) m = fmaxf(m, v[e]);
+    if (m > st.m) stats_raise(st, m, c);
+#pragma unroll
+    for (int e = 0; e < LEN; ++e) stats_add(st, v[e], c);
+    if (TOP && __ballot(m > list.bar)) {
+      float bar = list.bar;
+      if (first) {
+        // The T-th largest of the lanes' maxima bounds the wave's T-th score from below:
+        // without it the whole first chunk would pass through the list.
+        const uint64_t s = sort64(m > -INFINITY ? key_of(m, 0) : 0, lane);
+        bar = list_bar(s, o.top);
+      }
+#pragma unroll
+      for (int e = 0; e < LEN; ++e) {
+        bool in = first ? v[e] >= bar && v[e] > -INFINITY : v[e] > list.bar;
+        uint64_t pass = __ballot(in);
+        while (pass) {
+          const int from = (int)__builtin_ctzll(pass);
+          pass &= pass - 1;
+          const float s = __uint_as_float(
+              (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[e]), from));
+          const uint32_t id = (uint32_t)(k0 + (int64_t)(wave * 64 + from) * LEN + e);
+          list.key = list_insert(list.key, key_of(s, id), lane);
+        }
+      }
+      first = false;
+      list.bar = list_bar(list.key, o.top);
+    }
+  }
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {  // the wave's statistics
+    Stats b{__shfl_xor(st.m, off, kWave), __shfl_xor(st.sum, off, kWave),
+            __shfl_xor(st.ez, off, kWave)};
+    st = stats_join(st, b, c);
+  }
+  join_waves<TOP>(st, list.key, c, lane, wave, WAVES, sh_st, sh_key);
+
+  if (sp.parts > 1) {
+    uint32_t* mine = sp.words + ((int64_t)n * sp.parts + part) * kPartWords;
+    if (wave == 0) {
+      if (lane == 0) {
+        put_word(mine, __float_as_uint(st.m));
+        put_word(mine + 1, __float_as_uint(st.sum));
+        put_word(mine + 2, __float_as_uint(st.ez));
+      }
+      if (TOP && lane < o.top) {
+        put_word(mine + 4 + 2 * lane, (uint32_t)list.key);
+        put_word(mine + 5 + 2 * lane, (uint32_t)(list.key >> 32));
+      }
+      wait_own_memory_ops();
+      if (lane == 0) sh_last = take_ticket(sp.tickets + n) == (uint32_t)sp.parts - 1;
+    }
+    __syncthreads();
+    if (!sh_last) return;
+    // the last one: wave w takes parts w, w + WAVES, ...
+    if (threadIdx.x == 0) reset_counter(sp.tickets + n);
+    st = stats_none();
+    list.key = 0;
+    uint32_t* words = sp.words + (int64_t)n * sp.parts * kPartWords;
+    for (int p = wave; p < sp.parts; p += WAVES) {
+      uint32_t* w = words + (int64_t)p * kPartWords;
+      uint32_t s = 0;
+      if (lane < 3) s = take_word(w + lane);
+      uint64_t other = 0;
+      const int at = 63 - lane;  // the list in lanes 63, 62, ...
+      if (TOP && lane >= kMaxTop && at < o.top)
+        other = (uint64_t)take_word(w + 5 + 2 * at) << 32 | take_word(w + 4 + 2 * at);
+      const Stats b{__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)s, 0)),
+                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)s, 1)),
+                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)s, 2))};
+      st = stats_join(st, b, c);
+      if (TOP) list.key = merge64(lane < kMaxTop ? list.key : other, lane);
+    }
+    join_waves<TOP>(st, list.key, c, lane, wave, WAVES, sh_st, sh_key);
+  }
+  if (wave != 0) return;
+  const Row r = finish(st);
+  if (lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
+  if (TOP && lane < o.top) write_top(r, list.key, n, lane, a.scale, o);
+}
+
+// Parts of a row: enough workgroups for every compute unit to hold two, of at
+// least two steps each.
+Split split_of(int64_t N, int64_t K, int len) {
+  Split s{1, 0, nullptr, nullptr};
+  const int64_t step = (int64_t)kLongThreads * len, steps = cdiv(K, step);
+  int64_t parts = cdiv(2 * (int64_t)num_cus(), N);
+  if (parts > 64) parts = 64;
+  if (parts > steps / 2) parts = steps / 2;
+  if (parts < 1) parts = 1;
+  const int64_t per = cdiv(steps, parts);
+  s.parts = (int)cdiv(steps, per);
+  s.part_len = per * step;
+  return s;
+}
+constexpr size_t kAlign = 256;
+size_t tickets_bytes(int64_t N) { return ((size_t)N * 4 + kAlign - 1) / kAlign * kAlign; }
+
+template <typename T, int LPR, int VPL>
+hipError_t launch_short(const LogprobsArgs& a, const Out& o, hipStream_t stream) {
+  hipLaunchKernelGGL((logprobs_short_kernel<T, LPR, VPL>),
+                     dim3((unsigned)cdiv(a.N, 256 / LPR)), dim3(256), 0, stream, a, o);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_typed(const LogprobsArgs& a, const Out& o, Split s, hipStream_t stream) {
+  if (a.K <= 8 * 4) return launch_short<T, 8, 4>(a, o, stream);
+  if (a.K <= 16 * 8) return launch_short<T, 16, 8>(a, o, stream);
+  if (a.K <= 64 * 4) return launch_short<T, 64, 4>(a, o, stream);
+  if (a.K <= kShortK) return launch_short<T, 64, 16>(a, o, stream);
+  const dim3 grid((unsigned)(a.N * s.parts)), block(kLongThreads);
+  if (o.top && a.mask)
+    hipLaunchKernelGGL((logprobs_long_kernel<T, true, true>), grid, block, 0, stream, a, o, s);
+  else if (o.top)
+    hipLaunchKernelGGL((logprobs_long_kernel<T, true, false>), grid, block, 0, stream, a, o, s);
+  else if (a.mask)
+    hipLaunchKernelGGL((logprobs_long_kernel<T, false, true>), grid, block, 0, stream, a, o, s);
+  else
+    hipLaunchKernelGGL((logprobs_long_kernel<T, false, false>), grid, block, 0, stream, a, o, s);
+  return hipGetLastError();
+}
+
+// ---- gradient --------------------------------------------------------------------
+
+struct GradRow {
+  float m, logsum, entropy, g, h;
+  int32_t y;
+};
+__device__ __forceinline__ GradRow grad_row(const LogprobsArgs& a, const float* stats,
+                                            const float* entropy, const float* g_logp,
+                                            const float* g_entropy, int64_t n) {
+  GradRow r;
+  r.m = stats[2 * n];
+  r.logsum = stats[2 * n + 1];
+  r.entropy = entropy[n];
+  r.y = a.y ? a.y[n] : -1;
+  r.g = g_logp && r.y >= 0 && r.y < a.K ? g_logp[n] : 0.0f;
+  r.h = g_entropy ? g_entropy[n] : 0.0f;
+  if (r.m == -INFINITY) r.m = 0.0f;  // an empty row: every p below is 0
+  return r;
+}
+__device__ __forceinline__ float grad_of(const GradRow& r, float s, int32_t k, float scale) {
+  float t = (s - r.m) * scale - r.logsum;
+  if (t < -1000.0f) t = -1000.0f;  // p is 0 either way, and 0 * t too; NaN stays
+  const float p = exp2_fast(t * kLog2e);
+  float d = -p * (r.g + r.h * (t + r.entropy));
+  if (k == r.y && s > -INFINITY) d += r.g;
+  return d * scale;
+}
+
+// A thread takes LEN classes of one row. ROWS: a workgroup works within a row (blockIdx.y),
+// else a thread finds its row.
+template <typename T, bool MASK, bool ROWS>
+__global__ __launch_bounds__(256) void logprobs_grad_kernel(
+    LogprobsArgs a, const float* __restrict__ stats, const float* __restrict__ entropy,
+    const float* __restrict__ g_logp, const float* __restrict__ g_entropy, T* out, int64_t ldd,
+    uint32_t chunks) {
+  constexpr int LEN = Chunk<T>::kLen;
+  int64_t n;
+  uint32_t ch;
+  if (ROWS) {
+    n = blockIdx.x / cdiv(chunks, 256);
+    ch = (uint32_t)(blockIdx.x % (uint32_t)cdiv(chunks, 256)) * 256 + threadIdx.x;
+  } else {
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    n = (int64_t)(at / chunks);
+    ch = (uint32_t)(at % chunks);
+  }
+  if (n >= a.N || ch >= chunks) return;
+  const GradRow r = grad_row(a, stats, entropy, g_logp, g_entropy, n);
+  const int64_t k = (int64_t)ch * LEN;
+  const T* row = static_cast<const T*>(a.scores) + n * a.ld + k;
+  const uint8_t* mrow = MASK ? a.mask + n * a.ldm + k : nullptr;
+  T* dst = out + n * ldd + k;
+  if (k + LEN <= a.K) {
+    float v[LEN];
+    load_chunk(row, v);
+    if (MASK) mask_chunk<LEN>(mrow, v);
+    if constexpr (sizeof(T) == 4) {
+      f32x4 d;
+#pragma unroll
+      for (int e = 0; e < LEN; ++e) d[e] = grad_of(r, v[e], (int32_t)(k + e), a.scale);
+      *reinterpret_cast<f32x4_a4*>(dst) = d;
+    } else {
+      u32x4 d;
+#pragma unroll
+      for (int e = 0; e < LEN / 2; ++e)
+        d[e] = (uint32_t)to_bf16(grad_of(r, v[2 * e], (int32_t)(k + 2 * e), a.scale)) |
+               (uint32_t)to_bf16(grad_of(r, v[2 * e + 1], (int32_t)(k + 2 * e + 1), a.scale))
+                   << 16;
+      *reinterpret_cast<u32x4_a2*>(dst) = d;
+    }
+  } else {
+    for (int e = 0; k + e < a.K; ++e) {
+      const float s = !MASK || mrow[e] ? load_elem(row, e) : -INFINITY;
+      store_elem(dst, e, grad_of(r, s, (int32_t)(k + e), a.scale));
+    }
+  }
+}
+
+template <typename T>
+hipError_t launch_grad(const LogprobsArgs& a, const float* stats, const float* entropy,
+                       const float* g_logp, const float* g_entropy, void* out, int64_t ldd,
+                       hipStream_t stream) {
+  const uint32_t chunks = (uint32_t)cdiv(a.K, Chunk<T>::kLen);
+  T* d = static_cast<T*>(out);
+  // a row of 256 chunks fills a workgroup
+  const bool rows = chunks >= 256;
+  const int64_t blocks = rows ? a.N * cdiv(chunks, 256) : cdiv(a.N * chunks, 256);
+  const dim3 grid((unsigned)blocks), block(256);
+  if (rows && a.mask)
+    hipLaunchKernelGGL((logprobs_grad_kernel<T, true, true>), grid, block, 0, stream, a, stats,
+                       entropy, g_logp, g_entropy, d, ldd, chunks);
+  else if (rows)
+    hipLaunchKernelGGL((logprobs_grad_kernel<T, false, true>), grid, block, 0, stream, a, stats,
+                       entropy, g_logp, g_entropy, d, ldd, chunks);
+  else if (a.mask)
+    hipLaunchKernelGGL((logprobs_grad_kernel<T, true, false>), grid, block, 0, stream, a, stats,
+                       entropy, g_logp, g_entropy, d, ldd, chunks);
+  else
+    hipLaunchKernelGGL((logprobs_grad_kernel<T, false, false>), grid, block, 0, stream, a, stats,
+                       entropy, g_logp, g_entropy, d, ldd, chunks);
+  return hipGetLastError();
+}
+
+constexpr int64_t kMaxRows = int64_t(1) << 21;  // of a launch
+
+LogprobsArgs rows_from(const LogprobsArgs& a, int64_t n0, int64_t most) {
+  LogprobsArgs r = a;
+  r.scores = static_cast<const char*>(a.scores) + n0 * a.ld * (a.dt == 0 ? 4 : 2);
+  if (a.mask) r.mask = a.mask + n0 * a.ldm;
+  if (a.y) r.y = a.y + n0;
+  r.N = a.N - n0 < most ? a.N - n0 : most;
+  return r;
+}
+
+}  // namespace
+
+size_t logprobs_ws_bytes(int64_t N, int64_t K, int dt) {
+  if (K <= kShortK) return 0;
+  const Split s = split_of(N, K, dt == 0 ? 4 : 8);
+  if (s.parts == 1) return 0;
+  return tickets_bytes(N) + (size_t)N * s.parts * kPartWords * 4;
+}
+
+hipError_t launch_logprobs(const LogprobsArgs& all, float* logp, float* entropy, float* stats,
+                           int32_t* ids, float* top_logp, int top, void* workspace,
+                           hipStream_t stream) {
+  Split s = split_of(all.N, all.K, all.dt == 0 ? 4 : 8);  // (one part where N > kMaxRows)
+  s.tickets = static_cast<uint32_t*>(workspace);
+  s.words = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + tickets_bytes(all.N));
+  // a launch holds at most 2^32 threads
+  for (int64_t n0 = 0; n0 < all.N; n0 += kMaxRows) {
+    const LogprobsArgs a = rows_from(all, n0, kMaxRows);
+    const Out o{logp ? logp + n0 : nullptr, entropy + n0, stats + 2 * n0,
+                ids ? ids + n0 * top : nullptr, top_logp ? top_logp + n0 * top : nullptr, top};
+    const hipError_t e = a.dt == 0 ? launch_typed<float>(a, o, s, stream)
+                                   : launch_typed<bf16raw>(a, o, s, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_logprobs_grad(const LogprobsArgs& all, const float* stats,
+                                const float* entropy, const float* g_logp,
+                                const float* g_entropy, void* dscores, int64_t ldd,
+                                hipStream_t stream) {
+  // (a row takes up to 2^20 workgroups)
+  const int64_t per = cdiv(all.K, 256 * 4), step = per > 4 ? (kMaxRows * 4) / per : kMaxRows;
+  for (int64_t n0 = 0; n0 < all.N; n0 += step) {
+    const LogprobsArgs a = rows_from(all, n0, step);
+    const float *st = stats + 2 * n0, *en = entropy + n0, *gl = g_logp ? g_logp + n0 : nullptr,
+                *ge = g_entropy ? g_entropy + n0 : nullptr;
+    const hipError_t e =
+        a.dt == 0 ? launch_grad<float>(a, st, en, gl, ge, static_cast<float*>(dscores) + n0 * ldd,
+                                       ldd, stream)
+                  : launch_grad<bf16raw>(a, st, en, gl, ge,
+                                         static_cast<bf16raw*>(dscores) + n0 * ldd, ldd, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace ops
+}  // namespace hd

@@ -1,0 +1,524 @@
+// Products with 4-bit weights and group scales:
+//   Y[n,o] = act( sum_i X[n,i] * s[o,g] * (q[o,i] - z[o,g]) ),   g = i / G,
+// q in 0..15, z = 8 where the weights have no zero points.
+//
+// One pass over the weights is what bounds it: O*I/2 bytes of codes and two (with
+// zero points three) bytes a group, against X and Y, which are small. The codes go
+// to the bf16 matrix instruction, which costs the same for 1 and for 16 rows of X:
+// * a byte that holds a code 0..15 is, read as fp8 e4m3, the number q * 2^-9
+//   (0..7 are its subnormals, 8..15 its first binade), so two masks and a shift
+//   split eight codes and four conversions make eight bf16 values, exact;
+// * sum x*q and sum x run through separate chains, fresh for each group, and
+//   s * (sum x*q - z * sum x) is added in fp32. The second chain multiplies X by a
+//   constant operand, once for all tiles of outputs, and its result lies in
+//   the lanes that need it;
+// * fp32 X is the exact sum of three bf16 values (its 24 bits cut in three), one
+//   matrix instruction each. Products of 4 and 8 bits are exact in fp32.
+//
+// Layout: a tile is 16 outputs x 128 inputs, 1 KiB of codes, one 16-byte load for
+// each lane. Lane l holds output l % 16 and, in dword s, inputs 32 s + 8 (l / 16) + e,
+// e = 0..7, code e in the nibble 2 e (e < 4) or 2 e - 7: the operand order of
+// v_mfma_f32_16x16x32_bf16. Tiles of one 16-output row follow each other, so a wave
+// reads 1 KiB runs. Scales and zero points lie as the result's lanes need them:
+// [output tile][input tile][l / 16][group][4 outputs].
+//
+// A workgroup takes TD output tiles, its waves every W-th input tile, and the waves'
+// sums are added in LDS in a fixed order.
+#include "hd_ops.hpp"
+
+namespace hd {
+namespace ops {
+
+namespace {
+
+constexpr int kTileI = 128, kTileO = 16;
+
+__host__ __device__ inline NibbleLayout layout_of(int64_t O, int64_t I, int G) {
+  NibbleLayout L;
+  L.otiles = cdiv(O, kTileO);
+  L.itiles = cdiv(I, kTileI);
+  const int64_t tiles = L.otiles * L.itiles, groups = tiles * (kTileI / G) * kTileO;
+  L.scales = (size_t)tiles * 1024;
+  L.zeros = L.scales + ((size_t)groups * 2 + 255) / 256 * 256;
+  L.total = L.zeros + ((size_t)groups + 255) / 256 * 256;
+  return L;
+}
+
+// Nibble of element e (0..7) of a lane's dword.
+__host__ __device__ constexpr int nibble_of(int e) { return e < 4 ? 2 * e : 2 * e - 7; }
+
+// Index of (output o, group g of the row) in the scale and zero-point sections.
+__device__ __forceinline__ int64_t group_index(int64_t o, int64_t g, int64_t itiles, int gpt) {
+  const int64_t tile = (o / kTileO) * itiles + g / gpt;
+  const int r = (int)(o % kTileO);
+  return ((tile * 4 + r / 4) * gpt + g % gpt) * 4 + r % 4;
+}
+
+// ---- layout ------------------------------------------------------------------
+
+__global__ __launch_bounds__(256) void nibble_pack_kernel(const uint8_t* __restrict__ codes,
+                                                          int64_t O, int64_t I, int64_t itiles,
+                                                          int64_t total, uint32_t* out) {
+  // one dword: eight codes of one output
+  for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < total;
+       w += (int64_t)gridDim.x * 256) {
+    const int s = (int)(w & 3), lane = (int)(w >> 2) & 63;
+    const int64_t tile = w >> 8;
+    const int64_t o = tile / itiles * kTileO + lane % 16;
+    const int64_t i0 = tile % itiles * kTileI + 32 * s + 8 * (lane / 16);
+    const uint8_t* row = codes + o * cdiv(I, 2);
+    uint32_t v = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (o < O && i0 + e < I)
+        v |= (uint32_t)((row[(i0 + e) / 2] >> (4 * (e & 1))) & 15) << (4 * nibble_of(e));
+    out[w] = v;
+  }
+}
+
+__global__ __launch_bounds__(256) void nibble_pack_groups_kernel(
+    const bf16raw* __restrict__ scales, const uint8_t* __restrict__ zeros, int64_t O,
+    int64_t groups, int64_t itiles, int gpt, int64_t total, bf16raw* out_s, uint8_t* out_z) {
+  for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < total;
+       w += (int64_t)gridDim.x * 256) {
+    const int r = (int)(w % 4), gg = (int)(w / 4 % gpt), quad = (int)(w / 4 / gpt % 4);
+    const int64_t tile = w / (16 * gpt);
+    const int64_t o = tile / itiles * kTileO + 4 * quad + r, g = tile % itiles * gpt + gg;
+    const bool in = o < O && g < groups;
+    out_s[w] = in ? scales[o * groups + g] : (bf16raw)0;
+    out_z[w] = in && zeros ? (uint8_t)(zeros[o * groups + g] & 15) : (uint8_t)8;
+  }
+}
+
+// One wave quantises one tile: lane l the elements it will hold. W is [O][I]
+// (in_rows false) or [I][O].
+template <typename T>
+__global__ __launch_bounds__(64) void nibble_quantize_kernel(const T* __restrict__ W, int64_t ldw,
+                                                             int in_rows, int64_t O, int64_t I,
+                                                             int64_t itiles, int gpt,
+                                                             int with_zeros, u32x4* out,
+                                                             bf16raw* out_s, uint8_t* out_z) {
+  const int lane = threadIdx.x;
+  const int64_t tile = blockIdx.x;
+  const int64_t o = tile / itiles * kTileO + lane % 16;
+  const int64_t i0 = tile % itiles * kTileI + 8 * (lane / 16);
+  float v[4][8];
+  float lo[4], hi[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    lo[s] = 0.0f, hi[s] = 0.0f;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t i = i0 + 32 * s + e;
+      v[s][e] = (o < O && i < I) ? load_elem(W, in_rows ? i * ldw + o : o * ldw + i) : 0.0f;
+      lo[s] = fminf(lo[s], v[s][e]);
+      hi[s] = fmaxf(hi[s], v[s][e]);
+      bad |= v[s][e] != v[s][e];
+    }
+    if (bad) lo[s] = -INFINITY;  // NaN: the group's scale is no number either
+#pragma unroll
+    for (int off = 16; off < 64; off <<= 1) {  // the four lanes of one output
+      lo[s] = fminf(lo[s], __shfl_xor(lo[s], off, kWave));
+      hi[s] = fmaxf(hi[s], __shfl_xor(hi[s], off, kWave));
+    }
+  }
+  const int per = 4 / gpt;  // steps of one group
+  u32x4 packed;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    float l = 0.0f, h = 0.0f;
+    for (int t = s / per * per; t < s / per * per + per; ++t) {
+      // (t is small and known after unrolling for each gpt)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (u == t) l = fminf(l, lo[u]), h = fmaxf(h, hi[u]);
+    }
+    const float span = with_zeros ? (h - l) / 15.0f : fmaxf(h, -l) / 7.0f;
+    bf16raw sb = to_bf16(span);  // the codes are taken by the scale that is kept
+    const float sc = bf16_to_f32(sb);
+    const bool bad = !(sc < INFINITY);
+    if (bad) sb = 0x7fc0;  // NaN
+    const float r = sc > 0.0f && !bad ? 1.0f / sc : 0.0f;
+    const float z = with_zeros ? fminf(fmaxf(rintf(-l * r), 0.0f), 15.0f) : 8.0f;
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float q = fminf(fmaxf(rintf(v[s][e] * r) + z, 0.0f), 15.0f);
+      w |= (uint32_t)q << (4 * nibble_of(e));
+    }
+    packed[s] = w;
+    if (s % per == 0 && lane < 16) {
+      const int64_t at = ((tile * 4 + lane / 4) * gpt + s / per) * 4 + lane % 4;
+      out_s[at] = sb;
+      out_z[at] = (uint8_t)z;
+    }
+  }
+  out[tile * 64 + lane] = packed;
+}
+
+__device__ __forceinline__ float weight_at(const uint8_t* image, const bf16raw* scales,
+                                           const uint8_t* zeros, int64_t o, int64_t i,
+                                           int64_t itiles, int gpt, bool with_zeros) {
+  const int64_t tile = (o / kTileO) * itiles + i / kTileI;
+  const int in = (int)(i % kTileI), e = in % 8;
+  const int lane = (int)(o % kTileO) + 16 * (in % 32 / 8);
+  const uint32_t w = reinterpret_cast<const uint32_t*>(image)[(tile * 64 + lane) * 4 + in / 32];
+  const int q = (int)(w >> (4 * nibble_of(e))) & 15;
+  const int64_t at = group_index(o, i / (kTileI / gpt), itiles, gpt);
+  const int z = with_zeros ? (int)zeros[at] : 8;
+  return (float)(q - z) * bf16_to_f32(scales[at]);
+}
+
+__global__ __launch_bounds__(256) void nibble_unpack_kernel(const uint8_t* image,
+                                                            const bf16raw* scales,
+                                                            const uint8_t* zeros, float* W,
+                                                            int64_t O, int64_t I, int64_t itiles,
+                                                            int gpt, int with_zeros) {
+  for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < O * I;
+       w += (int64_t)gridDim.x * 256)
+    W[w] = weight_at(image, scales, zeros, w / I, w % I, itiles, gpt, with_zeros != 0);
+}
+
+// ---- product -----------------------------------------------------------------
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+// Eight codes of a dword as bf16 values 0..15.
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t w) {
+  const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
+  u32x4 v;
+  v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, false));
+  v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, true));
+  v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, false));
+  v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, true));
+  return as_bf16x8(v);
+}
+
+// Upper halves of two words, a below b.
+__device__ __forceinline__ uint32_t upper2(uint32_t a, uint32_t b) {
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+
+// Eight elements of X from column i, as PARTS bf16 operands: bf16 as they are, fp32
+// cut in three (each part the upper 16 bits of what is left: exact, and of no
+// larger magnitude, so nothing overflows; an infinity's rest is NaN, and such
+// outputs are taken again one by one). Columns past I are zero.
+template <typename T>
+struct XLoad;
+template <>
+struct XLoad<bf16raw> {
+  static constexpr int kParts = 1;
+  u32x4 v;
+  __device__ __forceinline__ void full(const bf16raw* p) {
+    v = *reinterpret_cast<const u32x4_a2*>(p);
+  }
+  __device__ __forceinline__ void tail(const bf16raw* p, int64_t left) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t a = 2 * e < left ? p[2 * e] : 0, b = 2 * e + 1 < left ? p[2 * e + 1] : 0;
+      v[e] = a | b << 16;
+    }
+  }
+  __device__ __forceinline__ void parts(bf16x8 (&out)[1]) const { out[0] = as_bf16x8(v); }
+};
+template <>
+struct XLoad<float> {
+  static constexpr int kParts = 3;
+  float v[8];
+  __device__ __forceinline__ void full(const float* p) {
+    const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p);
+    const f32x4 b = *reinterpret_cast<const f32x4_a4*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+  }
+  __device__ __forceinline__ void tail(const float* p, int64_t left) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : 0.0f;
+  }
+  __device__ __forceinline__ void parts(bf16x8 (&out)[3]) const {
+    u32x4 w[3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float a = v[2 * e], b = v[2 * e + 1];
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+        w[p][e] = upper2(ua, ub);
+        a -= __uint_as_float(ua & 0xffff0000u);
+        b -= __uint_as_float(ub & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) out[p] = as_bf16x8(w[p]);
+  }
+};
+
+// One output by itself, for those that are not finite.
+template <typename T>
+__device__ __noinline__ float product_one(const T* x, const uint8_t* image, const bf16raw* scales,
+                                          const uint8_t* zeros, int64_t o, int64_t I,
+                                          int64_t itiles, int gpt, bool with_zeros) {
+  float y = 0.0f;
+  for (int64_t i = 0; i < I; ++i)
+    y = fmaf(load_elem(x, i), weight_at(image, scales, zeros, o, i, itiles, gpt, with_zeros), y);
+  return y;
+}
+
+// W waves; NT tiles of 16 rows of X, TD tiles of 16 outputs, GPT groups in an input tile.
+template <typename T, int GPT, bool ZERO, int NT, int TD>
+__global__ __launch_bounds__(512) void nibble_product_kernel(
+    const T* __restrict__ X, int64_t ldx, const uint8_t* __restrict__ image, int64_t scales_at,
+    int64_t zeros_at, void* __restrict__ Y, int64_t ldy, int64_t N, int64_t O, int64_t I,
+    int64_t otiles, int itiles, int y_dt, int act) {
+  constexpr int P = XLoad<T>::kParts;
+  constexpr int STEPS = 4 / GPT;  // matrix steps of 32 inputs in a group
+  extern __shared__ f32x4 sums[];  // [W][TD][NT][64]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int col = lane & 15, quad = lane >> 4;
+  const int64_t ot0 = (int64_t)blockIdx.x * TD;
+  const int64_t n0 = (int64_t)blockIdx.y * (16 * NT);
+  const bf16raw* scales = reinterpret_cast<const bf16raw*>(image + scales_at);
+  const uint8_t* zeros = image + zeros_at;
+
+  const T* xrow[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int64_t n = n0 + 16 * t + col;
+    xrow[t] = X + (n < N ? n : N - 1) * ldx + 8 * quad;  // rows past N: any, never written
+  }
+  // per output tile, the row of input tiles (tiles past the last repeat it)
+  int64_t row[TD];
+#pragma unroll
+  for (int d = 0; d < TD; ++d) {
+    const int64_t ot = ot0 + d < otiles ? ot0 + d : otiles - 1;
+    row[d] = ot * itiles;
+  }
+
+  f32x4 acc[TD][NT];
+#pragma unroll
+  for (int d = 0; d < TD; ++d)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[d][t] = f32x4{0, 0, 0, 0};
+  u32x4 ones_w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ones_w[e] = ZERO ? 0x3f803f80u : 0xc100c100u;  // 1, or -8
+  const bf16x8 ones = as_bf16x8(ones_w);
+
+  for (int it = wave; it < itiles; it += waves) {
+    u32x4 code[TD];
+    uint2 sc[TD][GPT];
+    uint32_t zp[TD][GPT];
+#pragma unroll
+    for (int d = 0; d < TD; ++d) {
+      const int64_t tile = row[d] + it;
+      code[d] = reinterpret_cast<const u32x4*>(image)[tile * 64 + lane];
+#pragma unroll
+      for (int g = 0; g < GPT; ++g) {
+        const int64_t at = (tile * 4 + quad) * GPT + g;
+        sc[d][g] = reinterpret_cast<const uint2*>(scales)[at];
+        if (ZERO) zp[d][g] = reinterpret_cast<const uint32_t*>(zeros)[at];
+      }
+    }
+    const int64_t i0 = (int64_t)it * kTileI;
+    const bool full = i0 + kTileI <= I;
+    XLoad<T> x[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int64_t i = i0 + 32 * s;
+        if (full || i + 8 * quad + 8 <= I)
+          x[t][s].full(xrow[t] + i);
+        else
+          x[t][s].tail(xrow[t] + i, I - i - 8 * quad);
+      }
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) {
+      f32x4 sum[TD][NT], one[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        one[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int d = 0; d < TD; ++d) sum[d][t] = f32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int s = g * STEPS; s < (g + 1) * STEPS; ++s) {
+        bf16x8 xp[NT][P];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          x[t][s].parts(xp[t]);
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+            one[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xp[t][p], one[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int d = 0; d < TD; ++d) {
+          const bf16x8 q = codes_bf16(code[d][s]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+              sum[d][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, xp[t][p], sum[d][t], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < TD; ++d) {
+        float sf[4] = {__uint_as_float(sc[d][g].x << 16),
+                       __uint_as_float(sc[d][g].x & 0xffff0000u),
+                       __uint_as_float(sc[d][g].y << 16),
+                       __uint_as_float(sc[d][g].y & 0xffff0000u)};
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float v;
+            if (ZERO)
+              v = fmaf(-(float)((zp[d][g] >> (8 * r)) & 255u), one[t][r], sum[d][t][r]);
+            else
+              v = sum[d][t][r] + one[t][r];
+            acc[d][t][r] = fmaf(sf[r], v, acc[d][t][r]);
+          }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int d = 0; d < TD; ++d)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sums[((wave * TD + d) * NT + t) * 64 + lane] = acc[d][t];
+  __syncthreads();
+  for (int j = wave; j < TD * NT; j += waves) {
+    const int d = j / NT, t = j % NT;
+    f32x4 y = sums[j * 64 + lane];
+    for (int w = 1; w < waves; ++w) y += sums[(w * TD * NT + j) * 64 + lane];
+    const int64_t n = n0 + 16 * t + col;
+    const int64_t o0 = (ot0 + d) * kTileO + 4 * quad;
+    if (n >= N) continue;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t o = o0 + r;
+      if (o >= O) continue;
+      float v = y[r];
+      // Not finite: an infinity or NaN in X, or a sum x*q past the range where
+      // the products with q - z stay within it. Taken again as the formula says.
+      if (!(fabsf(v) < INFINITY))
+        v = product_one(X + n * ldx, image, scales, zeros, o, I, (int64_t)itiles, GPT, ZERO);
+      v = activate(v, act);
+      if (y_dt == 0)
+        static_cast<float*>(Y)[n * ldy + o] = v;
+      else
+        static_cast<bf16raw*>(Y)[n * ldy + o] = to_bf16(v);
+    }
+  }
+}
+
+struct ProductArgs {
+  const void* X;
+  int64_t ldx;
+  const uint8_t* image;
+  void* Y;
+  int64_t ldy, N, O, I;
+  NibbleLayout L;
+  int y_dt, act;
+  hipStream_t stream;
+};
+
+template <typename T, int GPT, bool ZERO, int NT, int TD>
+hipError_t launch_product_as(const ProductArgs& a) {
+  int waves = a.L.itiles < 8 ? (int)a.L.itiles : 8;
+  const size_t lds = sizeof(f32x4) * 64 * TD * NT * waves;
+  const dim3 grid((unsigned)cdiv(a.L.otiles, TD), (unsigned)cdiv(a.N, 16 * NT));
+  hipLaunchKernelGGL((nibble_product_kernel<T, GPT, ZERO, NT, TD>), grid, dim3(64 * waves), lds,
+                     a.stream, static_cast<const T*>(a.X), a.ldx, a.image, (int64_t)a.L.scales,
+                     (int64_t)a.L.zeros, a.Y, a.ldy, a.N, a.O, a.I, a.L.otiles, (int)a.L.itiles,
+                     a.y_dt, a.act);
+  return hipGetLastError();
+}
+
+template <typename T, int GPT, bool ZERO>
+hipError_t launch_product_rows(const ProductArgs& a) {
+  if (a.N <= 16) return launch_product_as<T, GPT, ZERO, 1, 2>(a);
+  if (a.N <= 32) return launch_product_as<T, GPT, ZERO, 2, 2>(a);
+  return launch_product_as<T, GPT, ZERO, 4, 1>(a);
+}
+
+template <typename T>
+hipError_t launch_product_typed(const ProductArgs& a, int G, bool zero) {
+  switch (G) {
+    case 32:
+      return zero ? launch_product_rows<T, 4, true>(a) : launch_product_rows<T, 4, false>(a);
+    case 64:
+      return zero ? launch_product_rows<T, 2, true>(a) : launch_product_rows<T, 2, false>(a);
+    default:
+      return zero ? launch_product_rows<T, 1, true>(a) : launch_product_rows<T, 1, false>(a);
+  }
+}
+
+unsigned blocks_for(int64_t total) {
+  const int64_t g = cdiv(total, 256);
+  return (unsigned)(g < 65536 ? g : 65536);
+}
+
+}  // namespace
+
+NibbleLayout nibble_layout(int64_t O, int64_t I, int G) { return layout_of(O, I, G); }
+
+hipError_t launch_nibble_pack(const uint8_t* codes, const bf16raw* scales, const uint8_t* zeros,
+                              int64_t O, int64_t I, int G, void* image, hipStream_t stream) {
+  const NibbleLayout L = layout_of(O, I, G);
+  uint8_t* im = static_cast<uint8_t*>(image);
+  const int gpt = kTileI / G;
+  const int64_t words = L.otiles * L.itiles * 256, groups = L.otiles * L.itiles * gpt * kTileO;
+  hipLaunchKernelGGL(nibble_pack_kernel, dim3(blocks_for(words)), dim3(256), 0, stream, codes, O,
+                     I, L.itiles, words, reinterpret_cast<uint32_t*>(im));
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(nibble_pack_groups_kernel, dim3(blocks_for(groups)), dim3(256), 0, stream,
+                     scales, zeros, O, cdiv(I, G), L.itiles, gpt, groups,
+                     reinterpret_cast<bf16raw*>(im + L.scales), im + L.zeros);
+  return hipGetLastError();
+}
+
+hipError_t launch_nibble_quantize(const void* W, int64_t ldw, bool in_rows, int64_t O, int64_t I,
+                                  int G, bool with_zeros, int dt, void* image,
+                                  hipStream_t stream) {
+  const NibbleLayout L = layout_of(O, I, G);
+  uint8_t* im = static_cast<uint8_t*>(image);
+  const dim3 grid((unsigned)(L.otiles * L.itiles));
+  bf16raw* s = reinterpret_cast<bf16raw*>(im + L.scales);
+  if (dt == 0)
+    hipLaunchKernelGGL(nibble_quantize_kernel<float>, grid, dim3(64), 0, stream,
+                       static_cast<const float*>(W), ldw, (int)in_rows, O, I, L.itiles,
+                       kTileI / G, (int)with_zeros, reinterpret_cast<u32x4*>(im), s,
+                       im + L.zeros);
+  else
+    hipLaunchKernelGGL(nibble_quantize_kernel<bf16raw>, grid, dim3(64), 0, stream,
+                       static_cast<const bf16raw*>(W), ldw, (int)in_rows, O, I, L.itiles,
+                       kTileI / G, (int)with_zeros, reinterpret_cast<u32x4*>(im), s,
+                       im + L.zeros);
+  return hipGetLastError();
+}
+
+hipError_t launch_nibble_unpack(const void* image, float* W, int64_t O, int64_t I, int G,
+                                bool with_zeros, hipStream_t stream) {
+  const NibbleLayout L = layout_of(O, I, G);
+  const uint8_t* im = static_cast<const uint8_t*>(image);
+  hipLaunchKernelGGL(nibble_unpack_kernel, dim3(blocks_for(O * I)), dim3(256), 0, stream, im,
+                     reinterpret_cast<const bf16raw*>(im + L.scales), im + L.zeros, W, O, I,
+                     L.itiles, kTileI / G, (int)with_zeros);
+  return hipGetLastError();
+}
+
+hipError_t launch_nibble_product(const void* X, int64_t ldx, const void* image, void* Y,
+                                 int64_t ldy, int64_t N, int64_t O, int64_t I, int G,
+                                 bool with_zeros, int x_dt, int y_dt, int act,
+                                 hipStream_t stream) {
+  const ProductArgs a{X,   ldx, static_cast<const uint8_t*>(image), Y,    ldy, N, O, I,
+                      layout_of(O, I, G), y_dt, act, stream};
+  return x_dt == 0 ? launch_product_typed<float>(a, G, with_zeros)
+                   : launch_product_typed<bf16raw>(a, G, with_zeros);
+}
+
+}  // namespace ops
+}  // namespace hd
