@@ -529,38 +529,54 @@ def train(X, B, y, K: int):
 
 
 # ---- Operators behind answers and learning ------------------------------------------------
+#
+# A call here takes a few microseconds on the GPU at the smallest sizes, so the binding
+# looks each property up once and asks for the stream by its device's index.
+
+_codes: dict = {}  # torch dtype -> hd_dtype, of the matrices these operators take
 
 
-def _check_rows(t, name: str, dtypes):
-    """A matrix on the GPU whose rows are contiguous; returns its row stride."""
-    if not t.is_cuda:
+def _float_codes() -> dict:
+    if not _codes:
+        torch = _torch()
+        _codes.update({torch.float32: HD_F32, torch.bfloat16: HD_BF16})
+    return _codes
+
+
+def _raw_stream(index: int) -> int:
+    return _torch()._C._cuda_getCurrentRawStream(index)
+
+
+def _rows(t, name: str):
+    """A float32 or bfloat16 matrix on the GPU whose rows are contiguous:
+    (rows, columns, row stride, hd_dtype, device index)."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError("tensors must be on the GPU")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}")
+    code = (_codes or _float_codes()).get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16")
     if t.dim() != 2:
         raise ValueError(f"{name} must be a matrix")
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    # (the stride of a single row or of none is not used, and may be anything)
-    ld = t.stride(0) if rows > 1 else cols
     if ld < cols:
-        raise ValueError(f"{name} must not have overlapping rows")
-    return ld
+        # (the stride of a single row or of none is not used, and may be anything)
+        if rows > 1:
+            raise ValueError(f"{name} must not have overlapping rows")
+        ld = cols
+    return rows, cols, ld, code, index
 
 
-def _check_vec(t, name: str, dtype, n: int, device):
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
+def _vec(t, name: str, dtype, n: int, index: int) -> int:
+    """The address of a contiguous vector of n on the device ``index``."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != (n,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous vector of {n}")
-
-
-def _floats():
-    torch = _torch()
-    return (torch.float32, torch.bfloat16)
+    if t.get_device() != index or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n} on GPU {index}")
+    return t.data_ptr()
 
 
 def _ptr(t):
@@ -617,11 +633,12 @@ def nibble_quantize(W, group: int = 64, inner_rows: bool = False,
     """4-bit weights from numbers: ``W`` [outer, inner] (class hypervectors), or with
     ``inner_rows`` [inner, outer] (base hypervectors B[F, D]); float32 or bfloat16.
     ``zeros``: min-max codes with zero points instead of symmetric ones."""
-    ld = _check_rows(W, "W", _floats())
-    outer, inner = (W.shape[1], W.shape[0]) if inner_rows else W.shape
+    outer, inner, ld, dt, index = _rows(W, "W")
+    if inner_rows:
+        outer, inner = inner, outer
     image, nbytes = _nibble_image(outer, inner, group, W.device)
     st = lib().hd_nibble_quantize(W.data_ptr(), ld, int(inner_rows), int(zeros), outer, inner,
-                                  group, _dt(W), image.data_ptr(), nbytes, _stream_ptr(W.device))
+                                  group, dt, image.data_ptr(), nbytes, _raw_stream(index))
     _raise(st, "hd_nibble_quantize")
     return NibbleWeights(image, outer, inner, group, bool(zeros))
 
@@ -639,23 +656,29 @@ def nibble_unpack(w: NibbleWeights):
 def nibble_product(X, w: NibbleWeights, act: str = "identity", dtype=None, out=None):
     """Y[N, outer] = act(X w^T) for X [N, inner] float32 or bfloat16; ``dtype`` of Y
     defaults to X's. ``act`` "hardsign" encodes (Stage I on 4-bit base vectors)."""
-    torch = _torch()
-    ldx = _check_rows(X, "X", _floats())
-    N, inner = X.shape
+    N, inner, ldx, x_dt, index = _rows(X, "X")
+    outer, image = w.outer, w.image
     if inner != w.inner:
         raise ValueError("shape mismatch")
-    if X.device != w.image.device:
+    if image.get_device() != index:
         raise ValueError("X and the weights must be on one device")
     if out is None:
-        out = torch.empty((N, w.outer), dtype=dtype or X.dtype, device=X.device)
-    elif out.device != X.device or tuple(out.shape) != (N, w.outer):
-        raise ValueError("out must be [N, outer] on X's device")
-    elif dtype is not None and out.dtype != dtype:
-        raise TypeError("out has another dtype")
-    ldy = _check_rows(out, "out", _floats())
-    st = lib().hd_nibble_product(X.data_ptr(), ldx, w.image.data_ptr(), int(w.zeros),
-                                 out.data_ptr(), ldy, N, w.outer, inner, w.group, _dt(X),
-                                 _dt(out), ACTS[act], _stream_ptr(X.device))
+        if dtype is None or dtype == X.dtype:
+            y_dt = x_dt
+        else:
+            y_dt = _codes.get(dtype)
+            if y_dt is None:
+                raise TypeError("dtype must be float32 or bfloat16")
+        out, ldy = _torch().empty(N, outer, dtype=dtype or X.dtype, device=X.device), outer
+    else:
+        _, _, ldy, y_dt, out_index = _rows(out, "out")
+        if out_index != index or out.shape != (N, outer):
+            raise ValueError("out must be [N, outer] on X's device")
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError("out has another dtype")
+    st = lib().hd_nibble_product(X.data_ptr(), ldx, image.data_ptr(), w.zeros, out.data_ptr(),
+                                 ldy, N, outer, inner, w.group, x_dt, y_dt, ACTS[act],
+                                 _raw_stream(index))
     _raise(st, "hd_nibble_product")
     return out
 
@@ -663,7 +686,8 @@ def nibble_product(X, w: NibbleWeights, act: str = "identity", dtype=None, out=N
 class LogProbs(NamedTuple):
     """What ``logprobs`` gives for N rows: ``logp`` [N] (None without ``y``),
     ``entropy`` [N], ``stats`` [N, 2] (the largest score m, and log sum exp
-    scale (s - m)), ``ids`` and ``top_logp`` [N, top] (None for top 0)."""
+    scale (s - m)), ``ids`` and ``top_logp`` [N, top] (None for top 0). They are
+    parts of one allocation."""
     logp: object
     entropy: object
     stats: object
@@ -671,22 +695,29 @@ class LogProbs(NamedTuple):
     top_logp: object
 
 
-def _mask_arg(mask, N: int, K: int, device):
-    """Pointer and row stride of a mask [K] or [N, K] (bool or uint8)."""
+def _mask_arg(mask, N: int, K: int, index: int):
+    """Address and row stride of a mask [K] or [N, K] (bool or uint8)."""
     torch = _torch()
     if mask is None:
         return None, 0
-    if mask.device != device:
+    if mask.get_device() != index:
         raise ValueError("mask must be on the scores' device")
     if mask.dtype not in (torch.bool, torch.uint8):
         raise TypeError("mask must be bool or uint8")
-    if tuple(mask.shape) == (K,) and (K == 1 or mask.stride(0) == 1):
+    if mask.shape == (K,):
+        if K > 1 and mask.stride(0) != 1:
+            raise ValueError("mask must be contiguous")
         return mask.data_ptr(), 0
-    if tuple(mask.shape) != (N, K):
+    if mask.shape != (N, K):
         raise ValueError("mask must be [K] or [N, K]")
-    if N > 1 and mask.stride(0) == 0 and (K == 1 or mask.stride(1) == 1):
-        return mask.data_ptr(), 0  # one row, expanded
-    return mask.data_ptr(), _check_rows(mask, "mask", (torch.bool, torch.uint8))
+    ldm, step = mask.stride()
+    if K > 1 and step != 1:
+        raise ValueError("mask must have contiguous rows")
+    if N == 1 or ldm == 0:  # one row, or one row expanded
+        return mask.data_ptr(), 0
+    if ldm < K:
+        raise ValueError("mask must not have overlapping rows")
+    return mask.data_ptr(), ldm
 
 
 def logprobs_workspace_bytes(N: int, K: int, dtype) -> int:
@@ -701,27 +732,32 @@ def logprobs(scores, y=None, top: int = 0, scale: float = 1.0, mask=None,
     classes that are False take no part. ``workspace`` may be a zeroed uint8
     device tensor of ``logprobs_workspace_bytes(...)`` bytes."""
     torch = _torch()
-    ld = _check_rows(scores, "scores", _floats())
-    N, K = scores.shape
+    N, K, ld, dt, index = _rows(scores, "scores")
     device = scores.device
-    if y is not None:
-        _check_vec(y, "y", torch.int32, N, device)
-    mptr, ldm = _mask_arg(mask, N, K, device)
-    dt = _dt(scores)
-    # logp, entropy and stats, and the alternatives, in one allocation each
-    f = torch.empty(4 * N, dtype=torch.float32, device=device)
-    entropy, stats = f[2 * N:3 * N], f[:2 * N].view(N, 2)
-    logp = f[3 * N:] if y is not None else None
-    ids = torch.empty((N, top), dtype=torch.int32, device=device) if top > 0 else None
-    best = torch.empty((N, top), dtype=torch.float32, device=device) if top > 0 else None
-    need = _need("hd_logprobs_workspace_bytes", device.index, N, K, dt)
-    ws = workspace if workspace is not None else _workspace(device, need, ("logprobs", N, K, dt))
-    st = lib().hd_logprobs(scores.data_ptr(), ld, mptr, ldm, _ptr(y), scale, _ptr(logp),
-                           entropy.data_ptr(), stats.data_ptr(), _ptr(ids), _ptr(best), N, K, top,
-                           dt, _ptr(ws), ws.numel() if ws is not None else 0,
-                           _stream_ptr(device))
+    yptr = _vec(y, "y", torch.int32, N, index) if y is not None else None
+    mptr, ldm = (None, 0) if mask is None else _mask_arg(mask, N, K, index)
+    each = N * top if top > 0 else 0
+    buf = torch.empty(4 * N + 2 * each, dtype=torch.float32, device=device)
+    at = buf.data_ptr()  # stats, entropy, logp, ids, top_logp
+    ws = workspace
+    if ws is None:
+        need = _need("hd_logprobs_workspace_bytes", index, N, K, dt)
+        if need:
+            ws = _workspace(device, need, ("logprobs", N, K, dt))
+    st = lib().hd_logprobs(scores.data_ptr(), ld, mptr, ldm, yptr, scale,
+                           at + 12 * N if yptr is not None else None, at + 8 * N, at,
+                           at + 16 * N if each else None, at + 16 * N + 4 * each if each else None,
+                           N, K, top, dt, _ptr(ws), ws.numel() if ws is not None else 0,
+                           _raw_stream(index))
     _raise(st, "hd_logprobs")
-    return LogProbs(logp, entropy, stats, ids, best)
+    if each:
+        stats, entropy, logp, ids, best = buf.split_with_sizes((2 * N, N, N, each, each))
+        ids, best = ids.view(torch.int32).view(N, top), best.view(N, top)
+    else:
+        stats, entropy, logp = buf.split_with_sizes((2 * N, N, N))
+        ids = torch.empty((N, top), dtype=torch.int32, device=device) if top > 0 else None
+        best = torch.empty((N, top), dtype=torch.float32, device=device) if top > 0 else None
+    return LogProbs(logp if yptr is not None else None, entropy, stats.view(N, 2), ids, best)
 
 
 def logprobs_grad(scores, y, lp: LogProbs, g_logp=None, g_entropy=None, scale: float = 1.0,
@@ -730,27 +766,25 @@ def logprobs_grad(scores, y, lp: LogProbs, g_logp=None, g_entropy=None, scale: f
     scores, [N, K] of their dtype; ``lp`` is what ``logprobs`` gave for the same
     scores, scale and mask. ``out`` may be the scores themselves."""
     torch = _torch()
-    ld = _check_rows(scores, "scores", _floats())
-    N, K = scores.shape
-    device = scores.device
-    if y is not None:
-        _check_vec(y, "y", torch.int32, N, device)
-    for t, name in ((g_logp, "g_logp"), (g_entropy, "g_entropy"), (lp.entropy, "entropy")):
-        if t is not None:
-            _check_vec(t, name, torch.float32, N, device)
-    if (tuple(lp.stats.shape) != (N, 2) or lp.stats.dtype != torch.float32
-            or not lp.stats.is_contiguous() or lp.stats.device != device):
+    f32 = torch.float32
+    N, K, ld, dt, index = _rows(scores, "scores")
+    yptr = _vec(y, "y", torch.int32, N, index) if y is not None else None
+    glp = _vec(g_logp, "g_logp", f32, N, index) if g_logp is not None else None
+    gep = _vec(g_entropy, "g_entropy", f32, N, index) if g_entropy is not None else None
+    entropy, stats = _vec(lp.entropy, "entropy", f32, N, index), lp.stats
+    if (stats.shape != (N, 2) or stats.dtype != f32 or not stats.is_contiguous()
+            or stats.get_device() != index):
         raise ValueError("stats must be float32 [N, 2] on the scores' device")
-    mptr, ldm = _mask_arg(mask, N, K, device)
+    mptr, ldm = (None, 0) if mask is None else _mask_arg(mask, N, K, index)
     if out is None:
-        out = torch.empty((N, K), dtype=scores.dtype, device=device)
-    elif tuple(out.shape) != (N, K) or out.dtype != scores.dtype or out.device != device:
-        raise ValueError("out must have the scores' shape, dtype and device")
-    ldd = _check_rows(out, "out", _floats())
-    st = lib().hd_logprobs_grad(scores.data_ptr(), ld, mptr, ldm, _ptr(y), scale,
-                                lp.stats.data_ptr(), lp.entropy.data_ptr(), _ptr(g_logp),
-                                _ptr(g_entropy), out.data_ptr(), ldd, N, K, _dt(scores),
-                                _stream_ptr(device))
+        out, ldd = torch.empty(N, K, dtype=scores.dtype, device=scores.device), K
+    else:
+        _, _, ldd, out_dt, out_index = _rows(out, "out")
+        if out.shape != (N, K) or out_dt != dt or out_index != index:
+            raise ValueError("out must have the scores' shape, dtype and device")
+    st = lib().hd_logprobs_grad(scores.data_ptr(), ld, mptr, ldm, yptr, scale, stats.data_ptr(),
+                                entropy, glp, gep, out.data_ptr(), ldd, N, K, dt,
+                                _raw_stream(index))
     _raise(st, "hd_logprobs_grad")
     return out
 
@@ -765,16 +799,15 @@ class Checkpoint:
 def ckpt_store(H, out=None) -> Checkpoint:
     """Keeps activations ``H`` [N, D] (float32 or bfloat16) in 8 bits, 64 rows of a
     column sharing a scale. ``out``: a Checkpoint of the same sizes to overwrite."""
-    torch = _torch()
-    ld = _check_rows(H, "H", _floats())
-    N, D = H.shape
+    N, D, ld, dt, index = _rows(H, "H")
+    nbytes = _need("hd_ckpt_bytes", index, N, D)
     if out is None:
-        out = Checkpoint(torch.empty(int(lib().hd_ckpt_bytes(N, D)), dtype=torch.uint8,
-                                     device=H.device), N, D)
-    elif (out.N, out.D) != (N, D) or out.image.device != H.device:
+        torch = _torch()
+        out = Checkpoint(torch.empty(nbytes, dtype=torch.uint8, device=H.device), N, D)
+    elif (out.N, out.D) != (N, D) or out.image.get_device() != index:
         raise ValueError("out must be a checkpoint of H's sizes on its device")
-    st = lib().hd_ckpt_store(H.data_ptr(), ld, N, D, _dt(H), out.image.data_ptr(),
-                             out.image.numel(), _stream_ptr(H.device))
+    st = lib().hd_ckpt_store(H.data_ptr(), ld, N, D, dt, out.image.data_ptr(), nbytes,
+                             _raw_stream(index))
     _raise(st, "hd_ckpt_store")
     return out
 
@@ -782,15 +815,22 @@ def ckpt_store(H, out=None) -> Checkpoint:
 def ckpt_load(kept: Checkpoint, dtype=None, out=None):
     """The activations a checkpoint stands for, [N, D] (float32 unless ``dtype`` or
     ``out`` says bfloat16)."""
-    torch = _torch()
-    N, D = kept.N, kept.D
+    N, D, image = kept.N, kept.D, kept.image
     if out is None:
-        out = torch.empty((N, D), dtype=dtype or torch.float32, device=kept.image.device)
-    elif tuple(out.shape) != (N, D) or out.device != kept.image.device:
-        raise ValueError("out must be [N, D] on the checkpoint's device")
-    ld = _check_rows(out, "out", _floats())
-    st = lib().hd_ckpt_load(kept.image.data_ptr(), out.data_ptr(), ld, N, D, _dt(out),
-                            _stream_ptr(out.device))
+        torch = _torch()
+        dtype = dtype or torch.float32
+        dt, ld = (_codes or _float_codes()).get(dtype), D
+        if dt is None:
+            raise TypeError("dtype must be float32 or bfloat16")
+        out = torch.empty(N, D, dtype=dtype, device=image.device)
+    else:
+        _, _, ld, dt, index = _rows(out, "out")
+        if out.shape != (N, D) or index != image.get_device():
+            raise ValueError("out must be [N, D] on the checkpoint's device")
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError("out has another dtype")
+    st = lib().hd_ckpt_load(image.data_ptr(), out.data_ptr(), ld, N, D, dt,
+                            _raw_stream(image.get_device()))
     _raise(st, "hd_ckpt_load")
     return out
 
@@ -800,25 +840,23 @@ def ckpt_class_grad(dS, kept: Checkpoint, out=None, accumulate: bool = False):
     ``dS`` [N, K] (float32 or bfloat16) and the checkpoint of the encodings H.
     ``out`` receives it, or with ``accumulate`` has it added."""
     torch = _torch()
-    ld = _check_rows(dS, "dS", _floats())
-    N, K = dS.shape
-    D = kept.D
+    N, K, ld, dt, index = _rows(dS, "dS")
+    D, image = kept.D, kept.image
     if N != kept.N:
         raise ValueError("shape mismatch")
-    if dS.device != kept.image.device:
+    if image.get_device() != index:
         raise ValueError("dS and the checkpoint must be on one device")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((K, D), dtype=torch.float32, device=dS.device)
+        out = torch.empty(K, D, dtype=torch.float32, device=dS.device)
     else:
         _check_dev(out)
-        if out.dtype != torch.float32 or tuple(out.shape) != (K, D) or out.device != dS.device:
+        if out.dtype != torch.float32 or out.shape != (K, D) or out.get_device() != index:
             raise ValueError("out must be float32 [K, D] on dS's device")
-    need = _need("hd_ckpt_class_grad_workspace_bytes", dS.device.index, N, D, K, _dt(dS))
+    need = _need("hd_ckpt_class_grad_workspace_bytes", index, N, D, K, dt)
     ws = torch.empty(need, dtype=torch.uint8, device=dS.device)
-    st = lib().hd_ckpt_class_grad(dS.data_ptr(), ld, kept.image.data_ptr(), out.data_ptr(), N, D,
-                                  K, _dt(dS), int(accumulate), ws.data_ptr(), ws.numel(),
-                                  _stream_ptr(dS.device))
+    st = lib().hd_ckpt_class_grad(dS.data_ptr(), ld, image.data_ptr(), out.data_ptr(), N, D, K,
+                                  dt, accumulate, ws.data_ptr(), need, _raw_stream(index))
     _raise(st, "hd_ckpt_class_grad")
     return out

@@ -46,17 +46,25 @@ __global__ __launch_bounds__(256) void ckpt_store_kernel(const T* __restrict__ H
   const bool pair = COLS == 2 && d + 1 < D;
   float v[COLS][kRows];
   const T* p = H + n0 * ldh + d;
+  // rows past the end read the last one again, so that no load waits on a branch
+  const int last = N - n0 < kRows ? (int)(N - n0) - 1 : kRows - 1;
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    const bool in = n0 + r < N;
+    const int64_t at = (r < last ? r : last) * ldh;
     if constexpr (COLS == 2) {
-      uint32_t w = 0;
-      if (in) w = pair ? *reinterpret_cast<const uint32_t*>(p + r * ldh) : p[r * ldh];
+      const uint32_t w =
+          pair ? *reinterpret_cast<const uint32_t*>(p + at) : (uint32_t)p[at];
       v[0][r] = __uint_as_float(w << 16);
       v[1][r] = __uint_as_float(w & 0xffff0000u);
     } else {
-      v[0][r] = in ? load_elem(p, r * ldh) : 0.0f;
+      v[0][r] = load_elem(p, at);
     }
+  }
+  if (last < kRows - 1) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) v[c][r] = r <= last ? v[c][r] : 0.0f;
   }
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {

@@ -290,17 +290,21 @@ __device__ __forceinline__ void join_waves(Stats& st, uint64_t& list, float c, i
 // Workspace of a split call: a counter for each row, then for each (row, part)
 // kPartWords words: m, sum, ez, and the list's keys.
 constexpr int kPartWords = 4 + 2 * kMaxTop;
+constexpr int kMaxParts = 64;
 struct Split {
   int parts;         // of a row
   int64_t part_len;  // scores in a part, a multiple of the step of a workgroup
   uint32_t *tickets, *words;
 };
 
-__device__ __forceinline__ uint32_t take_word(uint32_t* p) {
-  return __hip_atomic_exchange(p, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Words that pass between workgroups: device-scope stores, performed before the writer
+// takes its ticket, and device-scope loads after the last ticket. (Unlike exchanges, the
+// loads of all parts are in flight together.)
+__device__ __forceinline__ uint32_t get_word(const uint32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void put_word(uint32_t* p, uint32_t v) {
-  (void)__hip_atomic_exchange(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 template <typename T, bool TOP, bool MASK>
@@ -396,20 +400,33 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     st = stats_none();
     list.key = 0;
     uint32_t* words = sp.words + (int64_t)n * sp.parts * kPartWords;
-    for (int p = wave; p < sp.parts; p += WAVES) {
+    constexpr int EACH = kMaxParts / WAVES;
+    uint32_t head[EACH];
+    uint64_t keys[EACH];
+    const int at = 63 - lane;  // the list in lanes 63, 62, ...
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int p = wave + WAVES * i;
       uint32_t* w = words + (int64_t)p * kPartWords;
-      uint32_t s = 0;
-      if (lane < 3) s = take_word(w + lane);
-      uint64_t other = 0;
-      const int at = 63 - lane;  // the list in lanes 63, 62, ...
-      if (TOP && lane >= kMaxTop && at < o.top)
-        other = (uint64_t)take_word(w + 5 + 2 * at) << 32 | take_word(w + 4 + 2 * at);
-      const Stats b{__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)s, 0)),
-                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)s, 1)),
-                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)s, 2))};
-      st = stats_join(st, b, c);
-      if (TOP) list.key = merge64(lane < kMaxTop ? list.key : other, lane);
+      head[i] = 0, keys[i] = 0;
+      if (p >= sp.parts) continue;
+      if (lane < 3) head[i] = get_word(w + lane);
+      if (TOP && at < o.top)
+        keys[i] = (uint64_t)get_word(w + 5 + 2 * at) << 32 | get_word(w + 4 + 2 * at);
     }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int p = wave + WAVES * i;
+      if (p >= sp.parts) break;
+      const Stats b{__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)head[i], 0)),
+                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)head[i], 1)),
+                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)head[i], 2))};
+      st = stats_join(st, b, c);
+      if (TOP) list.key = merge64(lane < kMaxTop ? list.key : keys[i], lane);
+    }
+    // left zeroed
+    for (int64_t i = threadIdx.x; i < (int64_t)sp.parts * kPartWords; i += kLongThreads)
+      words[i] = 0;
     join_waves<TOP>(st, list.key, c, lane, wave, WAVES, sh_st, sh_key);
   }
   if (wave != 0) return;
@@ -424,7 +441,7 @@ Split split_of(int64_t N, int64_t K, int len) {
   Split s{1, 0, nullptr, nullptr};
   const int64_t step = (int64_t)kLongThreads * len, steps = cdiv(K, step);
   int64_t parts = cdiv(2 * (int64_t)num_cus(), N);
-  if (parts > 64) parts = 64;
+  if (parts > kMaxParts) parts = kMaxParts;
   if (parts > steps / 2) parts = steps / 2;
   if (parts < 1) parts = 1;
   const int64_t per = cdiv(steps, parts);
