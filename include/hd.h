@@ -329,10 +329,11 @@ const char *hd_infer_kernel(int64_t N, int64_t F, int64_t D, int64_t K, hd_dtype
  * hd_nibble_product: Y[n][o] = act( sum_i X[n][i] w[o][i] ), X[N][inner] of x_dt,
  * Y[N][outer] of y_dt, sums in fp32 (products of codes and X exact), one
  * rounding to y_dt. An X of fp32 is used in full. `zeros` says whether the
- * image was made with zero points. Made for few rows (a single reading, a
- * request batch): up to 64 rows read the weights once.
+ * image was made with zero points. Made for few rows, a single reading or a
+ * request batch. workspace: hd_nibble_workspace_bytes(...) bytes (0 for a single row of
+ * usual length), contents irrelevant before and undefined after the call.
  * Limits: outer, inner <= 2^30, ceil(outer/16) * ceil(inner/128) <= 2^24,
- * N <= 2^20.
+ * N <= 4096.
  */
 size_t hd_nibble_bytes(int64_t outer, int64_t inner, int64_t group);
 hd_status hd_nibble_pack(const uint8_t *codes, const uint16_t *scales, const uint8_t *zeros,
@@ -345,7 +346,9 @@ hd_status hd_nibble_unpack(const void *image, int zeros, float *W, int64_t outer
                            int64_t group, hipStream_t stream);
 hd_status hd_nibble_product(const void *X, int64_t ldx, const void *image, int zeros, void *Y,
                             int64_t ldy, int64_t N, int64_t outer, int64_t inner, int64_t group,
-                            hd_dtype x_dt, hd_dtype y_dt, hd_act act, hipStream_t stream);
+                            hd_dtype x_dt, hd_dtype y_dt, hd_act act, void *workspace,
+                            size_t workspace_bytes, hipStream_t stream);
+size_t hd_nibble_workspace_bytes(int64_t N, int64_t inner, hd_dtype x_dt);
 
 /*
  * Log probabilities of given classes, with the entropy and the best

@@ -53,6 +53,7 @@ SYMBOLS = (
     "hd_nibble_pack",
     "hd_nibble_quantize",
     "hd_nibble_unpack",
+    "hd_nibble_workspace_bytes",
     "hd_nibble_product",
     "hd_logprobs_workspace_bytes",
     "hd_logprobs",
@@ -135,8 +136,10 @@ def lib():
         L.hd_nibble_quantize.restype = i32
         L.hd_nibble_unpack.argtypes = [vp, i32, vp, i64, i64, i64, vp]
         L.hd_nibble_unpack.restype = i32
+        L.hd_nibble_workspace_bytes.argtypes = [i64, i64, i32]
+        L.hd_nibble_workspace_bytes.restype = sz
         L.hd_nibble_product.argtypes = [vp, i64, vp, i32, vp, i64, i64, i64, i64, i64, i32, i32,
-                                        i32, vp]
+                                        i32, vp, sz, vp]
         L.hd_nibble_product.restype = i32
         L.hd_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
         L.hd_logprobs_workspace_bytes.restype = sz
@@ -676,9 +679,14 @@ def nibble_product(X, w: NibbleWeights, act: str = "identity", dtype=None, out=N
             raise ValueError("out must be [N, outer] on X's device")
         if dtype is not None and out.dtype != dtype:
             raise TypeError("out has another dtype")
+    need = _need("hd_nibble_workspace_bytes", index, N, inner, x_dt)
+    ws = None
+    if need:
+        torch = _torch()
+        ws = torch.empty(need, dtype=torch.uint8, device=X.device)
     st = lib().hd_nibble_product(X.data_ptr(), ldx, image.data_ptr(), w.zeros, out.data_ptr(),
-                                 ldy, N, outer, inner, w.group, x_dt, y_dt, ACTS[act],
-                                 _raw_stream(index))
+                                 ldy, N, outer, inner, w.group, x_dt, y_dt, ACTS[act], _ptr(ws),
+                                 need, _raw_stream(index))
     _raise(st, "hd_nibble_product")
     return out
 

@@ -10,8 +10,8 @@
 //   split eight codes and four conversions make eight bf16 values, exact;
 // * sum x*q and sum x run through separate chains, fresh for each group, and
 //   s * (sum x*q - z * sum x) is added in fp32. The second chain multiplies X by a
-//   constant operand, once for all tiles of outputs, and its result lies in
-//   the lanes that need it;
+//   constant operand, once for all tiles of outputs; its result lies in the lanes
+//   that need it, as the value that the first chain starts from;
 // * fp32 X is the exact sum of three bf16 values (its 24 bits cut in three), one
 //   matrix instruction each. Products of 4 and 8 bits are exact in fp32.
 //
@@ -213,12 +213,14 @@ struct XLoad<bf16raw> {
   __device__ __forceinline__ void full(const bf16raw* p) {
     v = *reinterpret_cast<const u32x4_a2*>(p);
   }
-  __device__ __forceinline__ void tail(const bf16raw* p, int64_t left) {
+  __device__ __forceinline__ void tail(const bf16raw* row, int64_t i, int64_t I) {
+    uint32_t u[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t a = 2 * e < left ? p[2 * e] : 0, b = 2 * e + 1 < left ? p[2 * e + 1] : 0;
-      v[e] = a | b << 16;
-    }
+    for (int e = 0; e < 8; ++e) u[e] = row[i + e < I ? i + e : I - 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = i + e < I ? u[e] : 0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = u[2 * e] | u[2 * e + 1] << 16;
   }
   __device__ __forceinline__ void parts(bf16x8 (&out)[1]) const { out[0] = as_bf16x8(v); }
 };
@@ -232,9 +234,11 @@ struct XLoad<float> {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
   }
-  __device__ __forceinline__ void tail(const float* p, int64_t left) {
+  __device__ __forceinline__ void tail(const float* row, int64_t i, int64_t I) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] = row[i + e < I ? i + e : I - 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e < I ? v[e] : 0.0f;
   }
   __device__ __forceinline__ void parts(bf16x8 (&out)[3]) const {
     u32x4 w[3];
@@ -265,35 +269,85 @@ __device__ __noinline__ float product_one(const T* x, const uint8_t* image, cons
   return y;
 }
 
-// W waves; NT tiles of 16 rows of X, TD tiles of 16 outputs, GPT groups in an input tile.
-template <typename T, int GPT, bool ZERO, int NT, int TD>
+// What a wave loads of an input tile: codes, scales and zero points of TD output
+// tiles, and X.
+template <int GPT, bool ZERO, int TD>
+struct WeightFrag {
+  u32x4 code[TD];
+  u32x2 sc[TD][GPT];
+  uint32_t zp[TD][ZERO ? GPT : 1];
+};
+
+// Large matrices are read once and do not fit the caches: their loads pass by
+// (STREAM). Reading alone reaches 6.3 TB/s with ordinary loads and 7.1 so.
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load_weights(const V* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(p);
+  else
+    return *p;
+}
+
+// Eight inputs from column 8 ch of a row, as operands.
+template <typename T>
+__device__ __forceinline__ void x_operands(const T* row, int64_t ch, int64_t I,
+                                           bf16x8 (&out)[XLoad<T>::kParts]) {
+  XLoad<T> v;
+  if (8 * ch + 8 <= I)
+    v.full(row + 8 * ch);
+  else
+    v.tail(row, 8 * ch, I);
+  v.parts(out);
+}
+
+// X as operands in memory: [input tile][tile of 16 rows][step][part][lane]. Rows past N
+// are zero.
+template <typename T>
+__global__ __launch_bounds__(256) void nibble_x_kernel(const T* __restrict__ X, int64_t ldx,
+                                                       int64_t N, int64_t I, int ntiles,
+                                                       int64_t total, bf16x8* out) {
+  constexpr int P = XLoad<T>::kParts;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  const int lane = (int)at & 63, s = (int)(at >> 6) & 3;
+  const int64_t tile = at >> 8;
+  const int64_t n = tile % ntiles * 16 + lane % 16;
+  bf16x8 parts[P] = {};
+  if (n < N) x_operands(X + n * ldx, tile / ntiles * 16 + 4 * s + lane / 16, I, parts);
+#pragma unroll
+  for (int p = 0; p < P; ++p) out[((at >> 6) * P + p) * 64 + lane] = parts[p];
+}
+
+// NT tiles of 16 rows of X, TD tiles of 16 outputs, GPT groups in an input tile.
+// XLDS (NT = 1): the workgroup first lays X out in LDS as operands, [input tile][step][part]
+// [l / 16][row]; the lanes of columns past N read the last row's. Otherwise nibble_x_kernel
+// has done so in memory (xop): a wave's load is 1 KiB in a row, where reading the rows
+// of X themselves meets few of the L2's channels (strides of powers of two) and
+// takes as long for one row as for sixteen.
+template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
 __global__ __launch_bounds__(512) void nibble_product_kernel(
-    const T* __restrict__ X, int64_t ldx, const uint8_t* __restrict__ image, int64_t scales_at,
-    int64_t zeros_at, void* __restrict__ Y, int64_t ldy, int64_t N, int64_t O, int64_t I,
-    int64_t otiles, int itiles, int y_dt, int act) {
+    const T* __restrict__ X, int64_t ldx, const bf16x8* __restrict__ xop, int ntiles,
+    const uint8_t* __restrict__ image, int64_t scales_at, int64_t zeros_at, void* __restrict__ Y,
+    int64_t ldy, int64_t N, int64_t O, int64_t I, int64_t otiles, int itiles, int y_dt, int act) {
   constexpr int P = XLoad<T>::kParts;
   constexpr int STEPS = 4 / GPT;  // matrix steps of 32 inputs in a group
-  extern __shared__ f32x4 sums[];  // [W][TD][NT][64]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  typedef WeightFrag<GPT, ZERO, TD> Frag;
+  extern __shared__ f32x4 sums[];  // [waves][TD][NT][64]; XLDS: X first
+  // (the wave's number in a scalar register: addresses of its tiles too)
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  const int64_t ot0 = (int64_t)blockIdx.x * TD;
-  const int64_t n0 = (int64_t)blockIdx.y * (16 * NT);
+  // the workgroups of one set of output tiles follow each other
+  const int nblocks = (ntiles + NT - 1) / NT;
+  const int64_t ot0 = (int64_t)(blockIdx.x / nblocks) * TD;
+  const int nt0 = (int)(blockIdx.x % nblocks) * NT;
   const bf16raw* scales = reinterpret_cast<const bf16raw*>(image + scales_at);
   const uint8_t* zeros = image + zeros_at;
 
-  const T* xrow[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int64_t n = n0 + 16 * t + col;
-    xrow[t] = X + (n < N ? n : N - 1) * ldx + 8 * quad;  // rows past N: any, never written
-  }
   // per output tile, the row of input tiles (tiles past the last repeat it)
   int64_t row[TD];
 #pragma unroll
-  for (int d = 0; d < TD; ++d) {
-    const int64_t ot = ot0 + d < otiles ? ot0 + d : otiles - 1;
-    row[d] = ot * itiles;
-  }
+  for (int d = 0; d < TD; ++d) row[d] = (ot0 + d < otiles ? ot0 + d : otiles - 1) * itiles;
 
   f32x4 acc[TD][NT];
 #pragma unroll
@@ -305,84 +359,125 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
   for (int e = 0; e < 4; ++e) ones_w[e] = ZERO ? 0x3f803f80u : 0xc100c100u;  // 1, or -8
   const bf16x8 ones = as_bf16x8(ones_w);
 
-  for (int it = wave; it < itiles; it += waves) {
-    u32x4 code[TD];
-    uint2 sc[TD][GPT];
-    uint32_t zp[TD][GPT];
+  auto load = [&](int it, Frag& f) {
 #pragma unroll
     for (int d = 0; d < TD; ++d) {
       const int64_t tile = row[d] + it;
-      code[d] = reinterpret_cast<const u32x4*>(image)[tile * 64 + lane];
+      f.code[d] = load_weights<STREAM>(reinterpret_cast<const u32x4*>(image + tile * 1024) + lane);
 #pragma unroll
       for (int g = 0; g < GPT; ++g) {
-        const int64_t at = (tile * 4 + quad) * GPT + g;
-        sc[d][g] = reinterpret_cast<const uint2*>(scales)[at];
-        if (ZERO) zp[d][g] = reinterpret_cast<const uint32_t*>(zeros)[at];
+        f.sc[d][g] = load_weights<STREAM>(
+            reinterpret_cast<const u32x2*>(scales + tile * (16 * GPT)) + quad * GPT + g);
+        if (ZERO)
+          f.zp[d][g] = load_weights<STREAM>(
+              reinterpret_cast<const uint32_t*>(zeros + tile * (16 * GPT)) + quad * GPT + g);
       }
     }
-    const int64_t i0 = (int64_t)it * kTileI;
-    const bool full = i0 + kTileI <= I;
-    XLoad<T> x[NT][4];
+  };
+  struct Operands {
+    bf16x8 v[XLDS ? 1 : NT][4][P];
+  };
+  auto load_x = [&](int it, Operands& x) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < (XLDS ? 0 : NT); ++t) {
+      const int nt = nt0 + t < ntiles ? nt0 + t : ntiles - 1;  // (never written)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int64_t i = i0 + 32 * s;
-        if (full || i + 8 * quad + 8 <= I)
-          x[t][s].full(xrow[t] + i);
-        else
-          x[t][s].tail(xrow[t] + i, I - i - 8 * quad);
-      }
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          x.v[t][s][p] = xop[((((int64_t)it * ntiles + nt) * 4 + s) * P + p) * 64 + lane];
+    }
+  };
+  const bf16x8* xs = reinterpret_cast<const bf16x8*>(sums);
+  auto multiply = [&](const Frag& f, const Operands& x, int it) {
 #pragma unroll
     for (int g = 0; g < GPT; ++g) {
-      f32x4 sum[TD][NT], one[NT];
+      bf16x8 xp[STEPS][NT][P];
+      f32x4 one[NT];  // -8 sum x, or sum x
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         one[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int d = 0; d < TD; ++d) sum[d][t] = f32x4{0, 0, 0, 0};
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            if constexpr (XLDS)
+              xp[s][t][p] = xs[((it * 4 + g * STEPS + s) * P + p) * 4 * (int)N];
+            else
+              xp[s][t][p] = x.v[t][g * STEPS + s][p];
+            one[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xp[s][t][p], one[t], 0, 0, 0);
+          }
       }
 #pragma unroll
-      for (int s = g * STEPS; s < (g + 1) * STEPS; ++s) {
-        bf16x8 xp[NT][P];
+      for (int d = 0; d < TD; ++d) {
+        f32x4 sum[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          x[t][s].parts(xp[t]);
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int p = 0; p < P; ++p)
-            one[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xp[t][p], one[t], 0, 0, 0);
-        }
+          for (int r = 0; r < 4; ++r)
+            sum[t][r] = ZERO ? -(float)((f.zp[d][g] >> (8 * r)) & 255u) * one[t][r] : one[t][r];
 #pragma unroll
-        for (int d = 0; d < TD; ++d) {
-          const bf16x8 q = codes_bf16(code[d][s]);
+        for (int s = 0; s < STEPS; ++s) {
+          const bf16x8 q = codes_bf16(f.code[d][g * STEPS + s]);
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int p = 0; p < P; ++p)
-              sum[d][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, xp[t][p], sum[d][t], 0, 0, 0);
+              sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, xp[s][t][p], sum[t], 0, 0, 0);
         }
-      }
-#pragma unroll
-      for (int d = 0; d < TD; ++d) {
-        float sf[4] = {__uint_as_float(sc[d][g].x << 16),
-                       __uint_as_float(sc[d][g].x & 0xffff0000u),
-                       __uint_as_float(sc[d][g].y << 16),
-                       __uint_as_float(sc[d][g].y & 0xffff0000u)};
+        const u32x2 sc = f.sc[d][g];
+        const float sf[4] = {__uint_as_float(sc[0] << 16), __uint_as_float(sc[0] & 0xffff0000u),
+                             __uint_as_float(sc[1] << 16), __uint_as_float(sc[1] & 0xffff0000u)};
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float v;
-            if (ZERO)
-              v = fmaf(-(float)((zp[d][g] >> (8 * r)) & 255u), one[t][r], sum[d][t][r]);
-            else
-              v = sum[d][t][r] + one[t][r];
-            acc[d][t][r] = fmaf(sf[r], v, acc[d][t][r]);
-          }
+          for (int r = 0; r < 4; ++r) acc[d][t][r] = fmaf(sf[r], sum[t][r], acc[d][t][r]);
       }
     }
+  };
+
+  // Two tiles' registers: one tile's loads are in flight while the other is multiplied.
+  // They are issued without a condition, past the end for the last tile again, so that a
+  // wait covers only the older ones; the scheduling barriers keep the compiler from
+  // sinking them to their uses.
+  const int own = itiles > wave ? (itiles - wave + waves - 1) / waves : 0;
+  auto nth = [&](int i) { return wave + waves * (i < own ? i : own - 1); };
+  Frag f[2];
+  Operands x[2];
+  if (own > 0) {
+    load(nth(0), f[0]);
+    load_x(nth(0), x[0]);
+  }
+  if (XLDS) {
+    const int rows = (int)N, chunks = itiles * 16;  // of eight inputs
+    bf16x8* dst = reinterpret_cast<bf16x8*>(sums);
+    for (int c = threadIdx.x; c < chunks * rows; c += blockDim.x) {
+      const int n = c / chunks, ch = c % chunks;
+      bf16x8 parts[P];
+      x_operands(X + n * ldx, ch, I, parts);
+#pragma unroll
+      for (int p = 0; p < P; ++p) dst[((ch / 4 * P + p) * 4 + ch % 4) * rows + n] = parts[p];
+    }
+    __syncthreads();
+    xs += quad * rows + (col < rows ? col : rows - 1);
+  }
+  if (own > 0) {
+    int i = 0;
+    for (; i + 2 <= own; i += 2) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        load(nth(i + r + 1), f[1 - r]);
+        load_x(nth(i + r + 1), x[1 - r]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f[r], x[r], nth(i + r));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (i < own) multiply(f[0], x[0], nth(i));
   }
 
+  if (XLDS) __syncthreads();  // X is no longer read
+  const int64_t n0 = (int64_t)nt0 * 16;
 #pragma unroll
   for (int d = 0; d < TD; ++d)
 #pragma unroll
@@ -413,9 +508,12 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
   }
 }
 
+constexpr size_t kXLds = 64 * 1024;  // X in LDS: two workgroups to a compute unit
+
 struct ProductArgs {
   const void* X;
   int64_t ldx;
+  const bf16x8* xop;  // null: X in LDS
   const uint8_t* image;
   void* Y;
   int64_t ldy, N, O, I;
@@ -424,23 +522,46 @@ struct ProductArgs {
   hipStream_t stream;
 };
 
-template <typename T, int GPT, bool ZERO, int NT, int TD>
+constexpr int parts_of(int x_dt) { return x_dt == 0 ? 3 : 1; }
+
+// Bytes of X as operands: in LDS (few rows), in memory.
+size_t x_lds_bytes(int64_t N, int64_t itiles, int x_dt) {
+  return (size_t)N * itiles * 256 * parts_of(x_dt);
+}
+bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
+  return N <= 16 && x_lds_bytes(N, itiles, x_dt) <= kXLds;
+}
+
+template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
 hipError_t launch_product_as(const ProductArgs& a) {
-  int waves = a.L.itiles < 8 ? (int)a.L.itiles : 8;
-  const size_t lds = sizeof(f32x4) * 64 * TD * NT * waves;
-  const dim3 grid((unsigned)cdiv(a.L.otiles, TD), (unsigned)cdiv(a.N, 16 * NT));
-  hipLaunchKernelGGL((nibble_product_kernel<T, GPT, ZERO, NT, TD>), grid, dim3(64 * waves), lds,
-                     a.stream, static_cast<const T*>(a.X), a.ldx, a.image, (int64_t)a.L.scales,
-                     (int64_t)a.L.zeros, a.Y, a.ldy, a.N, a.O, a.I, a.L.otiles, (int)a.L.itiles,
-                     a.y_dt, a.act);
+  const int waves = a.L.itiles < 8 ? (int)a.L.itiles : 8;
+  const int ntiles = (int)cdiv(a.N, 16);
+  size_t lds = sizeof(f32x4) * 64 * TD * NT * waves;
+  if (XLDS) {
+    const size_t x = x_lds_bytes(a.N, a.L.itiles, sizeof(T) == 4 ? 0 : 1);
+    if (x > lds) lds = x;
+  }
+  hipLaunchKernelGGL((nibble_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS>),
+                     dim3((unsigned)(cdiv(a.L.otiles, TD) * cdiv(ntiles, NT))), dim3(64 * waves),
+                     lds, a.stream, static_cast<const T*>(a.X), a.ldx, a.xop, ntiles, a.image,
+                     (int64_t)a.L.scales, (int64_t)a.L.zeros, a.Y, a.ldy, a.N, a.O, a.I,
+                     a.L.otiles, (int)a.L.itiles, a.y_dt, a.act);
   return hipGetLastError();
 }
 
+constexpr size_t kStreamBytes = size_t(192) << 20;
+
 template <typename T, int GPT, bool ZERO>
 hipError_t launch_product_rows(const ProductArgs& a) {
-  if (a.N <= 16) return launch_product_as<T, GPT, ZERO, 1, 2>(a);
-  if (a.N <= 32) return launch_product_as<T, GPT, ZERO, 2, 2>(a);
-  return launch_product_as<T, GPT, ZERO, 4, 1>(a);
+  const bool stream = a.L.scales > kStreamBytes;
+  if (!a.xop)
+    return stream ? launch_product_as<T, GPT, ZERO, 1, 2, true, true>(a)
+                  : launch_product_as<T, GPT, ZERO, 1, 2, false, true>(a);
+  if (a.N <= 16 && stream) return launch_product_as<T, GPT, ZERO, 1, 2, true, false>(a);
+  // (fp32's three parts of two row tiles would not fit the registers)
+  if (a.N <= 16 || sizeof(T) == 4)
+    return launch_product_as<T, GPT, ZERO, 1, 2, false, false>(a);
+  if constexpr (sizeof(T) == 2) return launch_product_as<T, GPT, ZERO, 2, 2, false, false>(a);
 }
 
 template <typename T>
@@ -510,12 +631,33 @@ hipError_t launch_nibble_unpack(const void* image, float* W, int64_t O, int64_t 
   return hipGetLastError();
 }
 
+size_t nibble_ws_bytes(int64_t N, int64_t I, int x_dt) {
+  const int64_t itiles = cdiv(I, kTileI);
+  if (x_in_lds(N, itiles, x_dt)) return 0;
+  return (size_t)cdiv(N, 16) * itiles * 4096 * parts_of(x_dt);
+}
+
 hipError_t launch_nibble_product(const void* X, int64_t ldx, const void* image, void* Y,
                                  int64_t ldy, int64_t N, int64_t O, int64_t I, int G,
-                                 bool with_zeros, int x_dt, int y_dt, int act,
+                                 bool with_zeros, int x_dt, int y_dt, int act, void* workspace,
                                  hipStream_t stream) {
-  const ProductArgs a{X,   ldx, static_cast<const uint8_t*>(image), Y,    ldy, N, O, I,
-                      layout_of(O, I, G), y_dt, act, stream};
+  ProductArgs a{X,   ldx, nullptr, static_cast<const uint8_t*>(image), Y,  ldy, N, O,
+                I,   layout_of(O, I, G), y_dt, act, stream};
+  if (!x_in_lds(N, a.L.itiles, x_dt)) {
+    bf16x8* xop = static_cast<bf16x8*>(workspace);
+    const int ntiles = (int)cdiv(N, 16);
+    const int64_t total = a.L.itiles * ntiles * 256;
+    const dim3 grid((unsigned)cdiv(total, 256)), block(256);
+    if (x_dt == 0)
+      hipLaunchKernelGGL(nibble_x_kernel<float>, grid, block, 0, stream,
+                         static_cast<const float*>(X), ldx, N, I, ntiles, total, xop);
+    else
+      hipLaunchKernelGGL(nibble_x_kernel<bf16raw>, grid, block, 0, stream,
+                         static_cast<const bf16raw*>(X), ldx, N, I, ntiles, total, xop);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.xop = xop;
+  }
   return x_dt == 0 ? launch_product_typed<float>(a, G, with_zeros)
                    : launch_product_typed<bf16raw>(a, G, with_zeros);
 }

@@ -10,6 +10,7 @@ namespace hd {
 namespace ops {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // the same vectors where rows start at any element
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
@@ -38,8 +39,9 @@ hipError_t launch_nibble_unpack(const void* image, float* W, int64_t O, int64_t 
                                 bool with_zeros, hipStream_t stream);
 hipError_t launch_nibble_product(const void* X, int64_t ldx, const void* image, void* Y,
                                  int64_t ldy, int64_t N, int64_t O, int64_t I, int G,
-                                 bool with_zeros, int x_dt, int y_dt, int act,
+                                 bool with_zeros, int x_dt, int y_dt, int act, void* workspace,
                                  hipStream_t stream);
+size_t nibble_ws_bytes(int64_t N, int64_t I, int x_dt);  // of launch_nibble_product
 
 // ---- log probabilities (hd_logprobs.hip) ------------------------------------
 constexpr int kMaxTop = 32;  // alternatives of a row

@@ -15,6 +15,8 @@ size_t esize(int dt) { return dt == HD_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 hd_status from_hip(hipError_t e) { return e == hipSuccess ? HD_OK : HD_ERR_HIP; }
 
+constexpr int64_t kMaxRows = 4096;  // of X in one 4-bit product
+
 // The sizes of a 4-bit matrix: HD_OK, or what is wrong with them.
 hd_status nibble_sizes(int64_t outer, int64_t inner, int64_t group) {
   if (outer < 1 || inner < 1 || (group != 32 && group != 64 && group != 128)) return HD_ERR_ARG;
@@ -95,23 +97,32 @@ hd_status hd_nibble_unpack(const void* image, int zeros, float* W, int64_t outer
       hd::ops::launch_nibble_unpack(image, W, outer, inner, (int)group, zeros != 0, stream));
 }
 
+size_t hd_nibble_workspace_bytes(int64_t N, int64_t inner, hd_dtype x_dt) {
+  if (N < 1 || N > kMaxRows || inner < 1 || inner > kMaxDim || !float_dt(x_dt)) return 0;
+  return hd::ops::nibble_ws_bytes(N, inner, x_dt);
+}
+
 hd_status hd_nibble_product(const void* X, int64_t ldx, const void* image, int zeros, void* Y,
                             int64_t ldy, int64_t N, int64_t outer, int64_t inner, int64_t group,
-                            hd_dtype x_dt, hd_dtype y_dt, hd_act act, hipStream_t stream) {
+                            hd_dtype x_dt, hd_dtype y_dt, hd_act act, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream) {
   const hd_status st = nibble_sizes(outer, inner, group);
   if (N < 0 || !known_dt(x_dt) || !known_dt(y_dt) ||
       (act != HD_ACT_HARDSIGN && act != HD_ACT_IDENTITY))
     return HD_ERR_ARG;
   if (st != HD_OK) return st;
-  if (N > (int64_t(1) << 20) || !float_dt(x_dt) || !float_dt(y_dt)) return HD_ERR_UNSUPPORTED;
+  if (N > kMaxRows || !float_dt(x_dt) || !float_dt(y_dt)) return HD_ERR_UNSUPPORTED;
   if (ldx < inner || ldy < outer) return HD_ERR_ARG;
   if (N == 0) return HD_OK;
   if (!X || !image || !Y || !aligned(X, esize(x_dt)) || !aligned(Y, esize(y_dt)) ||
-      !aligned(image, 256))
+      !aligned(image, 256) || !aligned(workspace, 256))
     return HD_ERR_ARG;
+  const size_t need = hd::ops::nibble_ws_bytes(N, inner, x_dt);
+  if (need > 0 && !workspace) return HD_ERR_ARG;
+  if (workspace_bytes < need) return HD_ERR_WORKSPACE;
   return from_hip(hd::ops::launch_nibble_product(X, ldx, image, Y, ldy, N, outer, inner,
                                                  (int)group, zeros != 0, x_dt, y_dt, act,
-                                                 stream));
+                                                 workspace, stream));
 }
 
 size_t hd_logprobs_workspace_bytes(int64_t N, int64_t K, hd_dtype dt) {

@@ -81,6 +81,49 @@ def test_product_exact_on_integers(N, outer, inner, group, zeros, dtype):
     assert torch.equal(H, torch.where(ref >= 0, 1.0, -1.0).double())
 
 
+# every kernel there is: rows, type, group, zero points; several tiles to a wave and one
+# that ends inside
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [1, 20, 40])
+def test_every_kernel(N, dtype, group, zeros):
+    hd = hd_gpu()
+    for outer, inner in ((50, 4500), (35, 2560), (20, 1100)):
+        announce(f"nibble every {N}x{outer}x{inner} group {group} zeros {zeros} {dtype}")
+        codes, scales, z = P.random_nibble(outer, inner, group, zeros, seed=inner)
+        X = torch.randn(N, inner, generator=torch.Generator().manual_seed(N)).to(dtype)
+        w = hd.nibble_pack(codes.cuda(), scales.cuda(), cuda(z), inner=inner, group=group)
+        W, size = P.nibble_weights(codes, scales, z, inner, group)
+        ref = X.double() @ W.t()
+        Y = hd.nibble_product(X.cuda(), w, dtype=F32).cpu().double()
+        assert bool(((Y - ref).abs() <= P.nibble_bound(X, size, ref, F32)).all())
+
+
+# 4-bit weights past the caches take loads of their own
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_weights(dtype, group, zeros):
+    hd = hd_gpu()
+    outer, inner, rows = 30011, 16384, 64
+    announce(f"nibble large group {group} zeros {zeros} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    codes = torch.randint(0, 256, (outer, inner // 2), dtype=torch.uint8, generator=g,
+                          device="cuda")
+    scales = (torch.rand(outer, inner // group, generator=g, device="cuda") + 0.25).to(BF16)
+    z = torch.randint(0, 16, (outer, inner // group), dtype=torch.uint8, generator=g,
+                      device="cuda") if zeros else None
+    X = torch.randn(2, inner, generator=torch.Generator().manual_seed(2)).to(dtype)
+    Y = hd.nibble_product(X.cuda(), hd.nibble_pack(codes, scales, z, group=group),
+                          dtype=F32).cpu().double()
+    pick = torch.linspace(0, outer - 1, rows).long()
+    W, size = P.nibble_weights(codes[pick.cuda()].cpu(), scales[pick.cuda()].cpu(),
+                               None if z is None else z[pick.cuda()].cpu(), inner, group)
+    ref = X.double() @ W.t()
+    assert bool(((Y[:, pick] - ref).abs() <= P.nibble_bound(X, size, ref, F32)).all())
+
+
 def test_fp32_x_in_full():
     """Weight 1 (code 1, zero point 0) on one input: the three parts of an fp32 X add
     up to every bit of it."""
