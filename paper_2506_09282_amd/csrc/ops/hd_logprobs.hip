@@ -30,6 +30,8 @@ namespace {
 
 constexpr int kShortK = 1024;
 constexpr int kLongThreads = 256;
+// Scores past the caches: loads and stores that do not stay there.
+constexpr int64_t kStreamBytes = int64_t(192) << 20;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kUnder = -300.0f;  // 2^kUnder is 0: keeps 0 * -inf out of the sums
@@ -45,11 +47,6 @@ __device__ __forceinline__ uint64_t key_of(float s, uint32_t k) {
 __device__ __forceinline__ float key_score(uint64_t key) {
   const uint32_t b = (uint32_t)(key >> 32);
   return __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
-}
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int off) {
-  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, off, kWave);
-  const uint32_t hi = (uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), off, kWave);
-  return (uint64_t)hi << 32 | lo;
 }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
@@ -77,18 +74,29 @@ __device__ __forceinline__ void stats_add(Stats& a, float s, float c) {
   a.sum += e;
   a.ez = fmaf(e, fmaxf(z, kUnder), a.ez);  // (NaN is in e)
 }
-template <int LANES>
+// Over LANES neighbouring lanes; both lanes of a pair add the same two numbers.
+template <int LANES, int OFF = 1>
 __device__ __forceinline__ Stats stats_across(Stats a, float c) {
-#pragma unroll
-  for (int off = 1; off < LANES; off <<= 1) {
-    Stats b;
-    b.m = __shfl_xor(a.m, off, kWave);
-    b.sum = __shfl_xor(a.sum, off, kWave);
-    b.ez = __shfl_xor(a.ez, off, kWave);
-    // the same order in both lanes: the sums are commutative, so the bits agree
-    a = stats_join(a, b, c);
+  if constexpr (OFF < LANES) {
+    const Stats b{lane_xor<OFF>(a.m), lane_xor<OFF>(a.sum), lane_xor<OFF>(a.ez)};
+    return stats_across<LANES, 2 * OFF>(stats_join(a, b, c), c);
   }
   return a;
+}
+template <int LANES, int OFF = 1>
+__device__ __forceinline__ float max_across(float v) {
+  if constexpr (OFF < LANES) return max_across<LANES, 2 * OFF>(fmaxf(v, lane_xor<OFF>(v)));
+  return v;
+}
+template <int LANES, int OFF = 1>
+__device__ __forceinline__ float sum_across(float v) {
+  if constexpr (OFF < LANES) return sum_across<LANES, 2 * OFF>(v + lane_xor<OFF>(v));
+  return v;
+}
+template <int LANES, int OFF = 1>
+__device__ __forceinline__ uint64_t max_across(uint64_t v) {
+  if constexpr (OFF < LANES) return max_across<LANES, 2 * OFF>(max64(v, lane_xor<OFF>(v)));
+  return v;
 }
 
 struct Row {  // a finished row
@@ -164,16 +172,12 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out
     if (mrow && k < K && !mrow[k]) v[j] = -INFINITY;
     st.m = fmaxf(st.m, v[j]);
   }
-#pragma unroll
-  for (int off = 1; off < LPR; off <<= 1) st.m = fmaxf(st.m, __shfl_xor(st.m, off, kWave));
+  st.m = max_across<LPR>(st.m);
   const float c = a.scale * kLog2e;
 #pragma unroll
   for (int j = 0; j < VPL; ++j) stats_add(st, v[j], c);
-#pragma unroll
-  for (int off = 1; off < LPR; off <<= 1) {
-    st.sum += __shfl_xor(st.sum, off, kWave);
-    st.ez += __shfl_xor(st.ez, off, kWave);
-  }
+  st.sum = sum_across<LPR>(st.sum);
+  st.ez = sum_across<LPR>(st.ez);
   const Row r = finish(st);
   if (live && lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
   if (o.top == 0) return;
@@ -185,8 +189,7 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out
     uint64_t best = 0;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) best = max64(best, key[j]);
-#pragma unroll
-    for (int off = 1; off < LPR; off <<= 1) best = max64(best, shfl_xor64(best, off));
+    best = max_across<LPR>(best);
 #pragma unroll
     for (int j = 0; j < VPL; ++j) key[j] = key[j] == best ? 0 : key[j];
     if (live && lane == 0) write_top(r, best, n, t, a.scale, o);
@@ -195,27 +198,30 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out
 
 // ---- long rows -----------------------------------------------------------------
 
+// Compare and exchange with lane ^ OFF within blocks of SIZE lanes, of which every other
+// is sorted the other way round.
+template <int SIZE, int OFF>
+__device__ __forceinline__ uint64_t exchange(uint64_t v, int lane) {
+  const uint64_t w = lane_xor<OFF>(v);
+  const bool keep_max = ((lane & OFF) == 0) == (SIZE == 64 || (lane & SIZE) == 0);
+  return keep_max ? max64(v, w) : min64(v, w);
+}
+template <int SIZE, int OFF>
+__device__ __forceinline__ uint64_t merge(uint64_t v, int lane) {
+  v = exchange<SIZE, OFF>(v, lane);
+  if constexpr (OFF > 1) return merge<SIZE, OFF / 2>(v, lane);
+  return v;
+}
 // Sorts one key per lane, largest first.
+template <int SIZE = 2>
 __device__ __forceinline__ uint64_t sort64(uint64_t v, int lane) {
-  for (int size = 2; size <= 64; size <<= 1)
-    for (int off = size >> 1; off > 0; off >>= 1) {
-      const uint64_t w = shfl_xor64(v, off);
-      // descending blocks where the lane's `size` bit is clear (64: all of it)
-      const bool keep_max = ((lane & off) == 0) == ((lane & size) == 0 || size == 64);
-      v = keep_max ? max64(v, w) : min64(v, w);
-    }
+  v = merge<SIZE, SIZE / 2>(v, lane);
+  if constexpr (SIZE < 64) return sort64<2 * SIZE>(v, lane);
   return v;
 }
 // Lanes 0..31 hold a list, largest first, and lanes 32..63 another, smallest
 // first: the 64 keys, largest first.
-__device__ __forceinline__ uint64_t merge64(uint64_t v, int lane) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const uint64_t w = shfl_xor64(v, off);
-    v = (lane & off) == 0 ? max64(v, w) : min64(v, w);
-  }
-  return v;
-}
+__device__ __forceinline__ uint64_t merge64(uint64_t v, int lane) { return merge<64, 32>(v, lane); }
 
 // A wave's sorted list: lane j holds the (j+1)-th best key seen.
 struct TopList {
@@ -245,30 +251,36 @@ struct Chunk {  // 16 bytes of scores
   static constexpr int kLen = 16 / (int)sizeof(T);
 };
 
-__device__ __forceinline__ void load_chunk(const float* p, float (&v)[4]) {
-  const f32x4 x = *reinterpret_cast<const f32x4_a4*>(p);
+// A chunk on its way: its words, and the mask's.
+template <typename T, bool MASK, bool STREAM>
+struct Flight {
+  static constexpr int LEN = Chunk<T>::kLen;
+  u32x4 w;
+  uint32_t m[MASK ? LEN / 4 : 1];
+  __device__ __forceinline__ void load(const T* p, const uint8_t* mp) {
+    typedef uint32_t m_a __attribute__((aligned(1)));
+    if constexpr (STREAM)
+      w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(p));
+    else
+      w = *reinterpret_cast<const u32x4_a2*>(p);
+    if (MASK) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = x[e];
-}
-__device__ __forceinline__ void load_chunk(const bf16raw* p, float (&v)[8]) {
-  const u32x4 x = *reinterpret_cast<const u32x4_a2*>(p);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[2 * e] = __uint_as_float(x[e] << 16);
-    v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+      for (int i = 0; i < LEN / 4; ++i)
+        m[i] = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const m_a*>(mp) + i)
+                      : reinterpret_cast<const m_a*>(mp)[i];
+    }
   }
-}
-typedef uint32_t u32_a1 __attribute__((aligned(1)));
-template <int LEN>
-__device__ __forceinline__ void mask_chunk(const uint8_t* p, float (&v)[LEN]) {
+  __device__ __forceinline__ void scores(float (&v)[LEN]) const {
 #pragma unroll
-  for (int w = 0; w < LEN / 4; ++w) {
-    const uint32_t b = reinterpret_cast<const u32_a1*>(p)[w];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (!(b & (255u << (8 * e)))) v[4 * w + e] = -INFINITY;
+    for (int e = 0; e < LEN; ++e) {
+      if constexpr (sizeof(T) == 4)
+        v[e] = __uint_as_float(w[e]);
+      else
+        v[e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+      if (MASK && !(m[e / 4] & (255u << (8 * (e % 4))))) v[e] = -INFINITY;
+    }
   }
-}
+};
 
 // Joins the waves' statistics and lists of a workgroup; the result is whole in wave 0.
 template <bool TOP>
@@ -307,7 +319,16 @@ __device__ __forceinline__ void put_word(uint32_t* p, uint32_t v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <typename T, bool TOP, bool MASK>
+__device__ __forceinline__ uint64_t get_key(const uint32_t* p) {
+  return __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put_key(uint32_t* p, uint64_t v) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <typename T, bool TOP, bool MASK, bool STREAM>
 __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArgs a, Out o,
                                                                      Split sp) {
   constexpr int LEN = Chunk<T>::kLen, WAVES = kLongThreads / 64;
@@ -326,19 +347,7 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
   TopList list{0, -INFINITY};
   bool first = true;
   constexpr int STEP = kLongThreads * LEN;
-  for (int64_t k0 = part * sp.part_len; k0 < k_end; k0 += STEP) {
-    const int64_t k = k0 + (int64_t)threadIdx.x * LEN;
-    float v[LEN];
-    if (k + LEN <= k_end) {
-      load_chunk(row + k, v);
-      if (MASK) mask_chunk<LEN>(mrow + k, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < LEN; ++e) {
-        v[e] = k + e < k_end ? load_elem(row, k + e) : -INFINITY;
-        if (MASK && k + e < k_end && !mrow[k + e]) v[e] = -INFINITY;
-      }
-    }
+  auto add = [&](const float(&v)[LEN], int64_t k0) {
     float m = v[0];
 #pragma unroll
     for (int e = 1; e < LEN; ++e) m = fmaxf(m, v[e]);
@@ -355,7 +364,7 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       }
 #pragma unroll
       for (int e = 0; e < LEN; ++e) {
-        bool in = first ? v[e] >= bar && v[e] > -INFINITY : v[e] > list.bar;
+        const bool in = first ? v[e] >= bar && v[e] > -INFINITY : v[e] > bar;
         uint64_t pass = __ballot(in);
         while (pass) {
           const int from = (int)__builtin_ctzll(pass);
@@ -369,13 +378,45 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       first = false;
       list.bar = list_bar(list.key, o.top);
     }
+  };
+  // Whole steps, the next one's loads in flight (past the end the last one's again), then
+  // the step that ends inside.
+  const int64_t k_begin = part * sp.part_len, whole = (k_end - k_begin) / STEP;
+  if (whole > 0) {
+    Flight<T, MASK, STREAM> now, next;
+    auto fetch = [&](Flight<T, MASK, STREAM>& f, int64_t i) {
+      const int64_t k = k_begin + (i < whole ? i : whole - 1) * STEP + (int64_t)threadIdx.x * LEN;
+      f.load(row + k, MASK ? mrow + k : nullptr);
+    };
+    float v[LEN];
+    fetch(now, 0);
+    int64_t i = 0;
+    for (; i + 2 <= whole; i += 2) {
+      fetch(next, i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      now.scores(v);
+      add(v, k_begin + i * STEP);
+      fetch(now, i + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      next.scores(v);
+      add(v, k_begin + (i + 1) * STEP);
+    }
+    if (i < whole) {
+      now.scores(v);
+      add(v, k_begin + i * STEP);
+    }
   }
+  if (k_begin + whole * STEP < k_end) {
+    const int64_t k0 = k_begin + whole * STEP, k = k0 + (int64_t)threadIdx.x * LEN;
+    float v[LEN];
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {  // the wave's statistics
-    Stats b{__shfl_xor(st.m, off, kWave), __shfl_xor(st.sum, off, kWave),
-            __shfl_xor(st.ez, off, kWave)};
-    st = stats_join(st, b, c);
+    for (int e = 0; e < LEN; ++e) {
+      v[e] = k + e < k_end ? load_elem(row, k + e) : -INFINITY;
+      if (MASK && k + e < k_end && !mrow[k + e]) v[e] = -INFINITY;
+    }
+    add(v, k0);
   }
+  st = stats_across<64>(st, c);
   join_waves<TOP>(st, list.key, c, lane, wave, WAVES, sh_st, sh_key);
 
   if (sp.parts > 1) {
@@ -386,48 +427,48 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
         put_word(mine + 1, __float_as_uint(st.sum));
         put_word(mine + 2, __float_as_uint(st.ez));
       }
-      if (TOP && lane < o.top) {
-        put_word(mine + 4 + 2 * lane, (uint32_t)list.key);
-        put_word(mine + 5 + 2 * lane, (uint32_t)(list.key >> 32));
-      }
+      if (TOP && lane < o.top) put_key(mine + 4 + 2 * lane, list.key);
       wait_own_memory_ops();
       if (lane == 0) sh_last = take_ticket(sp.tickets + n) == (uint32_t)sp.parts - 1;
     }
     __syncthreads();
     if (!sh_last) return;
-    // the last one: wave w takes parts w, w + WAVES, ...
     if (threadIdx.x == 0) reset_counter(sp.tickets + n);
-    st = stats_none();
-    list.key = 0;
     uint32_t* words = sp.words + (int64_t)n * sp.parts * kPartWords;
-    constexpr int EACH = kMaxParts / WAVES;
-    uint32_t head[EACH];
-    uint64_t keys[EACH];
-    const int at = 63 - lane;  // the list in lanes 63, 62, ...
+    if (wave == 0) {
+      // lane p holds part p
+      uint32_t* w = words + (int64_t)lane * kPartWords;
+      uint64_t keys[kMaxTop] = {};
+      st = stats_none();
+      if (lane < sp.parts) {
+        st.m = __uint_as_float(get_word(w));
+        st.sum = __uint_as_float(get_word(w + 1));
+        st.ez = __uint_as_float(get_word(w + 2));
+        if (TOP) {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int p = wave + WAVES * i;
-      uint32_t* w = words + (int64_t)p * kPartWords;
-      head[i] = 0, keys[i] = 0;
-      if (p >= sp.parts) continue;
-      if (lane < 3) head[i] = get_word(w + lane);
-      if (TOP && at < o.top)
-        keys[i] = (uint64_t)get_word(w + 5 + 2 * at) << 32 | get_word(w + 4 + 2 * at);
-    }
+          for (int t = 0; t < kMaxTop; ++t)
+            if (t < o.top) keys[t] = get_key(w + 4 + 2 * t);
+        }
+      }
+      st = stats_across<64>(st, c);
+      if (TOP) {
+        // the T-th largest of the parts' best bounds the T-th of all from below
+        const uint64_t bar = lane_key(sort64(keys[0], lane), o.top - 1);
+        list.key = 0;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int p = wave + WAVES * i;
-      if (p >= sp.parts) break;
-      const Stats b{__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)head[i], 0)),
-                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)head[i], 1)),
-                    __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)head[i], 2))};
-      st = stats_join(st, b, c);
-      if (TOP) list.key = merge64(lane < kMaxTop ? list.key : keys[i], lane);
+        for (int t = 0; t < kMaxTop; ++t) {
+          uint64_t pass = __ballot(keys[t] != 0 && keys[t] >= bar);
+          while (pass) {
+            const int from = (int)__builtin_ctzll(pass);
+            pass &= pass - 1;
+            list.key = list_insert(list.key, lane_key(keys[t], from), lane);
+          }
+        }
+      }
     }
-    // left zeroed
+    __syncthreads();  // all is read: left zeroed
     for (int64_t i = threadIdx.x; i < (int64_t)sp.parts * kPartWords; i += kLongThreads)
       words[i] = 0;
-    join_waves<TOP>(st, list.key, c, lane, wave, WAVES, sh_st, sh_key);
   }
   if (wave != 0) return;
   const Row r = finish(st);
@@ -466,14 +507,21 @@ hipError_t launch_typed(const LogprobsArgs& a, const Out& o, Split s, hipStream_
   if (a.K <= 64 * 4) return launch_short<T, 64, 4>(a, o, stream);
   if (a.K <= kShortK) return launch_short<T, 64, 16>(a, o, stream);
   const dim3 grid((unsigned)(a.N * s.parts)), block(kLongThreads);
-  if (o.top && a.mask)
-    hipLaunchKernelGGL((logprobs_long_kernel<T, true, true>), grid, block, 0, stream, a, o, s);
-  else if (o.top)
-    hipLaunchKernelGGL((logprobs_long_kernel<T, true, false>), grid, block, 0, stream, a, o, s);
-  else if (a.mask)
-    hipLaunchKernelGGL((logprobs_long_kernel<T, false, true>), grid, block, 0, stream, a, o, s);
-  else
-    hipLaunchKernelGGL((logprobs_long_kernel<T, false, false>), grid, block, 0, stream, a, o, s);
+  const bool stream_by = a.N * a.K * (int64_t)sizeof(T) > kStreamBytes;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, o, s);
+  };
+  if (stream_by) {
+    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, true>);
+    else if (o.top) go(logprobs_long_kernel<T, true, false, true>);
+    else if (a.mask) go(logprobs_long_kernel<T, false, true, true>);
+    else go(logprobs_long_kernel<T, false, false, true>);
+  } else {
+    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, false>);
+    else if (o.top) go(logprobs_long_kernel<T, true, false, false>);
+    else if (a.mask) go(logprobs_long_kernel<T, false, true, false>);
+    else go(logprobs_long_kernel<T, false, false, false>);
+  }
   return hipGetLastError();
 }
 
@@ -507,7 +555,7 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float s, int32_t k, f
 
 // A thread takes LEN classes of one row. ROWS: a workgroup works within a row (blockIdx.y),
 // else a thread finds its row.
-template <typename T, bool MASK, bool ROWS>
+template <typename T, bool MASK, bool ROWS, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_grad_kernel(
     LogprobsArgs a, const float* __restrict__ stats, const float* __restrict__ entropy,
     const float* __restrict__ g_logp, const float* __restrict__ g_entropy, T* out, int64_t ldd,
@@ -530,23 +578,24 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(
   const uint8_t* mrow = MASK ? a.mask + n * a.ldm + k : nullptr;
   T* dst = out + n * ldd + k;
   if (k + LEN <= a.K) {
+    Flight<T, MASK, STREAM> f;
+    f.load(row, mrow);
     float v[LEN];
-    load_chunk(row, v);
-    if (MASK) mask_chunk<LEN>(mrow, v);
-    if constexpr (sizeof(T) == 4) {
-      f32x4 d;
+    f.scores(v);
+    u32x4 d;
 #pragma unroll
-      for (int e = 0; e < LEN; ++e) d[e] = grad_of(r, v[e], (int32_t)(k + e), a.scale);
-      *reinterpret_cast<f32x4_a4*>(dst) = d;
-    } else {
-      u32x4 d;
+    for (int e = 0; e < LEN; ++e) v[e] = grad_of(r, v[e], (int32_t)(k + e), a.scale);
 #pragma unroll
-      for (int e = 0; e < LEN / 2; ++e)
-        d[e] = (uint32_t)to_bf16(grad_of(r, v[2 * e], (int32_t)(k + 2 * e), a.scale)) |
-               (uint32_t)to_bf16(grad_of(r, v[2 * e + 1], (int32_t)(k + 2 * e + 1), a.scale))
-                   << 16;
-      *reinterpret_cast<u32x4_a2*>(dst) = d;
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 4)
+        d[e] = __float_as_uint(v[e]);
+      else
+        d[e] = (uint32_t)to_bf16(v[2 * e]) | (uint32_t)to_bf16(v[2 * e + 1]) << 16;
     }
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(d, reinterpret_cast<u32x4_a2*>(dst));
+    else
+      *reinterpret_cast<u32x4_a2*>(dst) = d;
   } else {
     for (int e = 0; k + e < a.K; ++e) {
       const float s = !MASK || mrow[e] ? load_elem(row, e) : -INFINITY;
@@ -565,18 +614,21 @@ hipError_t launch_grad(const LogprobsArgs& a, const float* stats, const float* e
   const bool rows = chunks >= 256;
   const int64_t blocks = rows ? a.N * cdiv(chunks, 256) : cdiv(a.N * chunks, 256);
   const dim3 grid((unsigned)blocks), block(256);
-  if (rows && a.mask)
-    hipLaunchKernelGGL((logprobs_grad_kernel<T, true, true>), grid, block, 0, stream, a, stats,
-                       entropy, g_logp, g_entropy, d, ldd, chunks);
-  else if (rows)
-    hipLaunchKernelGGL((logprobs_grad_kernel<T, false, true>), grid, block, 0, stream, a, stats,
-                       entropy, g_logp, g_entropy, d, ldd, chunks);
-  else if (a.mask)
-    hipLaunchKernelGGL((logprobs_grad_kernel<T, true, false>), grid, block, 0, stream, a, stats,
-                       entropy, g_logp, g_entropy, d, ldd, chunks);
-  else
-    hipLaunchKernelGGL((logprobs_grad_kernel<T, false, false>), grid, block, 0, stream, a, stats,
-                       entropy, g_logp, g_entropy, d, ldd, chunks);
+  const bool stream_by = a.N * a.K * (int64_t)sizeof(T) > kStreamBytes;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, stats, entropy, g_logp, g_entropy, d,
+                       ldd, chunks);
+  };
+  if (rows && stream_by) {
+    if (a.mask) go(logprobs_grad_kernel<T, true, true, true>);
+    else go(logprobs_grad_kernel<T, false, true, true>);
+  } else if (rows) {
+    if (a.mask) go(logprobs_grad_kernel<T, true, true, false>);
+    else go(logprobs_grad_kernel<T, false, true, false>);
+  } else {
+    if (a.mask) go(logprobs_grad_kernel<T, true, false, false>);
+    else go(logprobs_grad_kernel<T, false, false, false>);
+  }
   return hipGetLastError();
 }
 

@@ -24,6 +24,36 @@ __device__ __forceinline__ bf16raw to_bf16(float v) {
 __device__ __forceinline__ void store_elem(float* p, int64_t i, float v) { p[i] = v; }
 __device__ __forceinline__ void store_elem(bf16raw* p, int64_t i, float v) { p[i] = to_bf16(v); }
 
+// The value of lane ^ OFF, in the vector ALU alone (a shuffle through LDS takes several
+// times as long, and the sorts and sums across lanes are chains of these).
+template <int OFF>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  static_assert(OFF == 1 || OFF == 2 || OFF == 4 || OFF == 8 || OFF == 16 || OFF == 32, "");
+  if constexpr (OFF == 1) return __builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true);
+  if constexpr (OFF == 2) return __builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true);
+  if constexpr (OFF == 4) {  // lane ^ 7 (half a row mirrored), then ^ 3
+    const int m = __builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true);
+    return __builtin_amdgcn_mov_dpp(m, 0x1b, 0xf, 0xf, true);
+  }
+  if constexpr (OFF == 8) return __builtin_amdgcn_mov_dpp((int)v, 0x128, 0xf, 0xf, true);
+  if constexpr (OFF == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return (threadIdx.x & 16) ? r[0] : r[1];
+  }
+  if constexpr (OFF == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (threadIdx.x & 32) ? r[0] : r[1];
+  }
+}
+template <int OFF>
+__device__ __forceinline__ float lane_xor(float v) {
+  return __uint_as_float(lane_xor<OFF>(__float_as_uint(v)));
+}
+template <int OFF>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
+  return (uint64_t)lane_xor<OFF>((uint32_t)(v >> 32)) << 32 | lane_xor<OFF>((uint32_t)v);
+}
+
 // ---- products with 4-bit weights (hd_nibble.hip) ---------------------------
 struct NibbleLayout {
   int64_t otiles, itiles;           // tiles of 16 outputs, of 128 inputs
