@@ -44,9 +44,16 @@ __device__ __forceinline__ uint64_t key_of(float s, uint32_t k) {
   b ^= (b >> 31) ? 0xffffffffu : 0x80000000u;
   return (uint64_t)b << 32 | (uint32_t)~k;
 }
-__device__ __forceinline__ float key_score(uint64_t key) {
-  const uint32_t b = (uint32_t)(key >> 32);
+__device__ __forceinline__ float order_score(uint32_t b) {
   return __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
+}
+// The largest score below the one whose order is b (for comparisons, in which both zeros
+// are one).
+__device__ __forceinline__ float score_below(uint32_t b) {
+  return order_score(b == 0x80000000u ? b - 2 : b - 1);
+}
+__device__ __forceinline__ float key_score(uint64_t key) {
+  return order_score((uint32_t)(key >> 32));
 }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
@@ -94,8 +101,11 @@ __device__ __forceinline__ float sum_across(float v) {
   return v;
 }
 template <int LANES, int OFF = 1>
-__device__ __forceinline__ uint64_t max_across(uint64_t v) {
-  if constexpr (OFF < LANES) return max_across<LANES, 2 * OFF>(max64(v, lane_xor<OFF>(v)));
+__device__ __forceinline__ uint32_t min_across(uint32_t v) {
+  if constexpr (OFF < LANES) {
+    const uint32_t w = lane_xor<OFF>(v);
+    return min_across<LANES, 2 * OFF>(v < w ? v : w);
+  }
   return v;
 }
 
@@ -151,52 +161,7 @@ __device__ __forceinline__ void write_top(const Row& r, uint64_t key, int64_t n,
       r.bad ? NAN : there ? logp_of(r, key_score(key), scale) : -INFINITY;
 }
 
-// ---- short rows ----------------------------------------------------------------
-
-// LPR lanes to a row, VPL scores in each lane (class lane + LPR j).
-template <typename T, int LPR, int VPL>
-__global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out o) {
-  const int lane = threadIdx.x & (LPR - 1);
-  const int64_t n = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-  const bool live = n < a.N;
-  const int64_t nn = live ? n : a.N - 1;  // lanes past the end follow along and write nothing
-  const T* row = static_cast<const T*>(a.scores) + nn * a.ld;
-  const uint8_t* mrow = a.mask ? a.mask + nn * a.ldm : nullptr;
-  const int K = (int)a.K;
-  float v[VPL];
-  Stats st = stats_none();
-#pragma unroll
-  for (int j = 0; j < VPL; ++j) {
-    const int k = lane + LPR * j;
-    v[j] = k < K ? load_elem(row, k) : -INFINITY;
-    if (mrow && k < K && !mrow[k]) v[j] = -INFINITY;
-    st.m = fmaxf(st.m, v[j]);
-  }
-  st.m = max_across<LPR>(st.m);
-  const float c = a.scale * kLog2e;
-#pragma unroll
-  for (int j = 0; j < VPL; ++j) stats_add(st, v[j], c);
-  st.sum = sum_across<LPR>(st.sum);
-  st.ez = sum_across<LPR>(st.ez);
-  const Row r = finish(st);
-  if (live && lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
-  if (o.top == 0) return;
-  uint64_t key[VPL];
-#pragma unroll
-  for (int j = 0; j < VPL; ++j)
-    key[j] = v[j] > -INFINITY ? key_of(v[j], (uint32_t)(lane + LPR * j)) : 0;
-  for (int t = 0; t < o.top; ++t) {
-    uint64_t best = 0;
-#pragma unroll
-    for (int j = 0; j < VPL; ++j) best = max64(best, key[j]);
-    best = max_across<LPR>(best);
-#pragma unroll
-    for (int j = 0; j < VPL; ++j) key[j] = key[j] == best ? 0 : key[j];
-    if (live && lane == 0) write_top(r, best, n, t, a.scale, o);
-  }
-}
-
-// ---- long rows -----------------------------------------------------------------
+// ---- lists of the best keys --------------------------------------------------------
 
 // Compare and exchange with lane ^ OFF within blocks of SIZE lanes, of which every other
 // is sorted the other way round.
@@ -233,10 +198,6 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
   return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ float list_bar(uint64_t key, int top) {
-  const uint64_t k = lane_key(key, top - 1);
-  return k ? key_score(k) : -INFINITY;
-}
 // Inserts a key that is the same in all lanes.
 __device__ __forceinline__ uint64_t list_insert(uint64_t list, uint64_t key, int lane) {
   const int at = __popcll(__ballot(list > key));
@@ -245,6 +206,75 @@ __device__ __forceinline__ uint64_t list_insert(uint64_t list, uint64_t key, int
   const uint64_t up = (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;  // the lane below
   return lane < at ? list : lane == at ? key : up;
 }
+
+// ---- short rows ----------------------------------------------------------------
+
+// LPR lanes to a row, VPL scores in each lane (class lane + LPR j).
+template <typename T, int LPR, int VPL>
+__global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out o) {
+  const int lane = threadIdx.x & (LPR - 1);
+  const int64_t n = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const bool live = n < a.N;
+  const int64_t nn = live ? n : a.N - 1;  // lanes past the end follow along and write nothing
+  const T* row = static_cast<const T*>(a.scores) + nn * a.ld;
+  const uint8_t* mrow = a.mask ? a.mask + nn * a.ldm : nullptr;
+  const int K = (int)a.K;
+  float v[VPL];
+  Stats st = stats_none();
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) {
+    const int k = lane + LPR * j;
+    v[j] = k < K ? load_elem(row, k) : -INFINITY;
+    if (mrow && k < K && !mrow[k]) v[j] = -INFINITY;
+    st.m = fmaxf(st.m, v[j]);
+  }
+  st.m = max_across<LPR>(st.m);
+  const float c = a.scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < VPL; ++j) stats_add(st, v[j], c);
+  st.sum = sum_across<LPR>(st.sum);
+  st.ez = sum_across<LPR>(st.ez);
+  const Row r = finish(st);
+  if (live && lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
+  if (o.top == 0) return;
+  if constexpr (LPR == 64) {
+    // As in a long row: the T-th largest of the lanes' maxima is a bar, and what is not below
+    // it enters a list.
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) m = fmaxf(m, v[j]);
+    const uint64_t bar = lane_key(sort64(m > -INFINITY ? key_of(m, 0) : 0, lane), o.top - 1);
+    const float low = bar ? score_below((uint32_t)(bar >> 32)) : -INFINITY;
+    uint64_t list = 0;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j)
+      for (uint64_t pass = __ballot(v[j] > low); pass; pass &= pass - 1) {
+        const int from = (int)__builtin_ctzll(pass);
+        const float s =
+            __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[j]), from));
+        list = list_insert(list, key_of(s, (uint32_t)(from + LPR * j)), lane);
+      }
+    if (live && lane < o.top) write_top(r, list, n, lane, a.scale, o);
+  } else {
+    // The best score, then the lowest class that has it, T times.
+    for (int t = 0; t < o.top; ++t) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < VPL; ++j) m = fmaxf(m, v[j]);
+      m = max_across<LPR>(m);
+      uint32_t k = ~0u;
+#pragma unroll
+      for (int j = VPL - 1; j >= 0; --j) k = v[j] == m ? (uint32_t)(lane + LPR * j) : k;
+      k = min_across<LPR>(k);
+#pragma unroll
+      for (int j = 0; j < VPL; ++j)
+        if (k == (uint32_t)(lane + LPR * j)) v[j] = -INFINITY;
+      if (live && lane == 0) write_top(r, m > -INFINITY ? key_of(m, k) : 0, n, t, a.scale, o);
+    }
+  }
+}
+
+// ---- long rows -----------------------------------------------------------------
 
 template <typename T>
 struct Chunk {  // 16 bytes of scores
@@ -271,13 +301,27 @@ struct Flight {
     }
   }
   __device__ __forceinline__ void scores(float (&v)[LEN]) const {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < LEN; ++e) {
-      if constexpr (sizeof(T) == 4)
+      for (int e = 0; e < LEN; ++e) {
         v[e] = __uint_as_float(w[e]);
-      else
-        v[e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-      if (MASK && !(m[e / 4] & (255u << (8 * (e % 4))))) v[e] = -INFINITY;
+        if (MASK && !(m[0] & (255u << (8 * e)))) v[e] = -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < LEN / 2; ++e) {
+        uint32_t u = w[e];
+        if (MASK) {
+          // bit 7 of each byte: not 0; spread over the halves of a word by v_perm's sign
+          // selectors (bytes 1 and 3 of either operand)
+          const uint32_t f = ((m[e / 2] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | m[e / 2];
+          const uint32_t on =
+              __builtin_amdgcn_perm(f, f << 8, e % 2 ? 0x0b0b0909u : 0x0a0a0808u);
+          u = (u & on) | (0xff80ff80u & ~on);  // bf16 -inf
+        }
+        v[2 * e] = __uint_as_float(u << 16);
+        v[2 * e + 1] = __uint_as_float(u & 0xffff0000u);
+      }
     }
   }
 };
@@ -334,7 +378,7 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
   constexpr int LEN = Chunk<T>::kLen, WAVES = kLongThreads / 64;
   __shared__ Stats sh_st[WAVES];
   __shared__ uint64_t sh_key[WAVES * kMaxTop];
-  __shared__ uint32_t sh_last;
+  __shared__ uint32_t sh_last, sh_bar;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n = blockIdx.x / sp.parts;
   const int part = (int)(blockIdx.x % sp.parts);
@@ -343,76 +387,81 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
   const float c = a.scale * kLog2e;
   const int64_t k_end = (part + 1) * sp.part_len < a.K ? (part + 1) * sp.part_len : a.K;
 
+  if (TOP) {
+    if (threadIdx.x == 0) sh_bar = 0;
+    __syncthreads();
+  }
   Stats st = stats_none();
   TopList list{0, -INFINITY};
   bool first = true;
   constexpr int STEP = kLongThreads * LEN;
-  auto add = [&](const float(&v)[LEN], int64_t k0) {
+  auto add = [&](float(&v)[LEN], int64_t k0) {
     float m = v[0];
 #pragma unroll
     for (int e = 1; e < LEN; ++e) m = fmaxf(m, v[e]);
     if (m > st.m) stats_raise(st, m, c);
 #pragma unroll
     for (int e = 0; e < LEN; ++e) stats_add(st, v[e], c);
-    if (TOP && __ballot(m > list.bar)) {
-      float bar = list.bar;
-      if (first) {
-        // The T-th largest of the lanes' maxima bounds the wave's T-th score from below:
-        // without it the whole first chunk would pass through the list.
-        const uint64_t s = sort64(m > -INFINITY ? key_of(m, 0) : 0, lane);
-        bar = list_bar(s, o.top);
-      }
+    if (!TOP || !__ballot(m > list.bar)) return;
+    // What is below any wave's T-th score cannot be among the T best of the row. (Looked
+    // up only here: in every step it would cost more than it saves.)
+    const uint32_t shared_bar = *(volatile uint32_t*)&sh_bar;
+    if (shared_bar) list.bar = fmaxf(list.bar, score_below(shared_bar));
+    float bar = list.bar;
+    if (!__ballot(m > bar)) return;
+    const uint32_t id0 = (uint32_t)(k0 + (int64_t)threadIdx.x * LEN);
+    if (first) {
+      // The lanes' largest, sorted, begin the list; its T-th is a bar for the rest (without
+      // it the whole first chunk would pass one by one).
+      int at = 0;
 #pragma unroll
-      for (int e = 0; e < LEN; ++e) {
-        const bool in = first ? v[e] >= bar && v[e] > -INFINITY : v[e] > bar;
-        uint64_t pass = __ballot(in);
-        while (pass) {
-          const int from = (int)__builtin_ctzll(pass);
-          pass &= pass - 1;
-          const float s = __uint_as_float(
-              (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[e]), from));
-          const uint32_t id = (uint32_t)(k0 + (int64_t)(wave * 64 + from) * LEN + e);
-          list.key = list_insert(list.key, key_of(s, id), lane);
-        }
-      }
+      for (int e = LEN - 1; e >= 0; --e) at = v[e] == m ? e : at;
+      list.key = sort64(m > -INFINITY ? key_of(m, id0 + at) : 0, lane);
+      const uint64_t s = lane_key(list.key, o.top - 1);
+      if (s) bar = fmaxf(bar, score_below((uint32_t)(s >> 32)));
+#pragma unroll
+      for (int e = 0; e < LEN; ++e) v[e] = e == at ? -INFINITY : v[e];
       first = false;
-      list.bar = list_bar(list.key, o.top);
+    }
+#pragma unroll
+    for (int e = 0; e < LEN; ++e)
+      for (uint64_t pass = __ballot(v[e] > bar); pass; pass &= pass - 1) {
+        const int from = (int)__builtin_ctzll(pass);
+        const float s =
+            __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[e]), from));
+        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)id0, from) + e;
+        list.key = list_insert(list.key, key_of(s, id), lane);
+      }
+    const uint64_t last = lane_key(list.key, o.top - 1);
+    if (last) {
+      list.bar = fmaxf(list.bar, key_score(last));
+      if (lane == 0) atomicMax(&sh_bar, (uint32_t)(last >> 32));
     }
   };
-  // Whole steps, the next one's loads in flight (past the end the last one's again), then
-  // the step that ends inside.
+  // Whole steps, the next one's loads in flight while one is worked on (past the end the
+  // last one's again, so that they need no condition), then the step that ends inside.
   const int64_t k_begin = part * sp.part_len, whole = (k_end - k_begin) / STEP;
-  if (whole > 0) {
-    Flight<T, MASK, STREAM> now, next;
-    auto fetch = [&](Flight<T, MASK, STREAM>& f, int64_t i) {
-      const int64_t k = k_begin + (i < whole ? i : whole - 1) * STEP + (int64_t)threadIdx.x * LEN;
-      f.load(row + k, MASK ? mrow + k : nullptr);
-    };
+  const int64_t steps = cdiv(k_end - k_begin, STEP);
+  Flight<T, MASK, STREAM> flight;
+  auto fetch = [&](int64_t i) {
+    const int64_t k = k_begin + (i < whole ? i : whole - 1) * STEP + (int64_t)threadIdx.x * LEN;
+    flight.load(row + k, MASK ? mrow + k : nullptr);
+  };
+  if (whole > 0) fetch(0);
+  for (int64_t i = 0; i < steps; ++i) {
+    const int64_t k0 = k_begin + i * STEP;
     float v[LEN];
-    fetch(now, 0);
-    int64_t i = 0;
-    for (; i + 2 <= whole; i += 2) {
-      fetch(next, i + 1);
-      __builtin_amdgcn_sched_barrier(0);
-      now.scores(v);
-      add(v, k_begin + i * STEP);
-      fetch(now, i + 2);
-      __builtin_amdgcn_sched_barrier(0);
-      next.scores(v);
-      add(v, k_begin + (i + 1) * STEP);
-    }
     if (i < whole) {
-      now.scores(v);
-      add(v, k_begin + i * STEP);
-    }
-  }
-  if (k_begin + whole * STEP < k_end) {
-    const int64_t k0 = k_begin + whole * STEP, k = k0 + (int64_t)threadIdx.x * LEN;
-    float v[LEN];
+      flight.scores(v);
+      fetch(i + 1);
+      __builtin_amdgcn_sched_barrier(0);  // (or the loads sink below the work)
+    } else {
+      const int64_t k = k0 + (int64_t)threadIdx.x * LEN;
 #pragma unroll
-    for (int e = 0; e < LEN; ++e) {
-      v[e] = k + e < k_end ? load_elem(row, k + e) : -INFINITY;
-      if (MASK && k + e < k_end && !mrow[k + e]) v[e] = -INFINITY;
+      for (int e = 0; e < LEN; ++e) {
+        v[e] = k + e < k_end ? load_elem(row, k + e) : -INFINITY;
+        if (MASK && k + e < k_end && !mrow[k + e]) v[e] = -INFINITY;
+      }
     }
     add(v, k0);
   }
@@ -504,7 +553,7 @@ template <typename T>
 hipError_t launch_typed(const LogprobsArgs& a, const Out& o, Split s, hipStream_t stream) {
   if (a.K <= 8 * 4) return launch_short<T, 8, 4>(a, o, stream);
   if (a.K <= 16 * 8) return launch_short<T, 16, 8>(a, o, stream);
-  if (a.K <= 64 * 4) return launch_short<T, 64, 4>(a, o, stream);
+  if (a.K <= 16 * 16) return launch_short<T, 16, 16>(a, o, stream);
   if (a.K <= kShortK) return launch_short<T, 64, 16>(a, o, stream);
   const dim3 grid((unsigned)(a.N * s.parts)), block(kLongThreads);
   const bool stream_by = a.N * a.K * (int64_t)sizeof(T) > kStreamBytes;
