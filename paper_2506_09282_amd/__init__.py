@@ -193,7 +193,9 @@ def _check_dev(*ts):
 
 def _stream_ptr(device) -> int:
     torch = _torch()
-    return torch.cuda.current_stream(device).cuda_stream
+    if device.index is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)  # (without a Stream object)
 
 
 def _raise(st: int, where: str):

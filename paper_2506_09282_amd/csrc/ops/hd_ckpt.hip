@@ -191,21 +191,26 @@ __device__ __forceinline__ bf16x8 bytes_bf16(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// Four waves; each takes DT tiles of 32 columns and KT tiles of 32 classes over a
-// slice of the groups. The waves share the dS operand through LDS.
-template <int P, int KT, int DT>
-__global__ __launch_bounds__(256) void ckpt_class_grad_kernel(
+// W waves, each with DT tiles of 32 columns and KT tiles of 32 classes over a slice of the
+// groups; they share the dS operand of R groups at a time through LDS. The next loads (the
+// next group's kept values to registers, the next R operands on their way to the other
+// half of LDS) are in flight while one group is multiplied; they are issued without a
+// condition, past the end for the last group again, so that a wait covers only the
+// older ones.
+template <int P, int KT, int DT, int W, int R, bool STREAM>
+__global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
     const u32x4* __restrict__ q, const float* __restrict__ scale, const u32x4* __restrict__ ds,
     float* __restrict__ out, int64_t D, int K, int ktiles, int64_t groups, int64_t per_slice,
     int64_t slice_stride, int accumulate) {
-  constexpr int OPS = KT * kSteps * P;  // operand fragments of a group
-  __shared__ u32x4 op[2][OPS * 64];
+  constexpr int FRAGS = KT * kSteps * P * 64;  // 16-byte fragments of a group's operand
+  constexpr int THREADS = 64 * W, PER = (R * FRAGS + THREADS - 1) / THREADS;
+  extern __shared__ u32x4 op[];  // [2][R][FRAGS]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, half = lane >> 5;
-  const int64_t d0 = ((int64_t)blockIdx.x * 4 + wave) * (32 * DT);
+  const int64_t d0 = ((int64_t)blockIdx.x * W + wave) * (32 * DT);
   const int kt0 = blockIdx.y * KT;
   const int64_t b0 = (int64_t)blockIdx.z * per_slice;
-  const int64_t b1 = b0 + per_slice < groups ? b0 + per_slice : groups;
+  const int own = (int)(b0 + per_slice < groups ? per_slice : groups - b0);
   int64_t dcol[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t) {
@@ -220,69 +225,97 @@ __global__ __launch_bounds__(256) void ckpt_class_grad_kernel(
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[k][t][r] = 0.0f;
 
-  // class tiles past the last repeat it (their results are not written)
-  auto operand_at = [&](int64_t b, int i) {
-    const int k = i / (kSteps * P * 64);
-    const int kt = kt0 + k < ktiles ? kt0 + k : ktiles - 1;
-    return ((b * ktiles + kt) * kSteps * P) * 64 + i % (kSteps * P * 64);
+  struct Kept {
+    u32x4 w[DT][2];
+    float s[DT];
   };
-  constexpr int PER = (OPS * 64 + 255) / 256;
   u32x4 stage[PER];
-  auto fetch = [&](int64_t b) {
+  auto group = [&](int i) { return b0 + (i < own ? i : own - 1); };
+  auto fetch = [&](int64_t b, Kept& f) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const u32x4* at = q + (b * 4 + 2 * p + half) * D + dcol[t];
+        f.w[t][p] = STREAM ? __builtin_nontemporal_load(at) : *at;
+      }
+      f.s[t] = scale[b * D + dcol[t]];
+    }
+  };
+  auto fetch_op = [&](int i0) {  // the operands of groups i0 .. i0 + R - 1
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = threadIdx.x + 256 * i;
-      if (OPS * 64 % 256 == 0 || at < OPS * 64) stage[i] = ds[operand_at(b, at)];
+      int at = threadIdx.x + THREADS * i;
+      if (R * FRAGS % THREADS != 0 && at >= R * FRAGS) at = R * FRAGS - 1;
+      const int64_t b = group(i0 + at / FRAGS);
+      at %= FRAGS;
+      // class tiles past the last repeat it (their results are not written)
+      const int k = at / (kSteps * P * 64);
+      const int kt = kt0 + k < ktiles ? kt0 + k : ktiles - 1;
+      stage[i] = ds[(b * ktiles + kt) * (kSteps * P * 64) + at % (kSteps * P * 64)];
     }
   };
   auto put = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = threadIdx.x + 256 * i;
-      if (OPS * 64 % 256 == 0 || at < OPS * 64) op[buf][at] = stage[i];
+      const int at = threadIdx.x + THREADS * i;
+      if (R * FRAGS % THREADS == 0 || at < R * FRAGS) op[buf * (R * FRAGS) + at] = stage[i];
     }
   };
-  if (b0 < b1) {
-    fetch(b0);
-    put(0);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int64_t b = b0; b < b1; ++b, buf ^= 1) {
-    u32x4 w[DT][2];
-    float s[DT];
+  auto multiply = [&](const Kept& f, int buf) {
+    bf16x8 qb[DT][kSteps];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-#pragma unroll
-      for (int p = 0; p < 2; ++p) w[t][p] = q[(b * 4 + 2 * p + half) * D + dcol[t]];
-      s[t] = scale[b * D + dcol[t]];
-    }
-    if (b + 1 < b1) fetch(b + 1);
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      bf16x8 qb[kSteps];
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
       for (int i = 0; i < kSteps; ++i)
-        qb[i] = bytes_bf16(w[t][i / 2][2 * (i % 2)], w[t][i / 2][2 * (i % 2) + 1]);
+        qb[t][i] = bytes_bf16(f.w[t][i / 2][2 * (i % 2)], f.w[t][i / 2][2 * (i % 2) + 1]);
 #pragma unroll
-      for (int k = 0; k < KT; ++k) {
-        f32x16 g;
+    for (int k = 0; k < KT; ++k) {
+      f32x16 g[DT];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) g[r] = 0.0f;
+      for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
+        for (int r = 0; r < 16; ++r) g[t][r] = 0.0f;
 #pragma unroll
-          for (int p = 0; p < P; ++p)
-            g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, op[buf][((k * kSteps + i) * P + p) * 64 + lane]), qb[i],
-                g, 0, 0, 0);
+      for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[k][t][r] = fmaf(s[t], g[r], acc[k][t][r]);
+        for (int p = 0; p < P; ++p) {
+          const u32x4 a = op[buf * FRAGS + ((k * kSteps + i) * P + p) * 64 + lane];
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+            g[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qb[t][i],
+                                                           g[t], 0, 0, 0);
+        }
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[k][t][r] = fmaf(f.s[t], g[t][r], acc[k][t][r]);
+    }
+  };
+  Kept f[2];
+  fetch_op(0);
+  fetch(group(0), f[0]);
+  put(0);
+  __syncthreads();
+  int i = 0, buf = 0;
+  for (; i + 2 <= own; i += 2) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      // (the operand first: the kept values may stay in flight longer)
+      if (r % R == 0) fetch_op(i + r + R);
+      fetch(group(i + r + 1), f[1 - r]);
+      __builtin_amdgcn_sched_barrier(0);  // (or the loads sink to their uses)
+      multiply(f[r], buf * R + r % R);
+      __builtin_amdgcn_sched_barrier(0);
+      if (r % R == R - 1) {
+        buf ^= 1;
+        put(buf);
+        __syncthreads();
       }
     }
-    if (b + 1 < b1) put(buf ^ 1);
-    __syncthreads();
   }
+  if (i < own) multiply(f[0], buf * R);
+
   float* dst = out + (int64_t)blockIdx.z * slice_stride;
 #pragma unroll
   for (int k = 0; k < KT; ++k)
@@ -300,52 +333,105 @@ __global__ __launch_bounds__(256) void ckpt_class_grad_kernel(
     }
 }
 
+// The slices' sums, added in order; eight loads in flight.
 __global__ __launch_bounds__(256) void ckpt_grad_join_kernel(const float* __restrict__ part,
                                                              float* __restrict__ dC,
                                                              int64_t total, int slices,
                                                              int accumulate) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
-  float v = part[i];
-  for (int s = 1; s < slices; ++s) v += part[s * total + i];
+  float v = 0.0f;
+  for (int s = 0; s < slices; s += 8) {
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = part[(s + j < slices ? s + j : slices - 1) * total + i];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (s + j < slices) v += p[j];
+  }
   dC[i] = accumulate ? dC[i] + v : v;
 }
 
 struct GradPlan {
-  int ktiles, kt, kblocks;  // class tiles, those of a workgroup, workgroups along K
+  int ktiles, kt, dt, waves;  // class tiles; those and column tiles of a wave; waves
+  int kblocks;                // workgroups along K
   int64_t dblocks, per_slice;
   int slices;
   size_t operand, total;  // bytes of the dS operand, and with the partial sums
 };
 
-constexpr int kGradDT = 2;
+// Eight waves share an operand of three parts (65536 x 10240 x 26: 173 us, four waves
+// 180); four are better where it is one (bf16, K = 10: 122 us, eight 143).
+constexpr int waves_of(int parts) { return parts == 3 ? 8 : 4; }
+// Column tiles of a wave: two read the operand half as often, where the sums of all
+// class tiles leave the registers for it.
+constexpr int dtiles_of(int kt) { return kt == 1 ? 2 : 1; }
+// Groups between two barriers: two where the operand's halves fit LDS.
+constexpr int round_of(int parts, int kt) { return parts * kt <= 6 ? 2 : 1; }
 
 GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
+  const int parts = dt == 0 ? DsParts<float>::kParts : DsParts<bf16raw>::kParts;
   GradPlan p;
   p.ktiles = (int)cdiv(K, 32);
-  p.kt = p.ktiles >= 2 ? 2 : 1;
+  // the classes of one workgroup: up to 128, which read the kept values once
+  p.kt = p.ktiles < 4 ? p.ktiles : 4;
+  p.dt = dtiles_of(p.kt);
+  p.waves = waves_of(parts);
   p.kblocks = (int)cdiv(p.ktiles, p.kt);
-  p.dblocks = cdiv(D, 4 * 32 * kGradDT);
+  p.dblocks = cdiv(D, p.waves * 32 * p.dt);
+  // Two workgroups for each compute unit; a slice of at least four groups, since its
+  // partial sums are written and read again.
   const int64_t groups = groups_of(N);
-  int64_t slices = cdiv(3 * (int64_t)num_cus(), p.dblocks * p.kblocks);
+  int64_t slices = 2 * (int64_t)num_cus() / (p.dblocks * p.kblocks);
   if (slices > groups / 4) slices = groups / 4;
   if (slices < 1) slices = 1;
   p.per_slice = cdiv(groups, slices);
   p.slices = (int)cdiv(groups, p.per_slice);
-  const int parts = dt == 0 ? DsParts<float>::kParts : DsParts<bf16raw>::kParts;
   p.operand = (size_t)groups * p.ktiles * kSteps * parts * 1024;
   p.total = p.operand + (p.slices > 1 ? (size_t)p.slices * K * D * 4 : 0);
   return p;
 }
 
-template <typename T, int KT>
-void launch_grad_kernel(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
-                        float* out, int64_t D, int K, int64_t groups, bool accumulate,
-                        hipStream_t stream) {
-  hipLaunchKernelGGL((ckpt_class_grad_kernel<DsParts<T>::kParts, KT, kGradDT>),
-                     dim3((unsigned)p.dblocks, (unsigned)p.kblocks, (unsigned)p.slices), dim3(256),
-                     0, stream, q, s, ds, out, D, K, p.ktiles, groups, p.per_slice,
-                     (int64_t)K * D, (int)(accumulate && p.slices == 1));
+constexpr int64_t kStreamBytes = int64_t(192) << 20;
+
+template <typename T, int KT, bool STREAM>
+hipError_t launch_grad_as(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
+                          float* out, int64_t D, int K, int64_t groups, bool accumulate,
+                          hipStream_t stream) {
+  constexpr int P = DsParts<T>::kParts, W = waves_of(P), R = round_of(P, KT);
+  constexpr int lds = 2 * R * KT * kSteps * P * 1024;
+  const auto kernel = ckpt_class_grad_kernel<P, KT, dtiles_of(KT), W, R, STREAM>;
+  if (lds > 64 * 1024) {  // above the default limit: raised once per device and kernel
+    static PerDeviceOnce once;
+    const hipError_t e = once_per_device(once, [&] {
+      return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    });
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.dblocks, (unsigned)p.kblocks, (unsigned)p.slices),
+                     dim3(64 * W), lds, stream, q, s, ds, out, D, K, p.ktiles, groups,
+                     p.per_slice, (int64_t)K * D, (int)(accumulate && p.slices == 1));
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_grad_kernel(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
+                              float* out, int64_t D, int K, int64_t groups, bool accumulate,
+                              hipStream_t stream) {
+  // kept values past the caches, and read by one workgroup each
+  const bool by = groups * kRows * D > kStreamBytes && p.kblocks == 1;
+  auto go = [&](auto launch) { return launch(p, q, s, ds, out, D, K, groups, accumulate, stream); };
+  switch (p.kt) {
+    case 1:
+      return by ? go(launch_grad_as<T, 1, true>) : go(launch_grad_as<T, 1, false>);
+    case 2:
+      return by ? go(launch_grad_as<T, 2, true>) : go(launch_grad_as<T, 2, false>);
+    case 3:
+      return by ? go(launch_grad_as<T, 3, true>) : go(launch_grad_as<T, 3, false>);
+    default:
+      return by ? go(launch_grad_as<T, 4, true>) : go(launch_grad_as<T, 4, false>);
+  }
 }
 
 template <typename T>
@@ -364,11 +450,7 @@ hipError_t launch_grad_typed(const void* dS, int64_t lds, const void* image, flo
   const float* s =
       reinterpret_cast<const float*>(static_cast<const char*>(image) + scales_at(N, D));
   float* out = p.slices > 1 ? part : dC;
-  if (p.kt == 1)
-    launch_grad_kernel<T, 1>(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
-  else
-    launch_grad_kernel<T, 2>(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
-  e = hipGetLastError();
+  e = launch_grad_kernel<T>(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
   if (e != hipSuccess || p.slices == 1) return e;
   hipLaunchKernelGGL(ckpt_grad_join_kernel, dim3((unsigned)cdiv(K * D, 256)), dim3(256), 0, stream,
                      part, dC, K * D, p.slices, (int)accumulate);

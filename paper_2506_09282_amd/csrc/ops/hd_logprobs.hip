@@ -23,6 +23,10 @@
 //   the chip has room for; the last workgroup to finish joins the parts in order.
 #include "hd_ops.hpp"
 
+// A product that is rounded is meant to be (q = fl(c m) is taken off itself below); what is
+// to be fused is written so.
+#pragma clang fp contract(off)
+
 namespace hd {
 namespace ops {
 
@@ -30,6 +34,11 @@ namespace {
 
 constexpr int kShortK = 1024;
 constexpr int kLongThreads = 256;
+// 16-byte chunks that a thread takes in a step: two of bf16, whose work for each byte
+// is twice fp32's (4096 x 65536 top 4: 121 us with one, 116 with two; fp32 2048 x 100003 133
+// with one, 151 with two), and where rows are split, which leaves a wave one step and
+// its list one sort.
+constexpr int chunks_of(int esize, bool split) { return esize == 4 && !split ? 1 : 2; }
 // Scores past the caches: loads and stores that do not stay there.
 constexpr int64_t kStreamBytes = int64_t(192) << 20;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -58,38 +67,46 @@ __device__ __forceinline__ float key_score(uint64_t key) {
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
 
-// The running statistics of a part of a row. m is at least the lowest finite number, so
-// that -inf - m is -inf; the sum is 0 only where nothing was there.
+// The running statistics of a part of a row, in powers of two: z_k = c s_k - q with
+// c = scale log2(e) and q = c m rounded to fp32, one fused multiply-add. m is the largest
+// score, at least the lowest finite number (so that an -inf stays below it); sum is 0
+// only where nothing was there. Where c m is past fp32's range (`far`), z is
+// c (s - m) and q stands for 0 in it.
 struct Stats {
-  float m, sum, ez;  // ez: sum of z exp(z), z in powers of two
+  float m, q, sum, ez;  // ez: sum of z 2^z
 };
-__device__ __forceinline__ Stats stats_none() { return Stats{kLowest, 0.0f, 0.0f}; }
+__device__ __forceinline__ bool far_of(float q) { return !(fabsf(q) < INFINITY); }
+__device__ __forceinline__ Stats stats_none(float c) {
+  return Stats{kLowest, kLowest * c, 0.0f, 0.0f};
+}
+// How far, in powers of two, a's reference lies above that of m (q = fl(c m)); <= 0.
+__device__ __forceinline__ float stats_step(const Stats& a, float m, float q, float c) {
+  const float d = far_of(q) || far_of(a.q) ? (a.m - m) * c : a.q - q;
+  return fmaxf(d, kUnder);
+}
 __device__ __forceinline__ void stats_raise(Stats& a, float m, float c) {
-  const float d = fmaxf((a.m - m) * c, kUnder), f = exp2_fast(d);  // d <= 0
+  const float q = m * c, d = stats_step(a, m, q, c), f = exp2_fast(d);
   a.ez = f * fmaf(d, a.sum, a.ez);
   a.sum *= f;
   a.m = m;
+  a.q = q;
 }
-__device__ __forceinline__ Stats stats_join(Stats a, Stats b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  stats_raise(a, m, c);
-  stats_raise(b, m, c);
-  return Stats{m, a.sum + b.sum, a.ez + b.ez};
-}
-__device__ __forceinline__ void stats_add(Stats& a, float s, float c) {
-  const float z = (s - a.m) * c, e = exp2_fast(z);
+__device__ __forceinline__ void stats_add_z(Stats& a, float z) {
+  const float e = exp2_fast(z);
   a.sum += e;
   a.ez = fmaf(e, fmaxf(z, kUnder), a.ez);  // (NaN is in e)
 }
-// Over LANES neighbouring lanes; both lanes of a pair add the same two numbers.
-template <int LANES, int OFF = 1>
-__device__ __forceinline__ Stats stats_across(Stats a, float c) {
-  if constexpr (OFF < LANES) {
-    const Stats b{lane_xor<OFF>(a.m), lane_xor<OFF>(a.sum), lane_xor<OFF>(a.ez)};
-    return stats_across<LANES, 2 * OFF>(stats_join(a, b, c), c);
+template <int LEN>
+__device__ __forceinline__ void stats_add(Stats& a, const float (&s)[LEN], float c) {
+  if (far_of(a.q)) {
+#pragma unroll
+    for (int e = 0; e < LEN; ++e) stats_add_z(a, (s[e] - a.m) * c);
+  } else {
+#pragma unroll
+    for (int e = 0; e < LEN; ++e) stats_add_z(a, fmaf(s[e], c, -a.q));
   }
-  return a;
 }
+// Over LANES neighbouring lanes; both lanes of a pair add the same two numbers.
 template <int LANES, int OFF = 1>
 __device__ __forceinline__ float max_across(float v) {
   if constexpr (OFF < LANES) return max_across<LANES, 2 * OFF>(fmaxf(v, lane_xor<OFF>(v)));
@@ -109,17 +126,28 @@ __device__ __forceinline__ uint32_t min_across(uint32_t v) {
   return v;
 }
 
+template <int LANES>
+__device__ __forceinline__ Stats stats_across(Stats a, float c) {
+  stats_raise(a, max_across<LANES>(a.m), c);
+  a.sum = sum_across<LANES>(a.sum);
+  a.ez = sum_across<LANES>(a.ez);
+  return a;
+}
+
 struct Row {  // a finished row
   float m, logsum, entropy;
   bool none, bad;
 };
-__device__ __forceinline__ Row finish(Stats a) {
+__device__ __forceinline__ Row finish(Stats a, float c) {
   Row r;
   r.none = a.sum == 0.0f;
   r.bad = a.sum != a.sum;
-  r.logsum = r.none ? 0.0f : logf(a.sum);
+  // the sum is of 2^(c s - q): log sum exp scale (s - m) has q - c m, what q was rounded
+  // by, added
+  const float log_z = logf(a.sum);
+  r.logsum = r.none ? 0.0f : far_of(a.q) ? log_z : fmaf(fmaf(-a.m, c, a.q), kLn2, log_z);
   r.m = r.none ? -INFINITY : r.bad ? NAN : a.m;
-  r.entropy = r.none ? 0.0f : r.logsum - (a.ez * kLn2) / a.sum;
+  r.entropy = r.none ? 0.0f : log_z - (a.ez * kLn2) / a.sum;
   return r;
 }
 // log probability of a score in a finished row
@@ -219,8 +247,9 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out
   const T* row = static_cast<const T*>(a.scores) + nn * a.ld;
   const uint8_t* mrow = a.mask ? a.mask + nn * a.ldm : nullptr;
   const int K = (int)a.K;
+  const float c = a.scale * kLog2e;
   float v[VPL];
-  Stats st = stats_none();
+  Stats st = stats_none(c);
 #pragma unroll
   for (int j = 0; j < VPL; ++j) {
     const int k = lane + LPR * j;
@@ -229,12 +258,11 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a, Out
     st.m = fmaxf(st.m, v[j]);
   }
   st.m = max_across<LPR>(st.m);
-  const float c = a.scale * kLog2e;
-#pragma unroll
-  for (int j = 0; j < VPL; ++j) stats_add(st, v[j], c);
+  st.q = st.m * c;
+  stats_add(st, v, c);
   st.sum = sum_across<LPR>(st.sum);
   st.ez = sum_across<LPR>(st.ez);
-  const Row r = finish(st);
+  const Row r = finish(st, c);
   if (live && lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
   if (o.top == 0) return;
   if constexpr (LPR == 64) {
@@ -300,7 +328,7 @@ struct Flight {
                       : reinterpret_cast<const m_a*>(mp)[i];
     }
   }
-  __device__ __forceinline__ void scores(float (&v)[LEN]) const {
+  __device__ __forceinline__ void scores(float* v) const {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int e = 0; e < LEN; ++e) {
@@ -327,17 +355,16 @@ struct Flight {
 };
 
 // Joins the waves' statistics and lists of a workgroup; the result is whole in wave 0.
-template <bool TOP>
+template <bool TOP, int WAVES>
 __device__ __forceinline__ void join_waves(Stats& st, uint64_t& list, float c, int lane, int wave,
-                                           int waves, Stats* sh_st, uint64_t* sh_key) {
+                                           Stats* sh_st, uint64_t* sh_key) {
   if (lane == 0) sh_st[wave] = st;
   if (TOP && lane < kMaxTop) sh_key[wave * kMaxTop + lane] = list;
   __syncthreads();
   if (wave != 0) return;
-  st = sh_st[0];
-  for (int w = 1; w < waves; ++w) st = stats_join(st, sh_st[w], c);
+  st = stats_across<WAVES>(sh_st[lane % WAVES], c);
   if (TOP)
-    for (int w = 1; w < waves; ++w) {
+    for (int w = 1; w < WAVES; ++w) {
       const uint64_t other = sh_key[w * kMaxTop + (63 - lane) % kMaxTop];
       list = merge64(lane < kMaxTop ? list : other, lane);
     }
@@ -372,10 +399,11 @@ __device__ __forceinline__ void put_key(uint32_t* p, uint64_t v) {
                      __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <typename T, bool TOP, bool MASK, bool STREAM>
+template <typename T, bool TOP, bool MASK, bool STREAM, int kChunks>
 __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArgs a, Out o,
                                                                      Split sp) {
   constexpr int LEN = Chunk<T>::kLen, WAVES = kLongThreads / 64;
+  constexpr int VALS = kChunks * LEN;
   __shared__ Stats sh_st[WAVES];
   __shared__ uint64_t sh_key[WAVES * kMaxTop];
   __shared__ uint32_t sh_last, sh_bar;
@@ -391,17 +419,16 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     if (threadIdx.x == 0) sh_bar = 0;
     __syncthreads();
   }
-  Stats st = stats_none();
+  Stats st = stats_none(c);
   TopList list{0, -INFINITY};
-  bool first = true;
-  constexpr int STEP = kLongThreads * LEN;
-  auto add = [&](float(&v)[LEN], int64_t k0) {
+  constexpr int ROUND = kLongThreads * LEN, STEP = kChunks * ROUND;
+  auto class_of = [](int e) { return (uint32_t)(e / LEN * ROUND + e % LEN); };
+  auto add = [&](float(&v)[VALS], uint32_t id0) {  // id0: the class of v[0]
     float m = v[0];
 #pragma unroll
-    for (int e = 1; e < LEN; ++e) m = fmaxf(m, v[e]);
+    for (int e = 1; e < VALS; ++e) m = fmaxf(m, v[e]);
     if (m > st.m) stats_raise(st, m, c);
-#pragma unroll
-    for (int e = 0; e < LEN; ++e) stats_add(st, v[e], c);
+    stats_add(st, v, c);
     if (!TOP || !__ballot(m > list.bar)) return;
     // What is below any wave's T-th score cannot be among the T best of the row. (Looked
     // up only here: in every step it would cost more than it saves.)
@@ -409,27 +436,28 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     if (shared_bar) list.bar = fmaxf(list.bar, score_below(shared_bar));
     float bar = list.bar;
     if (!__ballot(m > bar)) return;
-    const uint32_t id0 = (uint32_t)(k0 + (int64_t)threadIdx.x * LEN);
-    if (first) {
-      // The lanes' largest, sorted, begin the list; its T-th is a bar for the rest (without
-      // it the whole first chunk would pass one by one).
+    if (bar == -INFINITY) {
+      // Fewer than T so far. The lanes' largest go in together, sorted; then their T-th is a
+      // bar for the rest (or a whole chunk would pass one by one).
       int at = 0;
 #pragma unroll
-      for (int e = LEN - 1; e >= 0; --e) at = v[e] == m ? e : at;
-      list.key = sort64(m > -INFINITY ? key_of(m, id0 + at) : 0, lane);
+      for (int e = VALS - 1; e >= 0; --e) at = v[e] == m ? e : at;
+      const uint64_t fresh = sort64(m > -INFINITY ? key_of(m, id0 + class_of(at)) : 0, lane);
+      const uint64_t held = lane_xor<32>(lane_xor<16>(lane_xor<8>(
+          lane_xor<4>(lane_xor<2>(lane_xor<1>(list.key))))));  // the other way round
+      list.key = merge64(lane < kMaxTop ? fresh : held, lane);
       const uint64_t s = lane_key(list.key, o.top - 1);
-      if (s) bar = fmaxf(bar, score_below((uint32_t)(s >> 32)));
+      if (s) bar = score_below((uint32_t)(s >> 32));
 #pragma unroll
-      for (int e = 0; e < LEN; ++e) v[e] = e == at ? -INFINITY : v[e];
-      first = false;
+      for (int e = 0; e < VALS; ++e) v[e] = e == at ? -INFINITY : v[e];
     }
 #pragma unroll
-    for (int e = 0; e < LEN; ++e)
+    for (int e = 0; e < VALS; ++e)
       for (uint64_t pass = __ballot(v[e] > bar); pass; pass &= pass - 1) {
         const int from = (int)__builtin_ctzll(pass);
         const float s =
             __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[e]), from));
-        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)id0, from) + e;
+        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)id0, from) + class_of(e);
         list.key = list_insert(list.key, key_of(s, id), lane);
       }
     const uint64_t last = lane_key(list.key, o.top - 1);
@@ -439,34 +467,52 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     }
   };
   // Whole steps, the next one's loads in flight while one is worked on (past the end the
-  // last one's again, so that they need no condition), then the step that ends inside.
+  // last one's again, so that they need no condition), then the step that ends inside. Steps
+  // are counted from the row's start wherever it lies, so that a result does not depend
+  // on alignment (rows of odd length cost a fifth for it: 2048 x 100003 bf16 96 us,
+  // 2048 x 100096 79). Classes come in ascending order, so that of equal scores the
+  // one already listed is the lower class.
   const int64_t k_begin = part * sp.part_len, whole = (k_end - k_begin) / STEP;
   const int64_t steps = cdiv(k_end - k_begin, STEP);
-  Flight<T, MASK, STREAM> flight;
+  Flight<T, MASK, STREAM> flight[kChunks];
+  auto place = [&](int64_t i, int u) {
+    return k_begin + i * STEP + u * ROUND + (int64_t)threadIdx.x * LEN;
+  };
   auto fetch = [&](int64_t i) {
-    const int64_t k = k_begin + (i < whole ? i : whole - 1) * STEP + (int64_t)threadIdx.x * LEN;
-    flight.load(row + k, MASK ? mrow + k : nullptr);
+#pragma unroll
+    for (int u = 0; u < kChunks; ++u) {
+      const int64_t k = place(i < whole ? i : whole - 1, u);
+      flight[u].load(row + k, MASK ? mrow + k : nullptr);
+    }
   };
   if (whole > 0) fetch(0);
   for (int64_t i = 0; i < steps; ++i) {
-    const int64_t k0 = k_begin + i * STEP;
-    float v[LEN];
+    float v[VALS];
     if (i < whole) {
-      flight.scores(v);
+#pragma unroll
+      for (int u = 0; u < kChunks; ++u) flight[u].scores(v + u * LEN);
       fetch(i + 1);
       __builtin_amdgcn_sched_barrier(0);  // (or the loads sink below the work)
     } else {
-      const int64_t k = k0 + (int64_t)threadIdx.x * LEN;
 #pragma unroll
-      for (int e = 0; e < LEN; ++e) {
-        v[e] = k + e < k_end ? load_elem(row, k + e) : -INFINITY;
-        if (MASK && k + e < k_end && !mrow[k + e]) v[e] = -INFINITY;
+      for (int u = 0; u < kChunks; ++u) {
+        const int64_t k = place(i, u);
+        if (k + LEN <= k_end) {
+          flight[u].load(row + k, MASK ? mrow + k : nullptr);
+          flight[u].scores(v + u * LEN);
+        } else {
+#pragma unroll
+          for (int e = 0; e < LEN; ++e) {
+            const bool in = k + e < k_end && (!MASK || mrow[k + e]);
+            v[u * LEN + e] = in ? load_elem(row, k + e) : -INFINITY;
+          }
+        }
       }
     }
-    add(v, k0);
+    add(v, (uint32_t)place(i, 0));
   }
   st = stats_across<64>(st, c);
-  join_waves<TOP>(st, list.key, c, lane, wave, WAVES, sh_st, sh_key);
+  join_waves<TOP, WAVES>(st, list.key, c, lane, wave, sh_st, sh_key);
 
   if (sp.parts > 1) {
     uint32_t* mine = sp.words + ((int64_t)n * sp.parts + part) * kPartWords;
@@ -488,9 +534,10 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       // lane p holds part p
       uint32_t* w = words + (int64_t)lane * kPartWords;
       uint64_t keys[kMaxTop] = {};
-      st = stats_none();
+      st = stats_none(c);
       if (lane < sp.parts) {
         st.m = __uint_as_float(get_word(w));
+        st.q = st.m * c;
         st.sum = __uint_as_float(get_word(w + 1));
         st.ez = __uint_as_float(get_word(w + 2));
         if (TOP) {
@@ -501,17 +548,13 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       }
       st = stats_across<64>(st, c);
       if (TOP) {
-        // the T-th largest of the parts' best bounds the T-th of all from below
-        const uint64_t bar = lane_key(sort64(keys[0], lane), o.top - 1);
-        list.key = 0;
+        // The parts' best, sorted, begin the list; its T-th is a bar for the rest.
+        list.key = sort64(keys[0], lane);
+        const uint64_t bar = lane_key(list.key, o.top - 1);
 #pragma unroll
-        for (int t = 0; t < kMaxTop; ++t) {
-          uint64_t pass = __ballot(keys[t] != 0 && keys[t] >= bar);
-          while (pass) {
-            const int from = (int)__builtin_ctzll(pass);
-            pass &= pass - 1;
-            list.key = list_insert(list.key, lane_key(keys[t], from), lane);
-          }
+        for (int t = 1; t < kMaxTop; ++t) {
+          for (uint64_t pass = __ballot(keys[t] > bar); pass; pass &= pass - 1)
+            list.key = list_insert(list.key, lane_key(keys[t], (int)__builtin_ctzll(pass)), lane);
         }
       }
     }
@@ -520,20 +563,19 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       words[i] = 0;
   }
   if (wave != 0) return;
-  const Row r = finish(st);
+  const Row r = finish(st, c);
   if (lane == 0) write_row(r, row, mrow, a.y, n, a.K, a.scale, o);
   if (TOP && lane < o.top) write_top(r, list.key, n, lane, a.scale, o);
 }
 
-// Parts of a row: enough workgroups for every compute unit to hold two, of at
-// least two steps each.
-Split split_of(int64_t N, int64_t K, int len) {
+// Parts of a row: enough workgroups for every compute unit to hold two.
+Split split_of(int64_t N, int64_t K, int esize) {
   Split s{1, 0, nullptr, nullptr};
-  const int64_t step = (int64_t)kLongThreads * len, steps = cdiv(K, step);
+  const int64_t step = (int64_t)kLongThreads * chunks_of(esize, true) * (16 / esize);
+  const int64_t steps = cdiv(K, step);
   int64_t parts = cdiv(2 * (int64_t)num_cus(), N);
   if (parts > kMaxParts) parts = kMaxParts;
-  if (parts > steps / 2) parts = steps / 2;
-  if (parts < 1) parts = 1;
+  if (parts > steps) parts = steps;
   const int64_t per = cdiv(steps, parts);
   s.parts = (int)cdiv(steps, per);
   s.part_len = per * step;
@@ -560,16 +602,22 @@ hipError_t launch_typed(const LogprobsArgs& a, const Out& o, Split s, hipStream_
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, o, s);
   };
-  if (stream_by) {
-    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, true>);
-    else if (o.top) go(logprobs_long_kernel<T, true, false, true>);
-    else if (a.mask) go(logprobs_long_kernel<T, false, true, true>);
-    else go(logprobs_long_kernel<T, false, false, true>);
+  constexpr int C1 = chunks_of(sizeof(T), false), C2 = chunks_of(sizeof(T), true);
+  if (s.parts > 1) {
+    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, false, C2>);
+    else if (o.top) go(logprobs_long_kernel<T, true, false, false, C2>);
+    else if (a.mask) go(logprobs_long_kernel<T, false, true, false, C2>);
+    else go(logprobs_long_kernel<T, false, false, false, C2>);
+  } else if (stream_by) {
+    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, true, C1>);
+    else if (o.top) go(logprobs_long_kernel<T, true, false, true, C1>);
+    else if (a.mask) go(logprobs_long_kernel<T, false, true, true, C1>);
+    else go(logprobs_long_kernel<T, false, false, true, C1>);
   } else {
-    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, false>);
-    else if (o.top) go(logprobs_long_kernel<T, true, false, false>);
-    else if (a.mask) go(logprobs_long_kernel<T, false, true, false>);
-    else go(logprobs_long_kernel<T, false, false, false>);
+    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, false, C1>);
+    else if (o.top) go(logprobs_long_kernel<T, true, false, false, C1>);
+    else if (a.mask) go(logprobs_long_kernel<T, false, true, false, C1>);
+    else go(logprobs_long_kernel<T, false, false, false, C1>);
   }
   return hipGetLastError();
 }
@@ -696,7 +744,7 @@ LogprobsArgs rows_from(const LogprobsArgs& a, int64_t n0, int64_t most) {
 
 size_t logprobs_ws_bytes(int64_t N, int64_t K, int dt) {
   if (K <= kShortK) return 0;
-  const Split s = split_of(N, K, dt == 0 ? 4 : 8);
+  const Split s = split_of(N, K, dt == 0 ? 4 : 2);
   if (s.parts == 1) return 0;
   return tickets_bytes(N) + (size_t)N * s.parts * kPartWords * 4;
 }
@@ -704,7 +752,7 @@ size_t logprobs_ws_bytes(int64_t N, int64_t K, int dt) {
 hipError_t launch_logprobs(const LogprobsArgs& all, float* logp, float* entropy, float* stats,
                            int32_t* ids, float* top_logp, int top, void* workspace,
                            hipStream_t stream) {
-  Split s = split_of(all.N, all.K, all.dt == 0 ? 4 : 8);  // (one part where N > kMaxRows)
+  Split s = split_of(all.N, all.K, all.dt == 0 ? 4 : 2);  // (one part where N > kMaxRows)
   s.tickets = static_cast<uint32_t*>(workspace);
   s.words = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + tickets_bytes(all.N));
   // a launch holds at most 2^32 threads
