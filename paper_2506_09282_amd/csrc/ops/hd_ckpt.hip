@@ -18,6 +18,8 @@
 // v_mfma_f32_32x32x16_bf16, neighbouring lanes are neighbouring columns, and
 // storing is coalesced too. dS is first cut and laid out as the other
 // operand (a small launch), so that the product's loop holds no transposition.
+#include <type_traits>
+
 #include "hd_ops.hpp"
 
 namespace hd {
@@ -35,86 +37,169 @@ __host__ __device__ inline int64_t scales_at(int64_t N, int64_t D) {
 
 // ---- store and load --------------------------------------------------------------
 
-// COLS columns to a thread (2: bf16 pairs, 4-byte loads).
-template <typename T, int COLS>
+// How a lane's four columns of 256 lie. Where rows start at multiples of 16 bytes (8 in
+// bf16) they are neighbours, in one load; elsewhere they are 64 apart and each load of a
+// wave is a run, which is faster than wide loads across the lines' ends (1999 x 4097
+// bf16 kept: 11.8 us wide, @@ so).
+// kNear, and past the caches (kStreamBytes) kNearOnce: rows pass once and do not stay there,
+// the kept values, a quarter or half as large, do.
+enum Columns { kApart, kNear, kNearOnce };
+constexpr int64_t kStreamBytes = int64_t(64) << 20;
+
+template <int M>
+__device__ __forceinline__ int64_t column_of(int64_t d0, int lane, int c) {
+  return M == kApart ? d0 + 64 * c + lane : d0 + 4 * lane + c;
+}
+
+template <bool ONCE>
+__device__ __forceinline__ void load_row4(const float* p, float (&v)[4]) {
+  const f32x4* at = reinterpret_cast<const f32x4*>(p);
+  const f32x4 x = ONCE ? __builtin_nontemporal_load(at) : *at;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) v[c] = x[c];
+}
+template <bool ONCE>
+__device__ __forceinline__ void load_row4(const bf16raw* p, float (&v)[4]) {
+  const u32x2* at = reinterpret_cast<const u32x2*>(p);
+  const u32x2 x = ONCE ? __builtin_nontemporal_load(at) : *at;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    v[c] = __uint_as_float(c % 2 ? x[c / 2] & 0xffff0000u : x[c / 2] << 16);
+}
+template <bool ONCE>
+__device__ __forceinline__ void store_row4(float* p, const float (&v)[4]) {
+  f32x4* at = reinterpret_cast<f32x4*>(p);
+  const f32x4 x = {v[0], v[1], v[2], v[3]};
+  if (ONCE)
+    __builtin_nontemporal_store(x, at);
+  else
+    *at = x;
+}
+template <bool ONCE>
+__device__ __forceinline__ void store_row4(bf16raw* p, const float (&v)[4]) {
+  u32x2* at = reinterpret_cast<u32x2*>(p);
+  const u32x2 x = {(uint32_t)to_bf16(v[0]) | (uint32_t)to_bf16(v[1]) << 16,
+                   (uint32_t)to_bf16(v[2]) | (uint32_t)to_bf16(v[3]) << 16};
+  if (ONCE)
+    __builtin_nontemporal_store(x, at);
+  else
+    *at = x;
+}
+
+// A workgroup takes a group of 256 columns: a wave 16 of its rows, a lane four
+// columns; the waves' largest values meet in LDS.
+template <typename T, int M>
 __global__ __launch_bounds__(256) void ckpt_store_kernel(const T* __restrict__ H, int64_t ldh,
                                                          int64_t N, int64_t D, u32x4* out,
                                                          float* out_s) {
-  const int64_t d = ((int64_t)blockIdx.x * 256 + threadIdx.x) * COLS;
-  if (d >= D) return;
-  const int64_t b = blockIdx.y, n0 = b * kRows;
-  const bool pair = COLS == 2 && d + 1 < D;
-  float v[COLS][kRows];
-  const T* p = H + n0 * ldh + d;
-  // rows past the end read the last one again, so that no load waits on a branch
-  const int last = N - n0 < kRows ? (int)(N - n0) - 1 : kRows - 1;
+  __shared__ u32x4 tops[4][64];
+  const int lane = threadIdx.x & 63, ch = threadIdx.x >> 6;
+  const int64_t d0 = (int64_t)blockIdx.x * 256, b = blockIdx.y;
+  const int64_t n0 = b * kRows + 16 * ch;
+  float v[16][4];
+  // rows and columns past the end read the last one again, so that no load waits on a branch
+  const T* col[4];
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    const int64_t at = (r < last ? r : last) * ldh;
-    if constexpr (COLS == 2) {
-      const uint32_t w =
-          pair ? *reinterpret_cast<const uint32_t*>(p + at) : (uint32_t)p[at];
-      v[0][r] = __uint_as_float(w << 16);
-      v[1][r] = __uint_as_float(w & 0xffff0000u);
-    } else {
-      v[0][r] = load_elem(p, at);
-    }
+  for (int c = 0; c < 4; ++c) {
+    const int64_t d = column_of<M>(d0, lane, c);
+    col[c] = H + (d < D ? d : D - 1);
   }
-  if (last < kRows - 1) {
+  if (M != kApart && d0 + 256 <= D) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
+    for (int r = 0; r < 16; ++r)
+      load_row4<M == kNearOnce>(col[0] + (n0 + r < N ? n0 + r : N - 1) * ldh, v[r]);
+  } else {
 #pragma unroll
-      for (int c = 0; c < COLS; ++c) v[c][r] = r <= last ? v[c][r] : 0.0f;
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        v[r][c] = load_elem(col[c], (n0 + r < N ? n0 + r : N - 1) * ldh);
+  }
+  if (n0 + 16 > N) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[r][c] = n0 + r < N ? v[r][c] : 0.0f;
+  }
+  u32x4 top = {0, 0, 0, 0};  // as bits, an infinity and NaN are larger than any number
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t a = __float_as_uint(v[r][c]) & 0x7fffffffu;
+      top[c] = a > top[c] ? a : top[c];
+    }
+  tops[ch][lane] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const u32x4 t = tops[w][lane];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) top[c] = t[c] > top[c] ? t[c] : top[c];
   }
 #pragma unroll
-  for (int c = 0; c < COLS; ++c) {
-    if (c == 1 && !pair) break;
-    uint32_t top = 0;  // as bits, an infinity and NaN are larger than any number
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const uint32_t a = __float_as_uint(v[c][r]) & 0x7fffffffu;
-      top = a > top ? a : top;
-    }
-    const bool bad = top >= 0x7f800000u;
-    const float s = __uint_as_float(top) * kInv127;
+  for (int c = 0; c < 4; ++c) {
+    const int64_t d = column_of<M>(d0, lane, c);
+    const bool bad = top[c] >= 0x7f800000u;
+    const float s = __uint_as_float(top[c]) * kInv127;
     float inv = 1.0f / s;
     if (bad || !(inv < INFINITY)) inv = 0.0f;  // 0, or too small for its inverse: kept as 0
+    u32x4 w;
 #pragma unroll
-    for (int ch = 0; ch < kRows / 16; ++ch) {
-      u32x4 w;
+    for (int i = 0; i < 4; ++i) {
+      w[i] = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float q = rintf((bad ? 0.0f : v[c][ch * 16 + 4 * i + e]) * inv);
-          w[i] |= ((uint32_t)(int)fminf(fmaxf(q, -127.0f), 127.0f) & 255u) << (8 * e);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float q = rintf((bad ? 0.0f : v[4 * i + e][c]) * inv);
+        w[i] |= ((uint32_t)(int)fminf(fmaxf(q, -127.0f), 127.0f) & 255u) << (8 * e);
       }
-      out[(b * 4 + ch) * D + d + c] = w;
     }
-    out_s[b * D + d + c] = bad ? NAN : s;
+    if (d < D) {
+      out[(b * 4 + ch) * D + d] = w;
+      if (ch == 0) out_s[b * D + d] = bad ? NAN : s;
+    }
   }
 }
 
-template <typename T>
+// A lane takes 16 rows of four columns.
+template <typename T, int M>
 __global__ __launch_bounds__(256) void ckpt_load_kernel(const u32x4* __restrict__ q,
                                                         const float* __restrict__ scale, T* H,
                                                         int64_t ldh, int64_t N, int64_t D) {
-  const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (d >= D) return;
-  const int64_t b = blockIdx.y;
-  const float s = scale[b * D + d];
-  u32x4 w[kRows / 16];
+  const int lane = threadIdx.x & 63, ch = threadIdx.x >> 6;
+  const int64_t d0 = (int64_t)blockIdx.x * 256, b = blockIdx.y;
+  const int64_t n0 = b * kRows + 16 * ch;
+  u32x4 w[4];
+  float s[4];
 #pragma unroll
-  for (int ch = 0; ch < kRows / 16; ++ch) w[ch] = q[(b * 4 + ch) * D + d];
+  for (int c = 0; c < 4; ++c) {
+    const int64_t d = column_of<M>(d0, lane, c), in = d < D ? d : D - 1;
+    w[c] = q[(b * 4 + ch) * D + in];
+    s[c] = scale[b * D + in];
+  }
 #pragma unroll
-  for (int ch = 0; ch < kRows / 16; ++ch)
+  for (int e = 0; e < 16; ++e) {
+    if (n0 + e >= N) break;
+    float v[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t n = b * kRows + ch * 16 + e;
-      if (n < N) store_elem(H, n * ldh + d, (float)(int8_t)(w[ch][e / 4] >> (8 * (e % 4))) * s);
+    for (int c = 0; c < 4; ++c) v[c] = (float)(int8_t)(w[c][e / 4] >> (8 * (e % 4))) * s[c];
+    T* row = H + (n0 + e) * ldh;
+    if (M != kApart && d0 + 256 <= D) {
+      store_row4<M == kNearOnce>(row + d0 + 4 * lane, v);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int64_t d = column_of<M>(d0, lane, c);
+        if (d < D) store_elem(row, d, v[c]);
+      }
     }
+  }
+}
+
+Columns columns_of(const void* rows, int64_t ld, int64_t N, int64_t D, int dt) {
+  const int64_t es = dt == 0 ? 4 : 2;
+  if ((uintptr_t)rows % (4 * es) != 0 || ld % 4 != 0) return kApart;
+  return N * D * es > kStreamBytes ? kNearOnce : kNear;
 }
 
 // ---- the other operand --------------------------------------------------------------
@@ -392,7 +477,7 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
   return p;
 }
 
-constexpr int64_t kStreamBytes = int64_t(192) << 20;
+constexpr int64_t kStreamKept = int64_t(192) << 20;
 
 template <typename T, int KT, bool STREAM>
 hipError_t launch_grad_as(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
@@ -420,7 +505,7 @@ hipError_t launch_grad_kernel(const GradPlan& p, const u32x4* q, const float* s,
                               float* out, int64_t D, int K, int64_t groups, bool accumulate,
                               hipStream_t stream) {
   // kept values past the caches, and read by one workgroup each
-  const bool by = groups * kRows * D > kStreamBytes && p.kblocks == 1;
+  const bool by = groups * kRows * D > kStreamKept && p.kblocks == 1;
   auto go = [&](auto launch) { return launch(p, q, s, ds, out, D, K, groups, accumulate, stream); };
   switch (p.kt) {
     case 1:
@@ -467,16 +552,19 @@ hipError_t launch_ckpt_store(const void* H, int64_t ldh, int64_t N, int64_t D, i
                              void* image, hipStream_t stream) {
   u32x4* q = static_cast<u32x4*>(image);
   float* s = reinterpret_cast<float*>(static_cast<char*>(image) + scales_at(N, D));
-  const unsigned groups = (unsigned)groups_of(N);
-  if (dt == 0)
-    hipLaunchKernelGGL((ckpt_store_kernel<float, 1>), dim3((unsigned)cdiv(D, 256), groups),
-                       dim3(256), 0, stream, static_cast<const float*>(H), ldh, N, D, q, s);
-  else if (ldh % 2 == 0 && (uintptr_t)H % 4 == 0)
-    hipLaunchKernelGGL((ckpt_store_kernel<bf16raw, 2>), dim3((unsigned)cdiv(D, 512), groups),
-                       dim3(256), 0, stream, static_cast<const bf16raw*>(H), ldh, N, D, q, s);
-  else
-    hipLaunchKernelGGL((ckpt_store_kernel<bf16raw, 1>), dim3((unsigned)cdiv(D, 256), groups),
-                       dim3(256), 0, stream, static_cast<const bf16raw*>(H), ldh, N, D, q, s);
+  const dim3 grid((unsigned)cdiv(D, 256), (unsigned)groups_of(N)), block(256);
+  auto go = [&](auto kernel, auto* rows) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, rows, ldh, N, D, q, s);
+  };
+  auto typed = [&](auto* rows) {
+    typedef std::remove_const_t<std::remove_pointer_t<decltype(rows)>> T;
+    switch (columns_of(rows, ldh, N, D, dt)) {
+      case kApart: return go(ckpt_store_kernel<T, kApart>, rows);
+      case kNear: return go(ckpt_store_kernel<T, kNear>, rows);
+      case kNearOnce: return go(ckpt_store_kernel<T, kNearOnce>, rows);
+    }
+  };
+  dt == 0 ? typed(static_cast<const float*>(H)) : typed(static_cast<const bf16raw*>(H));
   return hipGetLastError();
 }
 
@@ -485,13 +573,19 @@ hipError_t launch_ckpt_load(const void* image, void* H, int64_t ldh, int64_t N, 
   const u32x4* q = static_cast<const u32x4*>(image);
   const float* s =
       reinterpret_cast<const float*>(static_cast<const char*>(image) + scales_at(N, D));
-  const dim3 grid((unsigned)cdiv(D, 256), (unsigned)groups_of(N));
-  if (dt == 0)
-    hipLaunchKernelGGL(ckpt_load_kernel<float>, grid, dim3(256), 0, stream, q, s,
-                       static_cast<float*>(H), ldh, N, D);
-  else
-    hipLaunchKernelGGL(ckpt_load_kernel<bf16raw>, grid, dim3(256), 0, stream, q, s,
-                       static_cast<bf16raw*>(H), ldh, N, D);
+  const dim3 grid((unsigned)cdiv(D, 256), (unsigned)groups_of(N)), block(256);
+  auto go = [&](auto kernel, auto* rows) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, q, s, rows, ldh, N, D);
+  };
+  auto typed = [&](auto* rows) {
+    typedef std::remove_pointer_t<decltype(rows)> T;
+    switch (columns_of(rows, ldh, N, D, dt)) {
+      case kApart: return go(ckpt_load_kernel<T, kApart>, rows);
+      case kNear: return go(ckpt_load_kernel<T, kNear>, rows);
+      case kNearOnce: return go(ckpt_load_kernel<T, kNearOnce>, rows);
+    }
+  };
+  dt == 0 ? typed(static_cast<float*>(H)) : typed(static_cast<bf16raw*>(H));
   return hipGetLastError();
 }
 
