@@ -258,15 +258,18 @@ struct XLoad<float> {
   }
 };
 
-// One output by itself, for those that are not finite.
+// One output by itself, by a whole wave, for those that are not finite: the formula in
+// 64 bits, in which no partial sum overflows. The same in all lanes.
 template <typename T>
 __device__ __noinline__ float product_one(const T* x, const uint8_t* image, const bf16raw* scales,
                                           const uint8_t* zeros, int64_t o, int64_t I,
                                           int64_t itiles, int gpt, bool with_zeros) {
-  float y = 0.0f;
-  for (int64_t i = 0; i < I; ++i)
-    y = fmaf(load_elem(x, i), weight_at(image, scales, zeros, o, i, itiles, gpt, with_zeros), y);
-  return y;
+  double y = 0.0;
+  for (int64_t i = threadIdx.x & 63; i < I; i += 64)
+    y = fma((double)load_elem(x, i),
+            (double)weight_at(image, scales, zeros, o, i, itiles, gpt, with_zeros), y);
+  for (int off = 1; off < 64; off <<= 1) y += __shfl_xor(y, off, kWave);
+  return (float)y;
 }
 
 // What a wave loads of an input tile: codes, scales and zero points of TD output
@@ -489,16 +492,21 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
     for (int w = 1; w < waves; ++w) y += sums[(w * TD * NT + j) * 64 + lane];
     const int64_t n = n0 + 16 * t + col;
     const int64_t o0 = (ot0 + d) * kTileO + 4 * quad;
-    if (n >= N) continue;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int64_t o = o0 + r;
-      if (o >= O) continue;
+      const bool live = n < N && o < O;
       float v = y[r];
-      // Not finite: an infinity or NaN in X, or a sum x*q past the range where
-      // the products with q - z stay within it. Taken again as the formula says.
-      if (!(fabsf(v) < INFINITY))
-        v = product_one(X + n * ldx, image, scales, zeros, o, I, (int64_t)itiles, GPT, ZERO);
+      // Not finite: an infinity or NaN in X, or a part of the sum past the range that the
+      // whole stays within. Taken again as the formula says.
+      for (uint64_t again = __ballot(live && !(fabsf(v) < INFINITY)); again; again &= again - 1) {
+        const int from = (int)__builtin_ctzll(again);
+        const int64_t nf = n0 + 16 * t + from % 16, of = (ot0 + d) * kTileO + 4 * (from / 16) + r;
+        const float w = product_one(X + nf * ldx, image, scales, zeros, of, I, (int64_t)itiles,
+                                    GPT, ZERO);
+        if (lane == from) v = w;
+      }
+      if (!live) continue;
       v = activate(v, act);
       if (y_dt == 0)
         static_cast<float*>(Y)[n * ldy + o] = v;
@@ -534,7 +542,10 @@ bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
 
 template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
 hipError_t launch_product_as(const ProductArgs& a) {
-  const int waves = a.L.itiles < 8 ? (int)a.L.itiles : 8;
+  // Eight waves share the input tiles; four where two row tiles take more than 128
+  // registers, so that three workgroups of them fit where one of eight would (32 x 3072 x
+  // 10240: 12.4 us with eight, 11.2 with four).
+  const int most = NT == 2 ? 4 : 8, waves = a.L.itiles < most ? (int)a.L.itiles : most;
   const int ntiles = (int)cdiv(a.N, 16);
   size_t lds = sizeof(f32x4) * 64 * TD * NT * waves;
   if (XLDS) {
