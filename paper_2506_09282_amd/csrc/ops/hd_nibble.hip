@@ -392,6 +392,13 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
     }
   };
   const bf16x8* xs = reinterpret_cast<const bf16x8*>(sums);
+  // The two chains of fp32 are joined when both are finished: begun from the other, the first
+  // would carry its size through every addition (1 x 561 x 10240: 4.3e-7 of the result
+  // instead of 2.7e-7). bf16 saves the addition.
+  constexpr bool APART = sizeof(T) == 4;
+  auto start = [](const Frag& f, int d, int g, int r, float one) {
+    return ZERO ? -(float)((f.zp[d][g] >> (8 * r)) & 255u) * one : one;
+  };
   auto multiply = [&](const Frag& f, const Operands& x, int it) {
 #pragma unroll
     for (int g = 0; g < GPT; ++g) {
@@ -418,7 +425,7 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            sum[t][r] = ZERO ? -(float)((f.zp[d][g] >> (8 * r)) & 255u) * one[t][r] : one[t][r];
+            sum[t][r] = APART ? 0.0f : start(f, d, g, r, one[t][r]);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
           const bf16x8 q = codes_bf16(f.code[d][g * STEPS + s]);
@@ -434,7 +441,10 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[d][t][r] = fmaf(sf[r], sum[t][r], acc[d][t][r]);
+          for (int r = 0; r < 4; ++r) {
+            const float v = APART ? sum[t][r] + start(f, d, g, r, one[t][r]) : sum[t][r];
+            acc[d][t][r] = fmaf(sf[r], v, acc[d][t][r]);
+          }
       }
     }
   };
