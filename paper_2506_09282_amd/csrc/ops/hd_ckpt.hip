@@ -40,7 +40,7 @@ __host__ __device__ inline int64_t scales_at(int64_t N, int64_t D) {
 // How a lane's four columns of 256 lie. Where rows start at multiples of 16 bytes (8 in
 // bf16) they are neighbours, in one load; elsewhere they are 64 apart and each load of a
 // wave is a run, which is faster than wide loads across the lines' ends (1999 x 4097
-// bf16 kept: 11.8 us wide, @@ so).
+// bf16 kept: 11.8 us wide, 9.4 so).
 // kNear, and past the caches (kStreamBytes) kNearOnce: rows pass once and do not stay there,
 // the kept values, a quarter or half as large, do.
 enum Columns { kApart, kNear, kNearOnce };
@@ -204,40 +204,33 @@ Columns columns_of(const void* rows, int64_t ld, int64_t N, int64_t D, int dt) {
 
 // ---- the other operand --------------------------------------------------------------
 
-// dS as operand fragments: [group][tile of 32 classes][8 rows of half a wave: p, j]
-// [part][lane][16 bytes]; lane l holds class l % 32, rows 32 p + 16 (l / 32) + 8 j + e.
-template <typename T>
-struct DsParts;
-template <>
-struct DsParts<float> {
-  static constexpr int kParts = 3;
-};
-template <>
-struct DsParts<bf16raw> {
-  static constexpr int kParts = 1;
-};
+// dS as operand fragments: [group][tile of 32 rows][8 rows of half a wave: p, j]
+// [part][lane][16 bytes]; lane l holds row l % 32 of the tile, samples 32 p + 16 (l / 32)
+// + 8 j + e. A row of the operand is a class; with few classes (FOLD) the three parts of
+// fp32 are rows of their own, [part][class], which fills the tiles better.
 constexpr int kSteps = kRows / 16;  // matrix steps of a group
 
-template <typename T>
+template <typename T, int P, bool FOLD>
 __global__ __launch_bounds__(256) void ckpt_grad_operand_kernel(const T* __restrict__ dS,
                                                                 int64_t lds, int64_t N, int K,
                                                                 int ktiles, int64_t total,
                                                                 u32x4* out) {
-  constexpr int P = DsParts<T>::kParts;
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= total) return;
   const int lane = (int)(at & 63), step = (int)(at >> 6) % kSteps;
   const int64_t bt = (at >> 6) / kSteps;
   const int kt = (int)(bt % ktiles);
   const int64_t b = bt / ktiles;
-  const int k = 32 * kt + lane % 32;
+  const int row = 32 * kt + lane % 32, k = FOLD ? row % K : row, part = FOLD ? row / K : 0;
+  const bool live = FOLD ? part < 3 : k < K;
   const int64_t n0 = b * kRows + 32 * (step / 2) + 16 * (lane / 32) + 8 * (step % 2);
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    v[e] = (k < K && n0 + e < N) ? load_elem(dS, (n0 + e) * lds + k) : 0.0f;
+    v[e] = (live && n0 + e < N) ? load_elem(dS, (n0 + e) * lds + k) : 0.0f;
+  u32x4 mine;
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
+  for (int p = 0; p < (FOLD ? 3 : P); ++p) {
     u32x4 w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -250,13 +243,18 @@ __global__ __launch_bounds__(256) void ckpt_grad_operand_kernel(const T* __restr
                          ? 0.0f
                          : v[2 * e + 1] - __uint_as_float(c & 0xffff0000u);
       // (a NaN whose upper half alone would read as an infinity)
-      if (P == 3 && p == 0) {
+      if (sizeof(T) == 4 && p == 0) {
         if ((a & 0x7fffffffu) > 0x7f800000u) w[e] |= 0x00000040u;
         if ((c & 0x7fffffffu) > 0x7f800000u) w[e] |= 0x00400000u;
       }
     }
-    out[((bt * kSteps + step) * P + p) * 64 + lane] = w;
+    if (FOLD) {
+      if (p == part || p == 0) mine = w;
+    } else {
+      out[((bt * kSteps + step) * P + p) * 64 + lane] = w;
+    }
   }
+  if (FOLD) out[(bt * kSteps + step) * 64 + lane] = mine;
 }
 
 // ---- the gradient -----------------------------------------------------------------
@@ -276,13 +274,15 @@ __device__ __forceinline__ bf16x8 bytes_bf16(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, v);
 }
 
+constexpr int kFoldRow = 33;  // floats of a row in LDS
+
 // W waves, each with DT tiles of 32 columns and KT tiles of 32 classes over a slice of the
 // groups; they share the dS operand of R groups at a time through LDS. The next loads (the
 // next group's kept values to registers, the next R operands on their way to the other
 // half of LDS) are in flight while one group is multiplied; they are issued without a
 // condition, past the end for the last group again, so that a wait covers only the
 // older ones.
-template <int P, int KT, int DT, int W, int R, bool STREAM>
+template <int P, int KT, int DT, int W, int R, bool FOLD, bool STREAM>
 __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
     const u32x4* __restrict__ q, const float* __restrict__ scale, const u32x4* __restrict__ ds,
     float* __restrict__ out, int64_t D, int K, int ktiles, int64_t groups, int64_t per_slice,
@@ -402,6 +402,27 @@ __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
   if (i < own) multiply(f[0], buf * R);
 
   float* dst = out + (int64_t)blockIdx.z * slice_stride;
+  if constexpr (FOLD) {  // a class is the sum of three rows
+    float* rows = reinterpret_cast<float*>(op) + wave * (KT * 32 * kFoldRow);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      __syncthreads();  // (the operand, or the tile before, is read)
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          rows[(32 * k + 8 * (r / 4) + 4 * half + r % 4) * kFoldRow + col] = acc[k][t][r];
+      __syncthreads();
+      for (int i = lane; i < 32 * K; i += 64) {
+        const int k = i / 32;
+        const int64_t d = d0 + 32 * t + i % 32;
+        const float* at = rows + k * kFoldRow + i % 32;
+        const float v = at[0] + at[K * kFoldRow] + at[2 * K * kFoldRow];
+        if (d < D) dst[k * D + d] = accumulate ? dst[k * D + d] + v : v;
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < KT; ++k)
 #pragma unroll
@@ -438,7 +459,9 @@ __global__ __launch_bounds__(256) void ckpt_grad_join_kernel(const float* __rest
 }
 
 struct GradPlan {
-  int ktiles, kt, dt, waves;  // class tiles; those and column tiles of a wave; waves
+  bool fold;                  // fp32's parts as rows of their own
+  int parts, ktiles;          // of a row's operand; tiles of 32 rows
+  int kt, dt, waves;          // row tiles and column tiles of a wave; waves
   int kblocks;                // workgroups along K
   int64_t dblocks, per_slice;
   int slices;
@@ -455,13 +478,18 @@ constexpr int dtiles_of(int kt) { return kt == 1 ? 2 : 1; }
 constexpr int round_of(int parts, int kt) { return parts * kt <= 6 ? 2 : 1; }
 
 GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
-  const int parts = dt == 0 ? DsParts<float>::kParts : DsParts<bf16raw>::kParts;
   GradPlan p;
-  p.ktiles = (int)cdiv(K, 32);
+  // Three rows for each class where that is one tile instead of three parts of one
+  // (65536 x 10240 x 10: 127 us instead of 151) or four tiles instead of six parts (32768 x
+  // 10240 x 40: 136 instead of 147); two tiles instead of three parts lose (K = 20: 170 instead
+  // of 160).
+  p.fold = dt == 0 && (K <= 10 || (K > 32 && K <= 42));
+  p.parts = dt == 0 && !p.fold ? 3 : 1;
+  p.ktiles = (int)cdiv(p.fold ? 3 * K : K, 32);
   // the classes of one workgroup: up to 128, which read the kept values once
   p.kt = p.ktiles < 4 ? p.ktiles : 4;
   p.dt = dtiles_of(p.kt);
-  p.waves = waves_of(parts);
+  p.waves = waves_of(p.parts);
   p.kblocks = (int)cdiv(p.ktiles, p.kt);
   p.dblocks = cdiv(D, p.waves * 32 * p.dt);
   // Two workgroups for each compute unit; a slice of at least four groups, since its
@@ -472,20 +500,21 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
   if (slices < 1) slices = 1;
   p.per_slice = cdiv(groups, slices);
   p.slices = (int)cdiv(groups, p.per_slice);
-  p.operand = (size_t)groups * p.ktiles * kSteps * parts * 1024;
+  p.operand = (size_t)groups * p.ktiles * kSteps * p.parts * 1024;
   p.total = p.operand + (p.slices > 1 ? (size_t)p.slices * K * D * 4 : 0);
   return p;
 }
 
 constexpr int64_t kStreamKept = int64_t(192) << 20;
 
-template <typename T, int KT, bool STREAM>
+template <int P, int KT, bool FOLD, bool STREAM>
 hipError_t launch_grad_as(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
                           float* out, int64_t D, int K, int64_t groups, bool accumulate,
                           hipStream_t stream) {
-  constexpr int P = DsParts<T>::kParts, W = waves_of(P), R = round_of(P, KT);
-  constexpr int lds = 2 * R * KT * kSteps * P * 1024;
-  const auto kernel = ckpt_class_grad_kernel<P, KT, dtiles_of(KT), W, R, STREAM>;
+  constexpr int W = waves_of(P), R = round_of(P, KT);
+  constexpr int op_lds = 2 * R * KT * kSteps * P * 1024, fold_lds = W * KT * 32 * kFoldRow * 4;
+  constexpr int lds = FOLD && fold_lds > op_lds ? fold_lds : op_lds;
+  const auto kernel = ckpt_class_grad_kernel<P, KT, dtiles_of(KT), W, R, FOLD, STREAM>;
   if (lds > 64 * 1024) {  // above the default limit: raised once per device and kernel
     static PerDeviceOnce once;
     const hipError_t e = once_per_device(once, [&] {
@@ -500,23 +529,14 @@ hipError_t launch_grad_as(const GradPlan& p, const u32x4* q, const float* s, con
   return hipGetLastError();
 }
 
-template <typename T>
+template <int P, int KT, bool FOLD = false>
 hipError_t launch_grad_kernel(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
                               float* out, int64_t D, int K, int64_t groups, bool accumulate,
                               hipStream_t stream) {
   // kept values past the caches, and read by one workgroup each
-  const bool by = groups * kRows * D > kStreamKept && p.kblocks == 1;
-  auto go = [&](auto launch) { return launch(p, q, s, ds, out, D, K, groups, accumulate, stream); };
-  switch (p.kt) {
-    case 1:
-      return by ? go(launch_grad_as<T, 1, true>) : go(launch_grad_as<T, 1, false>);
-    case 2:
-      return by ? go(launch_grad_as<T, 2, true>) : go(launch_grad_as<T, 2, false>);
-    case 3:
-      return by ? go(launch_grad_as<T, 3, true>) : go(launch_grad_as<T, 3, false>);
-    default:
-      return by ? go(launch_grad_as<T, 4, true>) : go(launch_grad_as<T, 4, false>);
-  }
+  if (groups * kRows * D > kStreamKept && p.kblocks == 1)
+    return launch_grad_as<P, KT, FOLD, true>(p, q, s, ds, out, D, K, groups, accumulate, stream);
+  return launch_grad_as<P, KT, FOLD, false>(p, q, s, ds, out, D, K, groups, accumulate, stream);
 }
 
 template <typename T>
@@ -527,15 +547,38 @@ hipError_t launch_grad_typed(const void* dS, int64_t lds, const void* image, flo
   u32x4* operand = static_cast<u32x4*>(workspace);
   float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.operand);
   const int64_t total = groups * p.ktiles * kSteps * 64;
-  hipLaunchKernelGGL(ckpt_grad_operand_kernel<T>, dim3((unsigned)cdiv(total, 256)), dim3(256), 0,
-                     stream, static_cast<const T*>(dS), lds, N, (int)K, p.ktiles, total, operand);
+  auto lay_out = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(total, 256)), dim3(256), 0, stream,
+                       static_cast<const T*>(dS), lds, N, (int)K, p.ktiles, total, operand);
+  };
+  if constexpr (sizeof(T) == 4)
+    p.fold ? lay_out(ckpt_grad_operand_kernel<T, 1, true>)
+           : lay_out(ckpt_grad_operand_kernel<T, 3, false>);
+  else
+    lay_out(ckpt_grad_operand_kernel<T, 1, false>);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const u32x4* q = static_cast<const u32x4*>(image);
   const float* s =
       reinterpret_cast<const float*>(static_cast<const char*>(image) + scales_at(N, D));
   float* out = p.slices > 1 ? part : dC;
-  e = launch_grad_kernel<T>(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
+  auto go = [&](auto launch) {
+    return launch(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
+  };
+  if constexpr (sizeof(T) == 4) {
+    if (p.fold)
+      e = p.kt == 1 ? go(launch_grad_kernel<1, 1, true>) : go(launch_grad_kernel<1, 4, true>);
+    else
+      e = p.kt == 1   ? go(launch_grad_kernel<3, 1>)
+          : p.kt == 2 ? go(launch_grad_kernel<3, 2>)
+          : p.kt == 3 ? go(launch_grad_kernel<3, 3>)
+                      : go(launch_grad_kernel<3, 4>);
+  } else {
+    e = p.kt == 1   ? go(launch_grad_kernel<1, 1>)
+        : p.kt == 2 ? go(launch_grad_kernel<1, 2>)
+        : p.kt == 3 ? go(launch_grad_kernel<1, 3>)
+                    : go(launch_grad_kernel<1, 4>);
+  }
   if (e != hipSuccess || p.slices == 1) return e;
   hipLaunchKernelGGL(ckpt_grad_join_kernel, dim3((unsigned)cdiv(K * D, 256)), dim3(256), 0, stream,
                      part, dC, K * D, p.slices, (int)accumulate);

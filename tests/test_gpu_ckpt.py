@@ -136,6 +136,26 @@ def test_class_grad_exact_on_integers(N, D, K, dtype):
     assert torch.equal(got.cpu().double(), dS.double().t() @ H.double())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("K", [1, 2, 6, 10, 11, 16, 21, 22, 31, 32, 33, 42, 43, 64, 65, 96, 97, 129])
+def test_class_grad_every_count_of_classes(K, dtype):
+    """Each layout of the classes in tiles, exact on integers."""
+    hd = hd_gpu()
+    N, D = 700, 300
+    g = torch.Generator().manual_seed(K)
+    H = torch.where(torch.randn(N, D, generator=g) > 0, 127.0, -127.0)
+    dS = torch.randint(-3, 4, (N, K), generator=g).to(dtype)
+    dS[5:9] *= 0.015625  # (and parts of dS beyond the first eight bits)
+    dS[5:9] += 3.0
+    ref = dS.double().t() @ H.double()
+    kept = hd.ckpt_store(H.cuda())
+    got = hd.ckpt_class_grad(dS.cuda(), kept)
+    assert torch.equal(got.cpu().double(), ref)
+    acc = torch.ones(K, D, device="cuda")
+    hd.ckpt_class_grad(dS.cuda(), kept, out=acc, accumulate=True)
+    assert torch.equal(acc.cpu().double(), ref + 1.0)
+
+
 def test_fp32_gradients_in_full():
     """Every bit of an fp32 dS counts: one row, one group, q s = 1."""
     hd = hd_gpu()
