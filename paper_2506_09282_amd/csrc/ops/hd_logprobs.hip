@@ -354,6 +354,52 @@ struct Flight {
   }
 };
 
+// The value of the next lane (any in lane 63).
+__device__ __forceinline__ uint32_t lane_next(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x130, 0xf, 0xf, true);
+}
+
+// A whole wave's chunks, neighbours in memory, whose row starts between two words (bf16 rows of
+// odd length, masks of any): loads at the words before, which are as fast as aligned ones,
+// then each lane moves its words up and takes what is missing from the next lane; lane 63
+// loads its last values by themselves. `up` and `mup` are how many bytes before.
+template <typename T, bool MASK, bool STREAM>
+struct WaveFlight {
+  Flight<T, MASK, STREAM> f;
+  uint32_t last, mlast;  // lane 63's
+  __device__ __forceinline__ void load(const T* p, const uint8_t* mp, uint32_t up, uint32_t mup,
+                                       int lane) {
+    constexpr int LEN = Chunk<T>::kLen;
+    typedef uint32_t m_a __attribute__((aligned(1)));
+    f.load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) - up),
+           MASK ? mp - mup : nullptr);
+    if (up | mup) {
+      if (lane == 63) {
+        if (sizeof(T) == 2) last = reinterpret_cast<const bf16raw*>(p)[LEN - 1];
+        if (MASK) mlast = *reinterpret_cast<const m_a*>(mp + LEN - 4);
+      }
+    }
+  }
+  __device__ __forceinline__ void settle(uint32_t up, uint32_t mup, int lane) {
+    if (!(up | mup)) return;
+    if constexpr (sizeof(T) == 2) {
+      uint32_t next = lane_next(f.w[0]);
+      next = lane == 63 ? last : next;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        f.w[e] = __builtin_amdgcn_alignbyte(e < 3 ? f.w[e + 1] : next, f.w[e], up);
+    }
+    if constexpr (MASK) {
+      constexpr int M = Chunk<T>::kLen / 4;
+      const uint32_t next = lane_next(f.m[0]);
+#pragma unroll
+      for (int e = 0; e < M; ++e)
+        f.m[e] = __builtin_amdgcn_alignbyte(e < M - 1 ? f.m[e + 1] : next, f.m[e], mup);
+      if (lane == 63) f.m[M - 1] = mlast;
+    }
+  }
+};
+
 // Joins the waves' statistics and lists of a workgroup; the result is whole in wave 0.
 template <bool TOP, int WAVES>
 __device__ __forceinline__ void join_waves(Stats& st, uint64_t& list, float c, int lane, int wave,
@@ -469,12 +515,17 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
   // Whole steps, the next one's loads in flight while one is worked on (past the end the
   // last one's again, so that they need no condition), then the step that ends inside. Steps
   // are counted from the row's start wherever it lies, so that a result does not depend
-  // on alignment (rows of odd length cost a fifth for it: 2048 x 100003 bf16 96 us,
-  // 2048 x 100096 79). Classes come in ascending order, so that of equal scores the
+  // on alignment. Classes come in ascending order, so that of equal scores the
   // one already listed is the lower class.
   const int64_t k_begin = part * sp.part_len, whole = (k_end - k_begin) / STEP;
   const int64_t steps = cdiv(k_end - k_begin, STEP);
-  Flight<T, MASK, STREAM> flight[kChunks];
+  // (a row's first word may begin before it where a row is before it)
+  const bool inside = n > 0 || part > 0;
+  const uint32_t up = sizeof(T) == 2 && inside ? (uint32_t)((uintptr_t)(row + k_begin) & 2) : 0;
+  const uint32_t mup = MASK && (part > 0 || (n > 0 && a.ldm > 0))
+                           ? (uint32_t)((uintptr_t)(mrow + k_begin) & 3)
+                           : 0;
+  WaveFlight<T, MASK, STREAM> flight[kChunks];
   auto place = [&](int64_t i, int u) {
     return k_begin + i * STEP + u * ROUND + (int64_t)threadIdx.x * LEN;
   };
@@ -482,7 +533,7 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
 #pragma unroll
     for (int u = 0; u < kChunks; ++u) {
       const int64_t k = place(i < whole ? i : whole - 1, u);
-      flight[u].load(row + k, MASK ? mrow + k : nullptr);
+      flight[u].load(row + k, MASK ? mrow + k : nullptr, up, mup, lane);
     }
   };
   if (whole > 0) fetch(0);
@@ -490,7 +541,10 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     float v[VALS];
     if (i < whole) {
 #pragma unroll
-      for (int u = 0; u < kChunks; ++u) flight[u].scores(v + u * LEN);
+      for (int u = 0; u < kChunks; ++u) {
+        flight[u].settle(up, mup, lane);
+        flight[u].f.scores(v + u * LEN);
+      }
       fetch(i + 1);
       __builtin_amdgcn_sched_barrier(0);  // (or the loads sink below the work)
     } else {
@@ -498,8 +552,8 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       for (int u = 0; u < kChunks; ++u) {
         const int64_t k = place(i, u);
         if (k + LEN <= k_end) {
-          flight[u].load(row + k, MASK ? mrow + k : nullptr);
-          flight[u].scores(v + u * LEN);
+          flight[u].f.load(row + k, MASK ? mrow + k : nullptr);
+          flight[u].f.scores(v + u * LEN);
         } else {
 #pragma unroll
           for (int e = 0; e < LEN; ++e) {
