@@ -411,8 +411,8 @@ hd_status hd_logprobs_grad(const void *scores, int64_t ld, const uint8_t *mask, 
  * checkpoint of H:
  *   dC[k][d] = sum_n dS[n][k] * (q s)[n][d]      fp32 [K][D], contiguous;
  * accumulate != 0 adds to what dC holds. Products are exact, sums fp32.
- * workspace: hd_ckpt_class_grad_workspace_bytes(...) bytes, contents irrelevant
- * before and undefined after the call.
+ * workspace: hd_ckpt_class_grad_workspace_bytes(...) bytes (0 is possible), contents
+ * irrelevant before and undefined after the call.
  * Limits: N <= 65535 * 64, D <= 2^30, K <= 2^20, and ceil(N/64) * ceil(K/32) < 2^23.
  */
 size_t hd_ckpt_bytes(int64_t N, int64_t D);

@@ -865,8 +865,9 @@ def ckpt_class_grad(dS, kept: Checkpoint, out=None, accumulate: bool = False):
         if out.dtype != torch.float32 or out.shape != (K, D) or out.get_device() != index:
             raise ValueError("out must be float32 [K, D] on dS's device")
     need = _need("hd_ckpt_class_grad_workspace_bytes", index, N, D, K, dt)
-    ws = torch.empty(need, dtype=torch.uint8, device=dS.device)
+    ws = torch.empty(need, dtype=torch.uint8, device=dS.device) if need else None
     st = lib().hd_ckpt_class_grad(dS.data_ptr(), ld, image.data_ptr(), out.data_ptr(), N, D, K,
-                                  dt, accumulate, ws.data_ptr(), need, _raw_stream(index))
+                                  dt, accumulate, ws.data_ptr() if need else None, need,
+                                  _raw_stream(index))
     _raise(st, "hd_ckpt_class_grad")
     return out

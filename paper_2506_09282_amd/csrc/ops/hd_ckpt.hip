@@ -17,7 +17,8 @@
 // [group][column]. A lane's 16-byte load is 16 rows of a column, half an operand pair of
 // v_mfma_f32_32x32x16_bf16, neighbouring lanes are neighbouring columns, and
 // storing is coalesced too. dS is first cut and laid out as the other
-// operand (a small launch), so that the product's loop holds no transposition.
+// operand (a small launch), so that the product's loop holds no transposition; in a short
+// call each workgroup does that for itself.
 #include <type_traits>
 
 #include "hd_ops.hpp"
@@ -210,25 +211,9 @@ Columns columns_of(const void* rows, int64_t ld, int64_t N, int64_t D, int dt) {
 // fp32 are rows of their own, [part][class], which fills the tiles better.
 constexpr int kSteps = kRows / 16;  // matrix steps of a group
 
+// Eight values as P parts of an operand, or (FOLD) as the one part `part` (past 2: none).
 template <typename T, int P, bool FOLD>
-__global__ __launch_bounds__(256) void ckpt_grad_operand_kernel(const T* __restrict__ dS,
-                                                                int64_t lds, int64_t N, int K,
-                                                                int ktiles, int64_t total,
-                                                                u32x4* out) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const int lane = (int)(at & 63), step = (int)(at >> 6) % kSteps;
-  const int64_t bt = (at >> 6) / kSteps;
-  const int kt = (int)(bt % ktiles);
-  const int64_t b = bt / ktiles;
-  const int row = 32 * kt + lane % 32, k = FOLD ? row % K : row, part = FOLD ? row / K : 0;
-  const bool live = FOLD ? part < 3 : k < K;
-  const int64_t n0 = b * kRows + 32 * (step / 2) + 16 * (lane / 32) + 8 * (step % 2);
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    v[e] = (live && n0 + e < N) ? load_elem(dS, (n0 + e) * lds + k) : 0.0f;
-  u32x4 mine;
+__device__ __forceinline__ void cut(float (&v)[8], int part, u32x4 (&out)[P]) {
 #pragma unroll
   for (int p = 0; p < (FOLD ? 3 : P); ++p) {
     u32x4 w;
@@ -248,13 +233,44 @@ __global__ __launch_bounds__(256) void ckpt_grad_operand_kernel(const T* __restr
         if ((c & 0x7fffffffu) > 0x7f800000u) w[e] |= 0x00400000u;
       }
     }
-    if (FOLD) {
-      if (p == part || p == 0) mine = w;
-    } else {
-      out[((bt * kSteps + step) * P + p) * 64 + lane] = w;
-    }
+    if (!FOLD)
+      out[p] = w;
+    else if (p == part || p == 0)
+      out[0] = w;
   }
-  if (FOLD) out[(bt * kSteps + step) * 64 + lane] = mine;
+}
+
+// Where a lane's fragment comes from: its class (K: none), part and first sample.
+struct Source {
+  int k, part, n0;  // n0 within the group
+};
+template <bool FOLD>
+__device__ __forceinline__ Source source_of(int kt, int step, int lane, int K) {
+  const int row = 32 * kt + lane % 32;
+  const int n0 = 32 * (step / 2) + 16 * (lane / 32) + 8 * (step % 2);
+  if (FOLD) return {row < 3 * K ? row % K : K, row / K, n0};
+  return {row < K ? row : K, 0, n0};
+}
+
+template <typename T, int P, bool FOLD>
+__global__ __launch_bounds__(256) void ckpt_grad_operand_kernel(const T* __restrict__ dS,
+                                                                int64_t lds, int64_t N, int K,
+                                                                int ktiles, int64_t total,
+                                                                u32x4* out) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  const int lane = (int)(at & 63), step = (int)(at >> 6) % kSteps;
+  const int64_t bt = (at >> 6) / kSteps;
+  const Source from = source_of<FOLD>((int)(bt % ktiles), step, lane, K);
+  const int64_t n0 = bt / ktiles * kRows + from.n0;
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    v[e] = (from.k < K && n0 + e < N) ? load_elem(dS, (n0 + e) * lds + from.k) : 0.0f;
+  u32x4 w[P];
+  cut<T, P, FOLD>(v, from.part, w);
+#pragma unroll
+  for (int p = 0; p < P; ++p) out[((bt * kSteps + step) * P + p) * 64 + lane] = w[p];
 }
 
 // ---- the gradient -----------------------------------------------------------------
@@ -282,13 +298,18 @@ constexpr int kFoldRow = 33;  // floats of a row in LDS
 // half of LDS) are in flight while one group is multiplied; they are issued without a
 // condition, past the end for the last group again, so that a wait covers only the
 // older ones.
-template <int P, int KT, int DT, int W, int R, bool FOLD, bool STREAM>
+// T is u32x4 where dS has been laid out, else the type of dS's rows, which the workgroup
+// then cuts by itself.
+template <typename T, int P, int KT, int DT, int W, int R, bool FOLD, bool STREAM>
 __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
-    const u32x4* __restrict__ q, const float* __restrict__ scale, const u32x4* __restrict__ ds,
-    float* __restrict__ out, int64_t D, int K, int ktiles, int64_t groups, int64_t per_slice,
-    int64_t slice_stride, int accumulate) {
+    const u32x4* __restrict__ q, const float* __restrict__ scale, const T* __restrict__ ds,
+    int64_t lds, int64_t N, float* __restrict__ out, int64_t D, int K, int ktiles, int64_t groups,
+    int64_t per_slice, int64_t slice_stride, int accumulate) {
+  constexpr bool ROWS = sizeof(T) < 16;
   constexpr int FRAGS = KT * kSteps * P * 64;  // 16-byte fragments of a group's operand
-  constexpr int THREADS = 64 * W, PER = (R * FRAGS + THREADS - 1) / THREADS;
+  // fragments that a thread brings: whole ones, or all parts of PER of them
+  constexpr int THREADS = 64 * W, BRING = R * FRAGS / (ROWS ? P : 1);
+  constexpr int PER = (BRING + THREADS - 1) / THREADS;
   extern __shared__ u32x4 op[];  // [2][R][FRAGS]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, half = lane >> 5;
@@ -314,7 +335,8 @@ __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
     u32x4 w[DT][2];
     float s[DT];
   };
-  u32x4 stage[PER];
+  u32x4 stage[ROWS ? 1 : PER];
+  T raw[ROWS ? PER : 1][8];
   auto group = [&](int i) { return b0 + (i < own ? i : own - 1); };
   auto fetch = [&](int64_t b, Kept& f) {
 #pragma unroll
@@ -331,20 +353,44 @@ __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       int at = threadIdx.x + THREADS * i;
-      if (R * FRAGS % THREADS != 0 && at >= R * FRAGS) at = R * FRAGS - 1;
-      const int64_t b = group(i0 + at / FRAGS);
-      at %= FRAGS;
-      // class tiles past the last repeat it (their results are not written)
-      const int k = at / (kSteps * P * 64);
-      const int kt = kt0 + k < ktiles ? kt0 + k : ktiles - 1;
-      stage[i] = ds[(b * ktiles + kt) * (kSteps * P * 64) + at % (kSteps * P * 64)];
+      if (BRING % THREADS != 0 && at >= BRING) at = BRING - 1;
+      const int64_t b = group(i0 + at / (BRING / R));
+      at %= BRING / R;
+      if constexpr (ROWS) {
+        const Source from = source_of<FOLD>(kt0 + at / (kSteps * 64), at / 64 % kSteps, at % 64, K);
+        const T* col = ds + (from.k < K ? from.k : 0);
+        const int64_t n0 = b * kRows + from.n0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[i][e] = col[(n0 + e < N ? n0 + e : N - 1) * lds];
+      } else {
+        // class tiles past the last repeat it (their results are not written)
+        const int k = at / (kSteps * P * 64);
+        const int kt = kt0 + k < ktiles ? kt0 + k : ktiles - 1;
+        stage[i] = ds[(b * ktiles + kt) * (kSteps * P * 64) + at % (kSteps * P * 64)];
+      }
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](int buf, int i0) {  // what fetch_op(i0) brought
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int at = threadIdx.x + THREADS * i;
-      if (R * FRAGS % THREADS == 0 || at < R * FRAGS) op[buf * (R * FRAGS) + at] = stage[i];
+      if (BRING % THREADS != 0 && at >= BRING) continue;
+      if constexpr (ROWS) {
+        const int part_of = at % (BRING / R);
+        const Source from =
+            source_of<FOLD>(kt0 + part_of / (kSteps * 64), part_of / 64 % kSteps, part_of % 64, K);
+        const int64_t n0 = group(i0 + at / (BRING / R)) * kRows + from.n0;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = from.k < K && n0 + e < N ? load_elem(&raw[i][e], 0) : 0.0f;
+        u32x4 w[P];
+        cut<T, P, FOLD>(v, from.part, w);
+#pragma unroll
+        for (int p = 0; p < P; ++p) op[buf * (R * FRAGS) + (at / 64 * P + p) * 64 + at % 64] = w[p];
+      } else {
+        op[buf * (R * FRAGS) + at] = stage[i];
+      }
     }
   };
   auto multiply = [&](const Kept& f, int buf) {
@@ -380,7 +426,7 @@ __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
   Kept f[2];
   fetch_op(0);
   fetch(group(0), f[0]);
-  put(0);
+  put(0, 0);
   __syncthreads();
   int i = 0, buf = 0;
   for (; i + 2 <= own; i += 2) {
@@ -394,7 +440,7 @@ __global__ __launch_bounds__(64 * W, 2) void ckpt_class_grad_kernel(
       __builtin_amdgcn_sched_barrier(0);
       if (r % R == R - 1) {
         buf ^= 1;
-        put(buf);
+        put(buf, i + r + 1);
         __syncthreads();
       }
     }
@@ -459,6 +505,7 @@ __global__ __launch_bounds__(256) void ckpt_grad_join_kernel(const float* __rest
 }
 
 struct GradPlan {
+  bool rows;                  // dS as it is, not laid out first
   bool fold;                  // fp32's parts as rows of their own
   int parts, ktiles;          // of a row's operand; tiles of 32 rows
   int kt, dt, waves;          // row tiles and column tiles of a wave; waves
@@ -477,6 +524,9 @@ constexpr int dtiles_of(int kt) { return kt == 1 ? 2 : 1; }
 // Groups between two barriers: two where the operand's halves fit LDS.
 constexpr int round_of(int parts, int kt) { return parts * kt <= 6 ? 2 : 1; }
 
+// Values up to which a workgroup cuts dS by itself (see grad_plan).
+constexpr int64_t kRowsParts = int64_t(32) << 20, kRowsFold = int64_t(16) << 20;
+
 GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
   GradPlan p;
   // Three rows for each class where that is one tile instead of three parts of one
@@ -484,6 +534,12 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
   // 10240 x 40: 136 instead of 147); two tiles instead of three parts lose (K = 20: 170 instead
   // of 160).
   p.fold = dt == 0 && (K <= 10 || (K > 32 && K <= 42));
+  // A short call saves the launch that lays dS out; each workgroup then cuts all classes of its
+  // groups by itself, which pays while there are few (K = 26, D = 10000, fp32: 1000 rows 15.0
+  // us instead of 16.3, 4096 rows 27.1 either way, 65536 182 instead of 167; bf16: 300
+  // rows 8.7 instead of 10.6; K = 6: 1000 rows 11.7 instead of 14.1, 2000 14.7 instead of
+  // 14.2). Two class tiles are too many loads for it (2999 x 10000 x 60 bf16: 24 instead of 21).
+  p.rows = K <= 32 && N * D <= (p.fold ? kRowsFold : kRowsParts);
   p.parts = dt == 0 && !p.fold ? 3 : 1;
   p.ktiles = (int)cdiv(p.fold ? 3 * K : K, 32);
   // the classes of one workgroup: up to 128, which read the kept values once
@@ -500,21 +556,32 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
   if (slices < 1) slices = 1;
   p.per_slice = cdiv(groups, slices);
   p.slices = (int)cdiv(groups, p.per_slice);
-  p.operand = (size_t)groups * p.ktiles * kSteps * p.parts * 1024;
+  p.operand = p.rows ? 0 : (size_t)groups * p.ktiles * kSteps * p.parts * 1024;
   p.total = p.operand + (p.slices > 1 ? (size_t)p.slices * K * D * 4 : 0);
   return p;
 }
 
 constexpr int64_t kStreamKept = int64_t(192) << 20;
 
-template <int P, int KT, bool FOLD, bool STREAM>
-hipError_t launch_grad_as(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
-                          float* out, int64_t D, int K, int64_t groups, bool accumulate,
-                          hipStream_t stream) {
+struct GradArgs {
+  const void* dS;
+  int64_t lds;
+  const u32x4* q;
+  const float* scale;
+  const u32x4* operand;  // dS laid out
+  float* out;
+  int64_t N, D;
+  int K;
+  bool accumulate;
+  hipStream_t stream;
+};
+
+template <typename T, int P, int KT, bool FOLD, bool STREAM>
+hipError_t launch_grad_as(const GradPlan& p, const GradArgs& a, const T* ds) {
   constexpr int W = waves_of(P), R = round_of(P, KT);
   constexpr int op_lds = 2 * R * KT * kSteps * P * 1024, fold_lds = W * KT * 32 * kFoldRow * 4;
   constexpr int lds = FOLD && fold_lds > op_lds ? fold_lds : op_lds;
-  const auto kernel = ckpt_class_grad_kernel<P, KT, dtiles_of(KT), W, R, FOLD, STREAM>;
+  const auto kernel = ckpt_class_grad_kernel<T, P, KT, dtiles_of(KT), W, R, FOLD, STREAM>;
   if (lds > 64 * 1024) {  // above the default limit: raised once per device and kernel
     static PerDeviceOnce once;
     const hipError_t e = once_per_device(once, [&] {
@@ -524,60 +591,61 @@ hipError_t launch_grad_as(const GradPlan& p, const u32x4* q, const float* s, con
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.dblocks, (unsigned)p.kblocks, (unsigned)p.slices),
-                     dim3(64 * W), lds, stream, q, s, ds, out, D, K, p.ktiles, groups,
-                     p.per_slice, (int64_t)K * D, (int)(accumulate && p.slices == 1));
+                     dim3(64 * W), lds, a.stream, a.q, a.scale, ds, a.lds, a.N, a.out, a.D, a.K,
+                     p.ktiles, groups_of(a.N), p.per_slice, (int64_t)a.K * a.D,
+                     (int)(a.accumulate && p.slices == 1));
   return hipGetLastError();
 }
 
-template <int P, int KT, bool FOLD = false>
-hipError_t launch_grad_kernel(const GradPlan& p, const u32x4* q, const float* s, const u32x4* ds,
-                              float* out, int64_t D, int K, int64_t groups, bool accumulate,
-                              hipStream_t stream) {
+template <typename T, int P, int KT, bool FOLD>
+hipError_t launch_grad_kernel(const GradPlan& p, const GradArgs& a) {
+  if constexpr (KT == 1)
+    if (p.rows) return launch_grad_as<T, P, KT, FOLD, false>(p, a, static_cast<const T*>(a.dS));
   // kept values past the caches, and read by one workgroup each
-  if (groups * kRows * D > kStreamKept && p.kblocks == 1)
-    return launch_grad_as<P, KT, FOLD, true>(p, q, s, ds, out, D, K, groups, accumulate, stream);
-  return launch_grad_as<P, KT, FOLD, false>(p, q, s, ds, out, D, K, groups, accumulate, stream);
+  if (groups_of(a.N) * kRows * a.D > kStreamKept && p.kblocks == 1)
+    return launch_grad_as<u32x4, P, KT, FOLD, true>(p, a, a.operand);
+  return launch_grad_as<u32x4, P, KT, FOLD, false>(p, a, a.operand);
 }
 
 template <typename T>
 hipError_t launch_grad_typed(const void* dS, int64_t lds, const void* image, float* dC, int64_t N,
                              int64_t D, int64_t K, bool accumulate, const GradPlan& p,
                              void* workspace, hipStream_t stream) {
-  const int64_t groups = groups_of(N);
   u32x4* operand = static_cast<u32x4*>(workspace);
   float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.operand);
-  const int64_t total = groups * p.ktiles * kSteps * 64;
-  auto lay_out = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(total, 256)), dim3(256), 0, stream,
-                       static_cast<const T*>(dS), lds, N, (int)K, p.ktiles, total, operand);
-  };
-  if constexpr (sizeof(T) == 4)
-    p.fold ? lay_out(ckpt_grad_operand_kernel<T, 1, true>)
-           : lay_out(ckpt_grad_operand_kernel<T, 3, false>);
-  else
-    lay_out(ckpt_grad_operand_kernel<T, 1, false>);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const u32x4* q = static_cast<const u32x4*>(image);
-  const float* s =
-      reinterpret_cast<const float*>(static_cast<const char*>(image) + scales_at(N, D));
-  float* out = p.slices > 1 ? part : dC;
-  auto go = [&](auto launch) {
-    return launch(p, q, s, operand, out, D, (int)K, groups, accumulate, stream);
-  };
+  hipError_t e;
+  if (!p.rows) {
+    const int64_t total = groups_of(N) * p.ktiles * kSteps * 64;
+    auto lay_out = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(total, 256)), dim3(256), 0, stream,
+                         static_cast<const T*>(dS), lds, N, (int)K, p.ktiles, total, operand);
+    };
+    if constexpr (sizeof(T) == 4)
+      p.fold ? lay_out(ckpt_grad_operand_kernel<T, 1, true>)
+             : lay_out(ckpt_grad_operand_kernel<T, 3, false>);
+    else
+      lay_out(ckpt_grad_operand_kernel<T, 1, false>);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const GradArgs a{dS, lds, static_cast<const u32x4*>(image),
+                   reinterpret_cast<const float*>(static_cast<const char*>(image) +
+                                                  scales_at(N, D)),
+                   operand, p.slices > 1 ? part : dC, N, D, (int)K, accumulate, stream};
   if constexpr (sizeof(T) == 4) {
     if (p.fold)
-      e = p.kt == 1 ? go(launch_grad_kernel<1, 1, true>) : go(launch_grad_kernel<1, 4, true>);
+      e = p.kt == 1 ? launch_grad_kernel<T, 1, 1, true>(p, a)
+                    : launch_grad_kernel<T, 1, 4, true>(p, a);
     else
-      e = p.kt == 1   ? go(launch_grad_kernel<3, 1>)
-          : p.kt == 2 ? go(launch_grad_kernel<3, 2>)
-          : p.kt == 3 ? go(launch_grad_kernel<3, 3>)
-                      : go(launch_grad_kernel<3, 4>);
+      e = p.kt == 1   ? launch_grad_kernel<T, 3, 1, false>(p, a)
+          : p.kt == 2 ? launch_grad_kernel<T, 3, 2, false>(p, a)
+          : p.kt == 3 ? launch_grad_kernel<T, 3, 3, false>(p, a)
+                      : launch_grad_kernel<T, 3, 4, false>(p, a);
   } else {
-    e = p.kt == 1   ? go(launch_grad_kernel<1, 1>)
-        : p.kt == 2 ? go(launch_grad_kernel<1, 2>)
-        : p.kt == 3 ? go(launch_grad_kernel<1, 3>)
-                    : go(launch_grad_kernel<1, 4>);
+    e = p.kt == 1   ? launch_grad_kernel<T, 1, 1, false>(p, a)
+        : p.kt == 2 ? launch_grad_kernel<T, 1, 2, false>(p, a)
+        : p.kt == 3 ? launch_grad_kernel<T, 1, 3, false>(p, a)
+                    : launch_grad_kernel<T, 1, 4, false>(p, a);
   }
   if (e != hipSuccess || p.slices == 1) return e;
   hipLaunchKernelGGL(ckpt_grad_join_kernel, dim3((unsigned)cdiv(K * D, 256)), dim3(256), 0, stream,

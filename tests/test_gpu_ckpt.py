@@ -168,6 +168,56 @@ def test_fp32_gradients_in_full():
     assert bool(((got.double() - ref).abs() <= 2 * P.U32 * ref.abs()).all())
 
 
+@pytest.mark.parametrize("K", [3, 26])
+def test_fp32_gradients_of_few_classes_in_full(K):
+    """As above, where the workgroups cut dS by themselves."""
+    hd = hd_gpu()
+    H = torch.full((1, 40), 127.0)
+    dS = torch.randn(1, K, generator=torch.Generator().manual_seed(2))
+    dS[0, 0], dS[0, 1], dS[0, 2] = 1.0 + 2.0 ** -23, 16777215.0, -1e-30
+    got = hd.ckpt_class_grad(dS.cuda(), hd.ckpt_store(H.cuda())).cpu()
+    ref = dS.double().t() * 127.0
+    assert bool(((got.double() - ref).abs() <= 2 * P.U32 * ref.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("K", [6, 26])
+def test_class_grad_short_and_long_calls_agree(K, dtype):
+    """Few classes: a long call lays dS out first, a short one does not. Exact on integers."""
+    hd = hd_gpu()
+    N, D = 4300, 8200
+    announce(f"class grad {N}x{D}x{K} {dtype}")
+    g = torch.Generator().manual_seed(K)
+    H = torch.where(torch.randn(N, D, generator=g) > 0, 127.0, -127.0).cuda()
+    dS = torch.randint(-3, 4, (N, K), generator=g).to(dtype).cuda()
+    whole = hd.ckpt_class_grad(dS, hd.ckpt_store(H))
+    parts = torch.zeros(K, D, device="cuda")
+    for n0 in range(0, N, 800):
+        hd.ckpt_class_grad(dS[n0:n0 + 800], hd.ckpt_store(H[n0:n0 + 800]), out=parts,
+                           accumulate=True)
+    assert torch.equal(whole, parts)
+    at = [0, 1, 63, 4095, D - 1]
+    ref = dS.cpu().double().t() @ H[:, at].cpu().double()
+    assert torch.equal(whole[:, at].cpu().double(), ref)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("K", [5, 26])
+def test_class_grad_of_few_classes_not_finite_and_strided(K, dtype):
+    hd = hd_gpu()
+    N, D = 150, 70
+    kept = hd.ckpt_store(activations(N, D, F32, 1).cuda())
+    wide = torch.randn(N, K + 3, generator=torch.Generator().manual_seed(3)).to(dtype)
+    clean = hd.ckpt_class_grad(wide[:, 1:1 + K].contiguous().cuda(), kept).cpu()
+    assert torch.equal(hd.ckpt_class_grad(wide.cuda()[:, 1:1 + K], kept).cpu(), clean)
+    wide[5, 1 + 2], wide[140, 1 + 4] = math.nan, -math.inf
+    wide[:, 0] = wide[:, 1 + K] = math.nan  # (not read)
+    got = hd.ckpt_class_grad(wide.cuda()[:, 1:1 + K], kept).cpu()
+    assert bool(torch.isnan(got[2]).all()) and not bool(torch.isfinite(got[4]).any())
+    rest = [k for k in range(K) if k not in (2, 4)]
+    assert torch.equal(got[rest], clean[rest])
+
+
 def test_class_grad_not_finite():
     """NaN and infinities of dS stay in their class, those of H in their column."""
     hd = hd_gpu()
