@@ -552,10 +552,11 @@ bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
 
 template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
 hipError_t launch_product_as(const ProductArgs& a) {
-  // Eight waves share the input tiles; four where two row tiles take more than 128
-  // registers, so that three workgroups of them fit where one of eight would (32 x 3072 x
-  // 10240: 12.4 us with eight, 11.2 with four).
-  const int most = NT == 2 ? 4 : 8, waves = a.L.itiles < most ? (int)a.L.itiles : most;
+  // Eight waves share the input tiles; four where two row tiles or four output tiles take more
+  // than 128 registers, so that two or three workgroups of them fit where one of eight
+  // would (32 x 3072 x 10240: 12.4 us with eight, 11.2 with four; fp32 32 x 8192 x 16384, four
+  // output tiles: 40 and 36).
+  const int most = NT == 2 || TD > 2 ? 4 : 8, waves = a.L.itiles < most ? (int)a.L.itiles : most;
   const int ntiles = (int)cdiv(a.N, 16);
   size_t lds = sizeof(f32x4) * 64 * TD * NT * waves;
   if (XLDS) {
@@ -572,17 +573,37 @@ hipError_t launch_product_as(const ProductArgs& a) {
 
 constexpr size_t kStreamBytes = size_t(192) << 20;
 
+// X laid out in memory is read once for each workgroup's output tiles, and that weighs more
+// than the codes: four tiles (WIDE) instead of two halve it, but leave half the workgroups.
+// * fp32: where two tiles make more workgroups than compute units, of which each holds
+//   one (16 x 4096 x 10240: 13.6 us, with two tiles 18.0; 64 x 4096 x 16384: 43 and 67; but 16 x
+//   4096 x 8192, 256 workgroups: 14 and 12.9);
+// * bf16: where four tiles leave 7/4 workgroups for each compute unit, and two input tiles for
+//   each wave (32 x 8192 x 28672: 32.7 us, with two 37.9; 64 x 8192 x 16384: 31.4 and 38.2; but 64
+//   x 8192 x 12288, 384 workgroups: 36 and 34).
+// The zero points of groups of 32 leave registers for three in fp32 and, with two row tiles,
+// for two.
+template <typename T, int GPT, bool ZERO, int NT, bool STREAM>
+hipError_t launch_product_laid(const ProductArgs& a) {
+  constexpr int WIDE = !(GPT == 4 && ZERO) ? 4 : NT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4;
+  const int64_t rows = cdiv(a.N, 16 * NT), cus = num_cus();
+  const bool wide = sizeof(T) == 4 ? cdiv(a.L.otiles, 2) * rows > cus
+                                   : cdiv(a.L.otiles, 4) * rows >= 7 * cus / 4 && a.L.itiles >= 8;
+  if constexpr (WIDE > 2)
+    if (wide) return launch_product_as<T, GPT, ZERO, NT, WIDE, STREAM, false>(a);
+  return launch_product_as<T, GPT, ZERO, NT, 2, STREAM, false>(a);
+}
+
 template <typename T, int GPT, bool ZERO>
 hipError_t launch_product_rows(const ProductArgs& a) {
   const bool stream = a.L.scales > kStreamBytes;
   if (!a.xop)
     return stream ? launch_product_as<T, GPT, ZERO, 1, 2, true, true>(a)
                   : launch_product_as<T, GPT, ZERO, 1, 2, false, true>(a);
-  if (a.N <= 16 && stream) return launch_product_as<T, GPT, ZERO, 1, 2, true, false>(a);
+  if (a.N <= 16 && stream) return launch_product_laid<T, GPT, ZERO, 1, true>(a);
   // (fp32's three parts of two row tiles would not fit the registers)
-  if (a.N <= 16 || sizeof(T) == 4)
-    return launch_product_as<T, GPT, ZERO, 1, 2, false, false>(a);
-  if constexpr (sizeof(T) == 2) return launch_product_as<T, GPT, ZERO, 2, 2, false, false>(a);
+  if (a.N <= 16 || sizeof(T) == 4) return launch_product_laid<T, GPT, ZERO, 1, false>(a);
+  if constexpr (sizeof(T) == 2) return launch_product_laid<T, GPT, ZERO, 2, false>(a);
 }
 
 template <typename T>

@@ -124,6 +124,43 @@ def test_large_weights(dtype, group, zeros):
     assert bool(((Y[:, pick] - ref).abs() <= P.nibble_bound(X, size, ref, F32)).all())
 
 
+# many outputs: workgroups of more output tiles, the last ones past the end
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,outer,inner,dtype", [
+    (16, 8300, 1100, F32), (40, 4130, 1300, F32), (16, 28690, 2600, BF16),
+    (130, 5770, 1100, BF16), (20, 28700, 1030, BF16), (3, 28690, 16384, BF16)])
+def test_many_outputs(N, outer, inner, dtype, group, zeros):
+    hd = hd_gpu()
+    announce(f"nibble many outputs {N}x{outer}x{inner} group {group} zeros {zeros} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(N + inner)
+    codes = torch.randint(0, 256, (outer, inner // 2), dtype=torch.uint8, generator=g,
+                          device="cuda")
+    ngroups = -(-inner // group)
+    scales = (torch.rand(outer, ngroups, generator=g, device="cuda") + 0.25).to(BF16)
+    z = torch.randint(0, 16, (outer, ngroups), dtype=torch.uint8, generator=g,
+                      device="cuda") if zeros else None
+    X = torch.randn(N, inner, generator=torch.Generator().manual_seed(2)).to(dtype)
+    w = hd.nibble_pack(codes, scales, z, inner=inner, group=group)
+    Y = hd.nibble_product(X.cuda(), w, dtype=F32)
+    pick = torch.cat([torch.arange(70), torch.arange(outer - 70, outer)])
+    W, size = P.nibble_weights(codes[pick.cuda()].cpu(), scales[pick.cuda()].cpu(),
+                               None if z is None else z[pick.cuda()].cpu(), inner, group)
+    ref = X.double() @ W.t()
+    bound = P.nibble_bound(X, size, ref, F32)
+    assert bool(((Y[:, pick.cuda()].cpu().double() - ref).abs() <= bound).all())
+    # the outputs between: whole numbers, exact in every order of the sums
+    ones = torch.ones_like(scales)
+    w = hd.nibble_pack(codes, ones, z, inner=inner, group=group)
+    X = torch.randint(-8, 9, (N, inner), generator=torch.Generator().manual_seed(3)).to(dtype)
+    Y = hd.nibble_product(X.cuda(), w, dtype=F32)
+    for o in range(0, outer, 4096):
+        part = hd.nibble_pack(codes[o:o + 4096].contiguous(), ones[o:o + 4096].contiguous(),
+                              None if z is None else z[o:o + 4096].contiguous(), inner=inner,
+                              group=group)
+        assert torch.equal(Y[:, o:o + 4096], X.cuda().float() @ hd.nibble_unpack(part).t())
+
+
 def test_fp32_x_in_full():
     """Weight 1 (code 1, zero point 0) on one input: the three parts of an fp32 X add
     up to every bit of it."""
