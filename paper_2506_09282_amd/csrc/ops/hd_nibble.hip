@@ -526,17 +526,19 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
   }
 }
 
-constexpr size_t kXLds = 64 * 1024;  // X in LDS: two workgroups to a compute unit
+// X in LDS: two workgroups to a compute unit, or (fp32, of whose kernels a compute unit
+// holds one workgroup anyway) one.
+constexpr size_t kXLds = 64 * 1024, kXLdsOne = 128 * 1024;
 
 struct ProductArgs {
   const void* X;
   int64_t ldx;
-  const bf16x8* xop;  // null: X in LDS
+  const bf16x8* xop;  // X laid out
   const uint8_t* image;
   void* Y;
   int64_t ldy, N, O, I;
   NibbleLayout L;
-  int y_dt, act;
+  int lds_tiles, y_dt, act;
   hipStream_t stream;
 };
 
@@ -550,22 +552,44 @@ bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
   return N <= 16 && x_lds_bytes(N, itiles, x_dt) <= kXLds;
 }
 
+// Output tiles of a workgroup that keeps X in LDS; 0: X is laid out in memory. Each workgroup
+// lays X out again, so where it fills half of the LDS (fp32; bf16 gains nothing) that pays if
+// all of them run at once (1 x 16384 x 700: 16.9 us, with X in memory 24.1; 4 x 4096 x 10240 in
+// three tiles: 10.5 and 13.3; but 4 x 4096 x 28672 in four: 22.4 and 20.6), and for one row always,
+// which X in memory holds sixteen times (1 x 16384 x 57344: 122 and 157).
+int lds_tiles(int64_t N, int64_t otiles, int64_t itiles, int x_dt) {
+  if (x_in_lds(N, itiles, x_dt)) return 2;
+  if (x_dt != 0 || N > 16 || x_lds_bytes(N, itiles, x_dt) > kXLdsOne) return 0;
+  for (int tiles = 2; tiles <= 4; ++tiles)
+    if (cdiv(otiles, tiles) <= num_cus()) return tiles;
+  return N == 1 ? 4 : 0;
+}
+
 template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
 hipError_t launch_product_as(const ProductArgs& a) {
-  // Eight waves share the input tiles; four where two row tiles or four output tiles take more
-  // than 128 registers, so that two or three workgroups of them fit where one of eight
-  // would (32 x 3072 x 10240: 12.4 us with eight, 11.2 with four; fp32 32 x 8192 x 16384, four
-  // output tiles: 40 and 36).
-  const int most = NT == 2 || TD > 2 ? 4 : 8, waves = a.L.itiles < most ? (int)a.L.itiles : most;
+  // Eight waves share the input tiles; without X in LDS four where two row tiles or four output
+  // tiles take more than 128 registers, so that two or three workgroups of them fit where one
+  // of eight would (32 x 3072 x 10240: 12.4 us with eight, 11.2 with four; fp32 32 x 8192 x
+  // 16384, four output tiles: 40 and 36).
+  const int most = !XLDS && (NT == 2 || TD > 2) ? 4 : 8;
+  const int waves = a.L.itiles < most ? (int)a.L.itiles : most;
   const int ntiles = (int)cdiv(a.N, 16);
   size_t lds = sizeof(f32x4) * 64 * TD * NT * waves;
   if (XLDS) {
     const size_t x = x_lds_bytes(a.N, a.L.itiles, sizeof(T) == 4 ? 0 : 1);
     if (x > lds) lds = x;
   }
-  hipLaunchKernelGGL((nibble_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS>),
-                     dim3((unsigned)(cdiv(a.L.otiles, TD) * cdiv(ntiles, NT))), dim3(64 * waves),
-                     lds, a.stream, static_cast<const T*>(a.X), a.ldx, a.xop, ntiles, a.image,
+  const auto kernel = nibble_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS>;
+  if (lds > 64 * 1024) {  // above the default limit: raised once per device and kernel
+    static PerDeviceOnce once;
+    const hipError_t e = once_per_device(once, [&] {
+      return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)kXLdsOne);
+    });
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(cdiv(a.L.otiles, TD) * cdiv(ntiles, NT))),
+                     dim3(64 * waves), lds, a.stream, static_cast<const T*>(a.X), a.ldx, a.xop, ntiles, a.image,
                      (int64_t)a.L.scales, (int64_t)a.L.zeros, a.Y, a.ldy, a.N, a.O, a.I,
                      a.L.otiles, (int)a.L.itiles, a.y_dt, a.act);
   return hipGetLastError();
@@ -597,7 +621,14 @@ hipError_t launch_product_laid(const ProductArgs& a) {
 template <typename T, int GPT, bool ZERO>
 hipError_t launch_product_rows(const ProductArgs& a) {
   const bool stream = a.L.scales > kStreamBytes;
-  if (!a.xop)
+  if constexpr (sizeof(T) == 4) {
+    // (codes past the caches have more output tiles than three of them to a compute unit)
+    if (a.lds_tiles == 4)
+      return stream ? launch_product_as<T, GPT, ZERO, 1, 4, true, true>(a)
+                    : launch_product_as<T, GPT, ZERO, 1, 4, false, true>(a);
+    if (a.lds_tiles == 3) return launch_product_as<T, GPT, ZERO, 1, 3, false, true>(a);
+  }
+  if (a.lds_tiles == 2)
     return stream ? launch_product_as<T, GPT, ZERO, 1, 2, true, true>(a)
                   : launch_product_as<T, GPT, ZERO, 1, 2, false, true>(a);
   if (a.N <= 16 && stream) return launch_product_laid<T, GPT, ZERO, 1, true>(a);
@@ -684,8 +715,9 @@ hipError_t launch_nibble_product(const void* X, int64_t ldx, const void* image, 
                                  bool with_zeros, int x_dt, int y_dt, int act, void* workspace,
                                  hipStream_t stream) {
   ProductArgs a{X,   ldx, nullptr, static_cast<const uint8_t*>(image), Y,  ldy, N, O,
-                I,   layout_of(O, I, G), y_dt, act, stream};
-  if (!x_in_lds(N, a.L.itiles, x_dt)) {
+                I,   layout_of(O, I, G), 0, y_dt, act, stream};
+  a.lds_tiles = lds_tiles(N, a.L.otiles, a.L.itiles, x_dt);
+  if (a.lds_tiles == 0) {
     bf16x8* xop = static_cast<bf16x8*>(workspace);
     const int ntiles = (int)cdiv(N, 16);
     const int64_t total = a.L.itiles * ntiles * 256;

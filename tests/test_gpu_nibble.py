@@ -129,7 +129,10 @@ def test_large_weights(dtype, group, zeros):
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("N,outer,inner,dtype", [
     (16, 8300, 1100, F32), (40, 4130, 1300, F32), (16, 28690, 2600, BF16),
-    (130, 5770, 1100, BF16), (20, 28700, 1030, BF16), (3, 28690, 16384, BF16)])
+    (130, 5770, 1100, BF16), (20, 28700, 1030, BF16), (3, 28690, 16384, BF16),
+    # X of fp32 in more of the LDS: two, three, four output tiles
+    (1, 150, 16384, F32), (4, 10230, 4096, F32), (3, 16010, 4000, F32), (1, 20010, 16384, F32),
+    (1, 28690, 16384, F32)])
 def test_many_outputs(N, outer, inner, dtype, group, zeros):
     hd = hd_gpu()
     announce(f"nibble many outputs {N}x{outer}x{inner} group {group} zeros {zeros} {dtype}")
