@@ -400,6 +400,7 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
     }
   };
   const bf16x8* xs = reinterpret_cast<const bf16x8*>(sums);
+  const int lds_rows = N - 16 * nt0 < 16 ? (int)(N - 16 * nt0) : 16;  // of X in LDS
   // The two chains of fp32 are joined when both are finished: begun from the other, the first
   // would carry its size through every addition (1 x 561 x 10240: 4.3e-7 of the result
   // instead of 2.7e-7). bf16 saves the addition.
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if constexpr (XLDS)
-              xp[s][t][p] = xs[((it * 4 + g * STEPS + s) * P + p) * 4 * (int)N];
+              xp[s][t][p] = xs[((it * 4 + g * STEPS + s) * P + p) * 4 * lds_rows];
             else
               xp[s][t][p] = x.v[t][g * STEPS + s][p];
             one[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xp[s][t][p], one[t], 0, 0, 0);
@@ -470,12 +471,12 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
     load_x(nth(0), x[0]);
   }
   if (XLDS) {
-    const int rows = (int)N, chunks = itiles * 16;  // of eight inputs
+    const int rows = lds_rows, chunks = itiles * 16;  // of eight inputs
     bf16x8* dst = reinterpret_cast<bf16x8*>(sums);
     for (int c = threadIdx.x; c < chunks * rows; c += blockDim.x) {
       const int n = c / chunks, ch = c % chunks;
       bf16x8 parts[P];
-      x_operands(X + n * ldx, ch, I, parts);
+      x_operands(X + (16 * nt0 + n) * ldx, ch, I, parts);
 #pragma unroll
       for (int p = 0; p < P; ++p) dst[((ch / 4 * P + p) * 4 + ch % 4) * rows + n] = parts[p];
     }
@@ -552,9 +553,9 @@ struct ProductArgs {
 
 constexpr int parts_of(int x_dt) { return x_dt == 0 ? 3 : 1; }
 
-// Bytes of X as operands: in LDS (few rows), in memory.
+// Bytes of X as operands in LDS, up to 16 rows.
 size_t x_lds_bytes(int64_t N, int64_t itiles, int x_dt) {
-  return (size_t)N * itiles * 256 * parts_of(x_dt);
+  return (size_t)(N < 16 ? N : 16) * itiles * 256 * parts_of(x_dt);
 }
 bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
   return N <= 16 && x_lds_bytes(N, itiles, x_dt) <= kXLds;
@@ -567,6 +568,14 @@ bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
 // which X in memory holds sixteen times (1 x 16384 x 57344: 122 and 157).
 int lds_tiles(int64_t N, int64_t otiles, int64_t itiles, int x_dt) {
   if (x_in_lds(N, itiles, x_dt)) return 2;
+  // More rows: each workgroup a tile of 16, while the workgroups run at once and together
+  // lay out little (20 x 1000 x 8192 bf16: 9.1 us, with X in memory and a launch more 10.8; 64 x
+  // 617 x 4096 fp32 9.1 and 10.8; but 64 x 2000 x 4096 bf16 12.8 and 11.4, 20 x 617 x 10240 fp32
+  // 13.0 and 11.8).
+  if (x_lds_bytes(N, itiles, x_dt) <= kXLds) {
+    const int64_t groups = cdiv(otiles, 2) * cdiv(N, 16), cus = num_cus();
+    return groups <= 2 * cus && groups * itiles <= 16 * cus ? 2 : 0;
+  }
   if (x_dt != 0 || N > 16 || x_lds_bytes(N, itiles, x_dt) > kXLdsOne) return 0;
   for (int tiles = 2; tiles <= 4; ++tiles)
     if (cdiv(otiles, tiles) <= num_cus()) return tiles;
