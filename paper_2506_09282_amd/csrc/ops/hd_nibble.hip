@@ -568,17 +568,21 @@ bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
 // which X in memory holds sixteen times (1 x 16384 x 57344: 122 and 157).
 int lds_tiles(int64_t N, int64_t otiles, int64_t itiles, int x_dt) {
   if (x_in_lds(N, itiles, x_dt)) return 2;
-  // More rows: each workgroup a tile of 16, while the workgroups run at once and together
-  // lay out little (20 x 1000 x 8192 bf16: 9.1 us, with X in memory and a launch more 10.8; 64 x
-  // 617 x 4096 fp32 9.1 and 10.8; but 64 x 2000 x 4096 bf16 12.8 and 11.4, 20 x 617 x 10240 fp32
-  // 13.0 and 11.8).
-  if (x_lds_bytes(N, itiles, x_dt) <= kXLds) {
-    const int64_t groups = cdiv(otiles, 2) * cdiv(N, 16), cus = num_cus();
-    return groups <= 2 * cus && groups * itiles <= 16 * cus ? 2 : 0;
+  // More rows: each workgroup a tile of 16, where the workgroups run at once and together
+  // lay out little, for a launch less (20 x 1000 x 8192 bf16: 9.1 us, with X in memory 10.8; fp32
+  // 64 x 617 x 4096 9.1 and 10.8, 64 x 1280 x 2000 9.0 and 11.3; but 64 x 2000 x 4096 bf16 12.8
+  // and 11.4, 20 x 617 x 10240 fp32 13.0 and 11.8).
+  const size_t bytes = x_lds_bytes(N, itiles, x_dt);
+  const int64_t cus = num_cus();
+  if (N > 16) {
+    const int64_t groups = cdiv(otiles, 2) * cdiv(N, 16);
+    const bool fits = bytes <= kXLds ? groups <= 2 * cus
+                                     : x_dt == 0 && bytes <= kXLdsOne && groups <= cus;
+    return fits && groups * itiles <= 16 * cus ? 2 : 0;
   }
-  if (x_dt != 0 || N > 16 || x_lds_bytes(N, itiles, x_dt) > kXLdsOne) return 0;
+  if (x_dt != 0 || bytes > kXLdsOne) return 0;
   for (int tiles = 2; tiles <= 4; ++tiles)
-    if (cdiv(otiles, tiles) <= num_cus()) return tiles;
+    if (cdiv(otiles, tiles) <= cus) return tiles;
   return N == 1 ? 4 : 0;
 }
 
