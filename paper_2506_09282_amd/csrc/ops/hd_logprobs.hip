@@ -600,7 +600,8 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     if (wave == 0) {
       // lane p holds part p
       uint32_t* w = words + (int64_t)lane * kPartWords;
-      uint64_t keys[kMaxTop] = {};
+      uint64_t keys[kMaxTop] = {}, first = 0;
+      const int each = TOP ? 64 / sp.parts : 0;  // keys of a part that begin the list
       st = stats_none(c);
       if (lane < sp.parts) {
         st.m = __uint_as_float(get_word(w));
@@ -610,13 +611,18 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
         if (TOP) {
 #pragma unroll
           for (int t = 0; t < kMaxTop; ++t)
-            if (t < o.top) keys[t] = get_key(w + 4 + 2 * t);
+            if (t >= each && t < o.top) keys[t] = get_key(w + 4 + 2 * t);
         }
       }
+      if (TOP && lane < each * sp.parts && lane / sp.parts < o.top)
+        first = get_key(words + (int64_t)(lane % sp.parts) * kPartWords + 4 +
+                        2 * (lane / sp.parts));
       st = stats_across<64>(st, c);
       if (TOP) {
-        // The parts' best, sorted, begin the list; its T-th is a bar for the rest.
-        list.key = sort64(keys[0], lane);
+        // The parts' best, up to 64 together, sorted, begin the list; its T-th is a bar for the
+        // rest. (With one of each part ten parts' 320 keys would pass one by one: 1 x 20000
+        // top 32, 31 us.)
+        list.key = sort64(first, lane);
         const uint64_t bar = lane_key(list.key, o.top - 1);
 #pragma unroll
         for (int t = 1; t < kMaxTop; ++t) {
