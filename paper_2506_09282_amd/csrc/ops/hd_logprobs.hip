@@ -19,8 +19,8 @@
 // comparison.
 //
 // * up to kShortK classes: LPR lanes hold a row in registers.
-// * more: a workgroup walks a row, or a part of it where there are fewer rows than
-//   the chip has room for; the last workgroup to finish joins the parts in order.
+// * more: a wave walks a row, or a workgroup does, or a part of it, where there are fewer rows
+//   than the chip has room for; the last workgroup to finish joins the parts in order.
 // The gradient is a pass over the elements: statistics and entropy are its inputs, so it
 // reads each score once and needs no reduction.
 //
@@ -44,6 +44,7 @@ namespace {
 
 constexpr int kShortK = 1024;
 constexpr int kLongThreads = 256;
+constexpr int64_t kWaveBytes = 48 * 1024;  // of a row that one wave may take
 // 16-byte chunks that a thread takes in a step: two of bf16, whose work for each byte
 // is twice fp32's (4096 x 65536 top 4: 121 us with one, 116 with two; fp32 2048 x 100003 133
 // with one, 151 with two), and where rows are split, which leaves a wave one step and
@@ -458,10 +459,10 @@ __device__ __forceinline__ void put_key(uint32_t* p, uint64_t v) {
                      __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <typename T, bool TOP, bool MASK, bool STREAM, int kChunks>
-__global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArgs a, Out o,
-                                                                     Split sp) {
-  constexpr int LEN = Chunk<T>::kLen, WAVES = kLongThreads / 64;
+template <typename T, bool TOP, bool MASK, bool STREAM, int kChunks, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void logprobs_long_kernel(LogprobsArgs a, Out o,
+                                                                   Split sp) {
+  constexpr int LEN = Chunk<T>::kLen, kThreads = 64 * WAVES;
   constexpr int VALS = kChunks * LEN;
   __shared__ Stats sh_st[WAVES];
   __shared__ uint64_t sh_key[WAVES * kMaxTop];
@@ -480,7 +481,7 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
   }
   Stats st = stats_none(c);
   TopList list{0, -INFINITY};
-  constexpr int ROUND = kLongThreads * LEN, STEP = kChunks * ROUND;
+  constexpr int ROUND = kThreads * LEN, STEP = kChunks * ROUND;
   auto class_of = [](int e) { return (uint32_t)(e / LEN * ROUND + e % LEN); };
   auto add = [&](float(&v)[VALS], uint32_t id0) {  // id0: the class of v[0]
     float m = v[0];
@@ -632,7 +633,7 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
       }
     }
     __syncthreads();  // all is read: left zeroed
-    for (int64_t i = threadIdx.x; i < (int64_t)sp.parts * kPartWords; i += kLongThreads)
+    for (int64_t i = threadIdx.x; i < (int64_t)sp.parts * kPartWords; i += kThreads)
       words[i] = 0;
   }
   if (wave != 0) return;
@@ -664,35 +665,43 @@ hipError_t launch_short(const LogprobsArgs& a, const Out& o, hipStream_t stream)
   return hipGetLastError();
 }
 
+template <typename T, bool STREAM, int C, int WAVES>
+hipError_t launch_long(const LogprobsArgs& a, const Out& o, Split s, hipStream_t stream) {
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.N * s.parts)), dim3(64 * WAVES), 0, stream, a, o,
+                       s);
+    return hipGetLastError();
+  };
+  if (o.top)
+    return a.mask ? go(logprobs_long_kernel<T, true, true, STREAM, C, WAVES>)
+                  : go(logprobs_long_kernel<T, true, false, STREAM, C, WAVES>);
+  return a.mask ? go(logprobs_long_kernel<T, false, true, STREAM, C, WAVES>)
+                : go(logprobs_long_kernel<T, false, false, STREAM, C, WAVES>);
+}
+
 template <typename T>
 hipError_t launch_typed(const LogprobsArgs& a, const Out& o, Split s, hipStream_t stream) {
+  // Where few rows ask for many alternatives a wave takes a row: the T rounds of the narrower
+  // forms are steps that wait for each other (1000 x 100, kernel: top 32 7.4 us instead of
+  // 12.6, top 8 4.9 instead of 5.7, top 3 4.4 instead of 4.1; 8000 x 100 top 32 17.6 instead of 14.8).
+  if (o.top >= 8 && a.K <= 64 * 4 && a.N <= 8 * (int64_t)num_cus())
+    return launch_short<T, 64, 4>(a, o, stream);
   if (a.K <= 8 * 4) return launch_short<T, 8, 4>(a, o, stream);
   if (a.K <= 16 * 8) return launch_short<T, 16, 8>(a, o, stream);
   if (a.K <= 16 * 16) return launch_short<T, 16, 16>(a, o, stream);
   if (a.K <= kShortK) return launch_short<T, 64, 16>(a, o, stream);
-  const dim3 grid((unsigned)(a.N * s.parts)), block(kLongThreads);
   const bool stream_by = a.N * a.K * (int64_t)sizeof(T) > kStreamBytes;
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, o, s);
-  };
   constexpr int C1 = chunks_of(sizeof(T), false), C2 = chunks_of(sizeof(T), true);
-  if (s.parts > 1) {
-    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, false, C2>);
-    else if (o.top) go(logprobs_long_kernel<T, true, false, false, C2>);
-    else if (a.mask) go(logprobs_long_kernel<T, false, true, false, C2>);
-    else go(logprobs_long_kernel<T, false, false, false, C2>);
-  } else if (stream_by) {
-    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, true, C1>);
-    else if (o.top) go(logprobs_long_kernel<T, true, false, true, C1>);
-    else if (a.mask) go(logprobs_long_kernel<T, false, true, true, C1>);
-    else go(logprobs_long_kernel<T, false, false, true, C1>);
-  } else {
-    if (o.top && a.mask) go(logprobs_long_kernel<T, true, true, false, C1>);
-    else if (o.top) go(logprobs_long_kernel<T, true, false, false, C1>);
-    else if (a.mask) go(logprobs_long_kernel<T, false, true, false, C1>);
-    else go(logprobs_long_kernel<T, false, false, false, C1>);
-  }
-  return hipGetLastError();
+  if (s.parts > 1) return launch_long<T, false, C2, 4>(a, o, s, stream);
+  // A wave takes a row where there are enough: four waves start, join and sort their lists
+  // for a few steps each (30000 x 3000 fp32 top 5: 112 us, four 192; bf16 70 and 157; top 32 185 and
+  // 335; but 1100 x 3000 fp32, kernel: 15.3 and 12.2). In long rows four waves
+  // of a row are better (6000 x 16000 fp32 top 5: 115 and 107).
+  if (a.K * (int64_t)sizeof(T) <= kWaveBytes && a.N >= 7 * (int64_t)num_cus())
+    return stream_by ? launch_long<T, true, C1, 1>(a, o, s, stream)
+                     : launch_long<T, false, C1, 1>(a, o, s, stream);
+  return stream_by ? launch_long<T, true, C1, 4>(a, o, s, stream)
+                   : launch_long<T, false, C1, 4>(a, o, s, stream);
 }
 
 // ---- gradient --------------------------------------------------------------------

@@ -105,6 +105,43 @@ def test_logprobs(N, K, top, dtype, scale, mask):
         assert a is None or bool(((a == b) | ((a != a) & (b != b))).all())
 
 
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("top", [0, 3, 32])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,K", [(2100, 1025), (2050, 3001), (2049, 8192), (40, 100), (2100, 100)])
+def test_many_rows(N, K, dtype, top, masked):
+    """Rows of a wave each; and short rows whose form depends on their number."""
+    hd = hd_gpu()
+    announce(f"logprobs {N}x{K} top {top} {dtype} mask {masked}")
+    s, y, g = random_scores(N, K, dtype, seed=N + K)
+    s[3] = 1.0                                     # ties
+    s[4, ::2], s[4, 1::2] = 0.0, -0.0
+    s[5, K // 2], s[6, K - 1], s[7] = math.nan, math.inf, -math.inf
+    s[8] = torch.arange(K).to(dtype)               # each beats all before it
+    s[9] = torch.finfo(dtype).min
+    m = torch.rand(N, K, generator=g) < 0.6 if masked else None
+    if masked:
+        m[N - 1] = False
+        s[5, K // 2] = s[6, K - 1] = math.nan
+        m[5, K // 2] = m[6, K - 1] = False
+    got = hd.logprobs(s.cuda(), y.cuda(), top=top, scale=0.7, mask=cuda(m))
+    for rows in (slice(0, 12), slice(N - 8, N)):
+        sub = hd.LogProbs(*(None if v is None else v[rows] for v in got))
+        mm = m[rows] if masked else None
+        check(sub, P.logprobs(s[rows], y[rows], top, 0.7, mm), s[rows], 0.7, K, top)
+    # rows between: the same alternatives as in calls of a few rows
+    for n0 in range(12, N, 500):
+        few = hd.logprobs(s[n0:n0 + 7].cuda(), y[n0:n0 + 7].cuda(), top=top, scale=0.7,
+                          mask=cuda(m[n0:n0 + 7]) if masked else None)
+        if top:
+            assert torch.equal(few.ids, got.ids[n0:n0 + 7])
+    off = torch.empty(N, K + 5, dtype=dtype, device="cuda")[:, 3:3 + K]
+    off.copy_(s)
+    wide = hd.logprobs(off, y.cuda(), top=top, scale=0.7, mask=cuda(m))
+    for a, b in zip(wide, got):  # strides and alignment change no bit
+        assert a is None or bool(((a == b) | ((a != a) & (b != b))).all())
+
+
 @pytest.mark.parametrize("K", [5, 32, 100, 1000, 3000, 20001])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_ties_and_extremes(K, dtype):
