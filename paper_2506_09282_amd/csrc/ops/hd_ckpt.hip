@@ -49,18 +49,25 @@ __host__ __device__ inline int64_t scales_at(int64_t N, int64_t D) {
 // How a lane's four columns of 256 lie. Where rows start at multiples of 16 bytes (8 in
 // bf16) they are neighbours, in one load; elsewhere they are 64 apart and each load of a
 // wave is a run, which is faster than wide loads across the lines' ends (1999 x 4097
-// bf16 kept: 11.8 us wide, 9.4 so).
-// kNear, and past the caches (kStreamBytes) kNearOnce: rows pass once and do not stay there,
-// the kept values, a quarter or half as large, do (4096 x 10240 fp32, 168 MB, kept and taken
-// back: 70.3 us instead of 81.5; 84 MB: 37.1 instead of 35.9).
-enum Columns { kApart, kNear, kNearOnce };
+// bf16 kept: 11.8 us wide, 9.4 so). ..Once: past the caches (kStreamBytes) rows pass once and do
+// not stay there, the kept values, a quarter or half as large, do (4096 x 10240 fp32, 168 MB,
+// kept and taken back: 70.3 us instead of 81.5; 84 MB: 37.1 instead of 35.9; 65536 x 1001 fp32
+// kept: 68 instead of 106; 16384 x 8000 taken back: 97 instead of 120).
+enum Columns { kApart, kApartOnce, kNear, kNearOnce };
+constexpr bool near(int m) { return m == kNear || m == kNearOnce; }
+constexpr bool once(int m) { return m == kApartOnce || m == kNearOnce; }
 constexpr int64_t kStreamBytes = int64_t(96) << 20;
 
 template <int M>
 __device__ __forceinline__ int64_t column_of(int64_t d0, int lane, int c) {
-  return M == kApart ? d0 + 64 * c + lane : d0 + 4 * lane + c;
+  return near(M) ? d0 + 4 * lane + c : d0 + 64 * c + lane;
 }
 
+template <bool ONCE, typename T>
+__device__ __forceinline__ float load_row1(const T* p) {
+  const T x = ONCE ? __builtin_nontemporal_load(p) : *p;
+  return load_elem(&x, 0);
+}
 template <bool ONCE>
 __device__ __forceinline__ void load_row4(const float* p, float (&v)[4]) {
   const f32x4* at = reinterpret_cast<const f32x4*>(p);
@@ -114,16 +121,21 @@ __global__ __launch_bounds__(256) void ckpt_store_kernel(const T* __restrict__ H
     const int64_t d = column_of<M>(d0, lane, c);
     col[c] = H + (d < D ? d : D - 1);
   }
-  if (M != kApart && d0 + 256 <= D) {
+  if (near(M) && d0 + 256 <= D) {
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      load_row4<M == kNearOnce>(col[0] + (n0 + r < N ? n0 + r : N - 1) * ldh, v[r]);
+      load_row4<once(M)>(col[0] + (n0 + r < N ? n0 + r : N - 1) * ldh, v[r]);
+  } else if (near(M) && D % 4 == 0) {  // a lane's four columns are all there or all past D
+    const T* four = H + (d0 + 4 * lane < D ? d0 + 4 * lane : D - 4);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      load_row4<once(M)>(four + (n0 + r < N ? n0 + r : N - 1) * ldh, v[r]);
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        v[r][c] = load_elem(col[c], (n0 + r < N ? n0 + r : N - 1) * ldh);
+        v[r][c] = load_row1<once(M)>(col[c] + (n0 + r < N ? n0 + r : N - 1) * ldh);
   }
   if (n0 + 16 > N) {
 #pragma unroll
@@ -194,8 +206,8 @@ __global__ __launch_bounds__(256) void ckpt_load_kernel(const u32x4* __restrict_
 #pragma unroll
     for (int c = 0; c < 4; ++c) v[c] = (float)(int8_t)(w[c][e / 4] >> (8 * (e % 4))) * s[c];
     T* row = H + (n0 + e) * ldh;
-    if (M != kApart && d0 + 256 <= D) {
-      store_row4<M == kNearOnce>(row + d0 + 4 * lane, v);
+    if (near(M) && (d0 + 256 <= D || D % 4 == 0)) {
+      if (d0 + 4 * lane < D) store_row4<once(M)>(row + d0 + 4 * lane, v);
     } else {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -206,10 +218,14 @@ __global__ __launch_bounds__(256) void ckpt_load_kernel(const u32x4* __restrict_
   }
 }
 
+bool rows_aligned(const void* rows, int64_t ld, int dt) {
+  return (uintptr_t)rows % (dt == 0 ? 16 : 8) == 0 && ld % 4 == 0;
+}
 Columns columns_of(const void* rows, int64_t ld, int64_t N, int64_t D, int dt) {
-  const int64_t es = dt == 0 ? 4 : 2;
-  if ((uintptr_t)rows % (4 * es) != 0 || ld % 4 != 0) return kApart;
-  return N * D * es > kStreamBytes ? kNearOnce : kNear;
+  const bool past = N * D * (dt == 0 ? 4 : 2) > kStreamBytes;
+  // (fewer columns than a workgroup's would leave lanes of every load without work)
+  if (rows_aligned(rows, ld, dt) && D >= 256) return past ? kNearOnce : kNear;
+  return past ? kApartOnce : kApart;
 }
 
 // ---- the other operand --------------------------------------------------------------
@@ -682,6 +698,7 @@ hipError_t launch_ckpt_store(const void* H, int64_t ldh, int64_t N, int64_t D, i
     typedef std::remove_const_t<std::remove_pointer_t<decltype(rows)>> T;
     switch (columns_of(rows, ldh, N, D, dt)) {
       case kApart: return go(ckpt_store_kernel<T, kApart>, rows);
+      case kApartOnce: return go(ckpt_store_kernel<T, kApartOnce>, rows);
       case kNear: return go(ckpt_store_kernel<T, kNear>, rows);
       case kNearOnce: return go(ckpt_store_kernel<T, kNearOnce>, rows);
     }
@@ -702,7 +719,8 @@ hipError_t launch_ckpt_load(const void* image, void* H, int64_t ldh, int64_t N, 
   auto typed = [&](auto* rows) {
     typedef std::remove_pointer_t<decltype(rows)> T;
     switch (columns_of(rows, ldh, N, D, dt)) {
-      case kApart: return go(ckpt_load_kernel<T, kApart>, rows);
+      case kApart:  // (narrow stores are ordinary ones)
+      case kApartOnce: return go(ckpt_load_kernel<T, kApart>, rows);
       case kNear: return go(ckpt_load_kernel<T, kNear>, rows);
       case kNearOnce: return go(ckpt_load_kernel<T, kNearOnce>, rows);
     }

@@ -61,9 +61,10 @@ def test_logprobs_past_the_caches(N, K, dtype, top, masked):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_checkpoints_past_the_caches(dtype):
+@pytest.mark.parametrize("D", [10240, 10241, 10244])
+def test_checkpoints_past_the_caches(D, dtype):
     hd = hd_gpu()
-    N, D = 64 * 80, 10240
+    N = 64 * 80
     announce(f"ckpt {N}x{D} {dtype}")
     H = torch.randn(N, D, generator=torch.Generator(device="cuda").manual_seed(4),
                     device="cuda").to(dtype)
