@@ -64,9 +64,17 @@ __device__ __forceinline__ int64_t group_index(int64_t o, int64_t g, int64_t iti
 
 // ---- layout ------------------------------------------------------------------
 
+// Half a dword's codes to every other nibble.
+__device__ __forceinline__ uint32_t spread(uint32_t v) {
+  v = (v | v << 8) & 0x00ff00ffu;
+  return (v | v << 4) & 0x0f0f0f0fu;
+}
+
+// `words`: rows start at multiples of four bytes, so a dword's codes are one in them too.
 __global__ __launch_bounds__(256) void nibble_pack_kernel(const uint8_t* __restrict__ codes,
                                                           int64_t O, int64_t I, int64_t itiles,
-                                                          int64_t total, uint32_t* out) {
+                                                          int words, int64_t total,
+                                                          uint32_t* out) {
   // one dword: eight codes of one output
   for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < total;
        w += (int64_t)gridDim.x * 256) {
@@ -76,6 +84,11 @@ __global__ __launch_bounds__(256) void nibble_pack_kernel(const uint8_t* __restr
     const int64_t i0 = tile % itiles * kTileI + 32 * s + 8 * (lane / 16);
     const uint8_t* row = codes + o * cdiv(I, 2);
     uint32_t v = 0;
+    if (words && o < O && i0 + 8 <= I) {
+      const uint32_t q = *reinterpret_cast<const uint32_t*>(row + i0 / 2);
+      out[w] = spread(q & 0xffffu) | spread(q >> 16) << 4;
+      continue;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (o < O && i0 + e < I)
@@ -689,8 +702,9 @@ hipError_t launch_nibble_pack(const uint8_t* codes, const bf16raw* scales, const
   uint8_t* im = static_cast<uint8_t*>(image);
   const int gpt = kTileI / G;
   const int64_t words = L.otiles * L.itiles * 256, groups = L.otiles * L.itiles * gpt * kTileO;
+  const bool aligned = (uintptr_t)codes % 4 == 0 && cdiv(I, 2) % 4 == 0;
   hipLaunchKernelGGL(nibble_pack_kernel, dim3(blocks_for(words)), dim3(256), 0, stream, codes, O,
-                     I, L.itiles, words, reinterpret_cast<uint32_t*>(im));
+                     I, L.itiles, (int)aligned, words, reinterpret_cast<uint32_t*>(im));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(nibble_pack_groups_kernel, dim3(blocks_for(groups)), dim3(256), 0, stream,

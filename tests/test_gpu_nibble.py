@@ -164,6 +164,21 @@ def test_many_outputs(N, outer, inner, dtype, group, zeros):
         assert torch.equal(Y[:, o:o + 4096], X.cuda().float() @ hd.nibble_unpack(part).t())
 
 
+@pytest.mark.parametrize("inner", [64, 70, 200])
+def test_codes_at_any_address(inner):
+    hd = hd_gpu()
+    codes, scales, z = P.random_nibble(37, inner, 32, True, seed=inner)
+    want = hd.nibble_pack(codes.cuda(), scales.cuda(), z.cuda(), inner=inner, group=32)
+    room = torch.empty(codes.numel() + 8, dtype=torch.uint8, device="cuda")
+    for off in (1, 2, 4):
+        there = room[off:off + codes.numel()].view(codes.shape)
+        there.copy_(codes)
+        got = hd.nibble_pack(there, scales.cuda(), z.cuda(), inner=inner, group=32)
+        assert torch.equal(hd.nibble_unpack(got), hd.nibble_unpack(want))
+    W, _ = P.nibble_weights(codes, scales, z, inner, 32)
+    assert torch.equal(hd.nibble_unpack(want).cpu().double(), W)
+
+
 def test_fp32_x_in_full():
     """Weight 1 (code 1, zero point 0) on one input: the three parts of an fp32 X add
     up to every bit of it."""
