@@ -84,18 +84,26 @@ __device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b
 // The running statistics of a part of a row, in powers of two: z_k = c s_k - q with
 // c = scale log2(e) and q = c m rounded to fp32, one fused multiply-add. m is the largest
 // score, at least the lowest finite number (so that an -inf stays below it); sum is 0
-// only where nothing was there. Where c m is past fp32's range (`far`), z is
-// c (s - m) and q stands for 0 in it.
+// only where nothing was there. At the row's largest score z is what q was rounded by, up to
+// half a unit in q's last place: 1/2 below kFar, but past it soon more than exp2 holds. There
+// (`far`) z is c (s - m), whose difference is exact for neighbours, and q stands for 0 in it.
 struct Stats {
   float m, q, sum, ez;  // ez: sum of z 2^z
 };
-__device__ __forceinline__ bool far_of(float q) { return !(fabsf(q) < INFINITY); }
+constexpr float kFar = 16777216.0f;  // 2^24
+__device__ __forceinline__ bool far_of(float q) { return !(fabsf(q) < kFar); }
 __device__ __forceinline__ Stats stats_none(float c) {
   return Stats{kLowest, kLowest * c, 0.0f, 0.0f};
 }
-// How far, in powers of two, a's reference lies above that of m (q = fl(c m)); <= 0.
+// How far, in powers of two, a's reference lies above that of m (q = fl(c m)): at most 0, or
+// what q and a.q were rounded by. A reference is q, or where that is far c m itself.
 __device__ __forceinline__ float stats_step(const Stats& a, float m, float q, float c) {
-  const float d = far_of(q) || far_of(a.q) ? (a.m - m) * c : a.q - q;
+  float d = a.q - q;
+  if (far_of(q) || far_of(a.q)) {
+    d = (a.m - m) * c;
+    if (!far_of(a.q)) d += fmaf(-a.m, c, a.q);
+    if (!far_of(q)) d += fmaf(m, c, -q);
+  }
   return fmaxf(d, kUnder);
 }
 __device__ __forceinline__ void stats_raise(Stats& a, float m, float c) {
