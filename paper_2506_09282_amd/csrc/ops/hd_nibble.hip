@@ -5,13 +5,18 @@
 // One pass over the weights is what bounds it: O*I/2 bytes of codes and two (with
 // zero points three) bytes a group, against X and Y, which are small. The codes go
 // to the bf16 matrix instruction, which costs the same for 1 and for 16 rows of X:
-// * a byte that holds a code 0..15 is, read as fp8 e4m3, the number q * 2^-9
-//   (0..7 are its subnormals, 8..15 its first binade), so two masks and a shift
-//   split eight codes and four conversions make eight bf16 values, exact;
-// * sum x*q and sum x run through separate chains, fresh for each group, and
-//   s * (sum x*q - z * sum x) is added in fp32. The second chain multiplies X by a
-//   constant operand, once for all tiles of outputs; its result lies in the lanes
-//   that need it, as the value that the first chain starts from;
+// * the zero point is taken off the codes, whose differences q - z are exact in bf16: signed
+//   bytes, a conversion each and a byte permutation for two (`codes_less_zero`). A sum over
+//   a group holds the products themselves and is added to the output's with s in fp32;
+// * bf16 results of bf16 X take a shorter way. A byte that holds a code 0..15 is, read as fp8
+//   e4m3, the number q * 2^-9 (0..7 are its subnormals, 8..15 its first binade), so two masks
+//   and a shift split eight codes and four conversions make eight bf16 values, exact.
+//   sum x*q starts from -z * sum x, which a constant operand gives once for all tiles of
+//   outputs, in the lanes that need it. Over an X of one sign both are larger than their
+//   difference, by up to 16 times its products, and so are fp32's roundings: about 2^-19 of the
+//   products' sum, where the result's own rounding is 2^-9 of it. Results that stay in
+//   fp32, or whose sign is taken, do not go this way (1 x 16384 x 57344 bf16, G = 128: 90 us a
+//   call so, 94 with exact differences; G = 64 with zero points 95 and 109);
 // * fp32 X is the exact sum of three bf16 values (its 24 bits cut in three), one
 //   matrix instruction each. Products of 4 and 8 bits are exact in fp32.
 //
@@ -221,6 +226,33 @@ __device__ __forceinline__ uint32_t upper2(uint32_t a, uint32_t b) {
   return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
 
+// Eight codes of a dword less their zero point, as bf16: q - z with ZERO, where `less` holds
+// 128 - z in each byte; else 16 (q - 8), a code moved to the upper half of its byte. Either is
+// a signed byte, whose float has its bits in the upper half.
+constexpr float kExactUnit = 0.0625f;  // of the latter
+template <bool ZERO>
+__device__ __forceinline__ bf16x8 codes_less_zero(uint32_t w, uint32_t less) {
+  uint32_t lo, hi;
+  if (ZERO) {
+    lo = ((w & 0x0f0f0f0fu) + less) ^ 0x80808080u;
+    hi = (((w >> 4) & 0x0f0f0f0fu) + less) ^ 0x80808080u;
+  } else {
+    lo = ((w << 4) ^ 0x80808080u) & 0xf0f0f0f0u;
+    hi = (w ^ 0x80808080u) & 0xf0f0f0f0u;
+  }
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = (float)(int8_t)(lo >> (8 * e));
+    f[4 + e] = (float)(int8_t)(hi >> (8 * e));
+  }
+  u32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    v[e] = upper2(__float_as_uint(f[2 * e]), __float_as_uint(f[2 * e + 1]));
+  return as_bf16x8(v);
+}
+
 // Eight elements of X from column i, as PARTS bf16 operands: bf16 as they are, fp32
 // cut in three (each part the upper 16 bits of what is left: exact, and of no
 // larger magnitude, so nothing overflows; an infinity's rest is NaN, and such
@@ -348,7 +380,8 @@ __global__ __launch_bounds__(256) void nibble_x_kernel(const T* __restrict__ X, 
 // has done so in memory (xop): a wave's load is 1 KiB in a row, where reading the rows
 // of X themselves meets few of the L2's channels (strides of powers of two) and
 // takes as long for one row as for sixteen.
-template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
+// EXACT: zero points are taken off the codes, else off the sums (bf16 X and Y alone).
+template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS, bool EXACT>
 __global__ __launch_bounds__(512) void nibble_product_kernel(
     const T* __restrict__ X, int64_t ldx, const bf16x8* __restrict__ xop, int ntiles,
     const uint8_t* __restrict__ image, int64_t scales_at, int64_t zeros_at, void* __restrict__ Y,
@@ -392,7 +425,10 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
       for (int g = 0; g < GPT; ++g) {
         f.sc[d][g] = load_weights<STREAM>(
             reinterpret_cast<const u32x2*>(scales + tile * (16 * GPT)) + quad * GPT + g);
-        if (ZERO)
+        if (ZERO && EXACT)  // of the output whose codes the lane holds
+          f.zp[d][g] = load_weights<STREAM>(zeros + tile * (16 * GPT) +
+                                            ((col / 4) * GPT + g) * 4 + col % 4);
+        else if (ZERO)  // of the four whose sums it will hold
           f.zp[d][g] = load_weights<STREAM>(
               reinterpret_cast<const uint32_t*>(zeros + tile * (16 * GPT)) + quad * GPT + g);
       }
@@ -414,10 +450,7 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
   };
   const bf16x8* xs = reinterpret_cast<const bf16x8*>(sums);
   const int lds_rows = N - 16 * nt0 < 16 ? (int)(N - 16 * nt0) : 16;  // of X in LDS
-  // The two chains of fp32 are joined when both are finished: begun from the other, the first
-  // would carry its size through every addition (1 x 561 x 10240: 4.3e-7 of the result
-  // instead of 2.7e-7). bf16 saves the addition.
-  constexpr bool APART = sizeof(T) == 4;
+  // what the sums of x q start from: -z sum x
   auto start = [](const Frag& f, int d, int g, int r, float one) {
     return ZERO ? -(float)((f.zp[d][g] >> (8 * r)) & 255u) * one : one;
   };
@@ -437,7 +470,8 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
               xp[s][t][p] = xs[((it * 4 + g * STEPS + s) * P + p) * 4 * lds_rows];
             else
               xp[s][t][p] = x.v[t][g * STEPS + s][p];
-            one[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xp[s][t][p], one[t], 0, 0, 0);
+            if (!EXACT)
+              one[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xp[s][t][p], one[t], 0, 0, 0);
           }
       }
 #pragma unroll
@@ -447,10 +481,13 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            sum[t][r] = APART ? 0.0f : start(f, d, g, r, one[t][r]);
+            sum[t][r] = EXACT ? 0.0f : start(f, d, g, r, one[t][r]);
+        uint32_t less = 0;
+        if (ZERO && EXACT) less = 0x80808080u - __builtin_amdgcn_perm(0, f.zp[d][g], 0u);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          const bf16x8 q = codes_bf16(f.code[d][g * STEPS + s]);
+          const uint32_t w = f.code[d][g * STEPS + s];
+          const bf16x8 q = EXACT ? codes_less_zero<ZERO>(w, less) : codes_bf16(w);
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -463,10 +500,7 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float v = APART ? sum[t][r] + start(f, d, g, r, one[t][r]) : sum[t][r];
-            acc[d][t][r] = fmaf(sf[r], v, acc[d][t][r]);
-          }
+          for (int r = 0; r < 4; ++r) acc[d][t][r] = fmaf(sf[r], sum[t][r], acc[d][t][r]);
       }
     }
   };
@@ -528,7 +562,7 @@ __global__ __launch_bounds__(512) void nibble_product_kernel(
     for (int r = 0; r < 4; ++r) {
       const int64_t o = o0 + r;
       const bool live = n < N && o < O;
-      float v = y[r];
+      float v = EXACT && !ZERO ? y[r] * kExactUnit : y[r];
       // Not finite: an infinity or NaN in X, or a part of the sum past the range that the
       // whole stays within. Taken again as the formula says.
       for (uint64_t again = __ballot(live && !(fabsf(v) < INFINITY)); again; again &= again - 1) {
@@ -561,6 +595,7 @@ struct ProductArgs {
   int64_t ldy, N, O, I;
   NibbleLayout L;
   int lds_tiles, y_dt, act;
+  bool exact;
   hipStream_t stream;
 };
 
@@ -599,8 +634,8 @@ int lds_tiles(int64_t N, int64_t otiles, int64_t itiles, int x_dt) {
   return N == 1 ? 4 : 0;
 }
 
-template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
-hipError_t launch_product_as(const ProductArgs& a) {
+template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS, bool EXACT>
+hipError_t launch_product_kernel(const ProductArgs& a) {
   // Eight waves share the input tiles; without X in LDS four where two row tiles or four output
   // tiles take more than 128 registers, so that two or three workgroups of them fit where one
   // of eight would (32 x 3072 x 10240: 12.4 us with eight, 11.2 with four; fp32 32 x 8192 x
@@ -613,7 +648,7 @@ hipError_t launch_product_as(const ProductArgs& a) {
     const size_t x = x_lds_bytes(a.N, a.L.itiles, sizeof(T) == 4 ? 0 : 1);
     if (x > lds) lds = x;
   }
-  const auto kernel = nibble_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS>;
+  const auto kernel = nibble_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS, EXACT>;
   if (lds > 64 * 1024) {  // above the default limit: raised once per device and kernel
     static PerDeviceOnce once;
     const hipError_t e = once_per_device(once, [&] {
@@ -627,6 +662,13 @@ hipError_t launch_product_as(const ProductArgs& a) {
                      ntiles, a.image, (int64_t)a.L.scales, (int64_t)a.L.zeros, a.Y, a.ldy, a.N,
                      a.O, a.I, a.L.otiles, (int)a.L.itiles, a.y_dt, a.act);
   return hipGetLastError();
+}
+
+template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
+hipError_t launch_product_as(const ProductArgs& a) {
+  if constexpr (sizeof(T) == 2)
+    if (!a.exact) return launch_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS, false>(a);
+  return launch_product_kernel<T, GPT, ZERO, NT, TD, STREAM, XLDS, true>(a);
 }
 
 // Above three quarters of the 256 MiB cache that the dies share a matrix does not stay there
@@ -754,7 +796,7 @@ hipError_t launch_nibble_product(const void* X, int64_t ldx, const void* image, 
                                  bool with_zeros, int x_dt, int y_dt, int act, void* workspace,
                                  hipStream_t stream) {
   ProductArgs a{X,   ldx, nullptr, static_cast<const uint8_t*>(image), Y,  ldy, N, O,
-                I,   layout_of(O, I, G), 0, y_dt, act, stream};
+                I,   layout_of(O, I, G), 0, y_dt, act, x_dt == 0 || y_dt == 0 || act == 0, stream};
   a.lds_tiles = lds_tiles(N, a.L.otiles, a.L.itiles, x_dt);
   if (a.lds_tiles == 0) {
     bf16x8* xop = static_cast<bf16x8*>(workspace);
