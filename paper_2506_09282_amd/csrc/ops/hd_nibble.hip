@@ -160,17 +160,22 @@ __global__ __launch_bounds__(64) void nibble_quantize_kernel(const T* __restrict
       for (int u = 0; u < 4; ++u)
         if (u == t) l = fminf(l, lo[u]), h = fmaxf(h, hi[u]);
     }
-    const float span = with_zeros ? (h - l) / 15.0f : fmaxf(h, -l) / 7.0f;
+    float span = with_zeros ? (h - l) / 15.0f : fmaxf(h, -l) / 7.0f;
+    if (with_zeros && h < INFINITY && l > -INFINITY && !(span < INFINITY))
+      span = h / 15.0f - l / 15.0f;  // (the difference alone is past fp32's range)
     bf16raw sb = to_bf16(span);  // the codes are taken by the scale that is kept
     const float sc = bf16_to_f32(sb);
     const bool bad = !(sc < INFINITY);
     if (bad) sb = 0x7fc0;  // NaN
-    const float r = sc > 0.0f && !bad ? 1.0f / sc : 0.0f;
-    const float z = with_zeros ? fminf(fmaxf(rintf(-l * r), 0.0f), 15.0f) : 8.0f;
+    // a scale below 2^-128 has no inverse in fp32: its weights, 2^4 times as large at most, are
+    // moved up first, which is exact
+    const float up = sc < 0x1p-126f ? 0x1p24f : 1.0f;
+    const float r = sc > 0.0f && !bad ? 1.0f / (sc * up) : 0.0f;
+    const float z = with_zeros ? fminf(fmaxf(rintf(-l * up * r), 0.0f), 15.0f) : 8.0f;
     uint32_t w = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float q = fminf(fmaxf(rintf(v[s][e] * r) + z, 0.0f), 15.0f);
+      const float q = fminf(fmaxf(rintf(v[s][e] * up * r) + z, 0.0f), 15.0f);
       w |= (uint32_t)q << (4 * nibble_of(e));
     }
     packed[s] = w;
