@@ -205,7 +205,10 @@ def _raise(st: int, where: str):
 
 # Workspaces are cached per (device, stream, size); the library leaves the
 # parts that must start at zero zeroed after every call of the same shape,
-# so a cached buffer is only zeroed when first allocated for that key.
+# so a cached buffer is only zeroed when first allocated for that key. A call that is
+# captured into a graph has a workspace of that graph's instead, zeroed by each replay: a
+# graph's memory holds nothing before its first replay, and replays may run beside
+# eager calls and other graphs.
 _ws_cache: dict = {}
 
 
@@ -219,6 +222,8 @@ def _workspace(device, nbytes: int, key):
     torch = _torch()
     if nbytes == 0:
         return None
+    if torch.cuda.is_current_stream_capturing():
+        return torch.zeros(nbytes, dtype=torch.uint8, device=device)
     k = (device.index, _stream_ptr(device), key, nbytes)
     ws = _ws_cache.get(k)
     if ws is None:
