@@ -218,15 +218,17 @@ def _need(query: str, device: int, *sizes) -> int:
     return int(getattr(lib(), query)(*sizes))
 
 
-def _workspace(device, nbytes: int, key):
+def _workspace(device, nbytes: int, key, grows: bool = False):
+    """A zeroed workspace of ``nbytes``, or with ``grows`` (for calls that leave all of it
+    zeroed, so that one serves every shape) of at least that."""
     torch = _torch()
     if nbytes == 0:
         return None
     if torch.cuda.is_current_stream_capturing():
         return torch.zeros(nbytes, dtype=torch.uint8, device=device)
-    k = (device.index, _stream_ptr(device), key, nbytes)
+    k = (device.index, _stream_ptr(device), key, 0 if grows else nbytes)
     ws = _ws_cache.get(k)
-    if ws is None:
+    if ws is None or ws.numel() < nbytes:
         ws = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         _ws_cache[k] = ws
     return ws
@@ -758,7 +760,7 @@ def logprobs(scores, y=None, top: int = 0, scale: float = 1.0, mask=None,
     if ws is None:
         need = _need("hd_logprobs_workspace_bytes", index, N, K, dt)
         if need:
-            ws = _workspace(device, need, ("logprobs", N, K, dt))
+            ws = _workspace(device, need, "logprobs", grows=True)
     st = lib().hd_logprobs(scores.data_ptr(), ld, mptr, ldm, yptr, scale,
                            at + 12 * N if yptr is not None else None, at + 8 * N, at,
                            at + 16 * N if each else None, at + 16 * N + 4 * each if each else None,
