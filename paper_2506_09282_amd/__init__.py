@@ -761,6 +761,8 @@ def logprobs(scores, y=None, top: int = 0, scale: float = 1.0, mask=None,
         need = _need("hd_logprobs_workspace_bytes", index, N, K, dt)
         if need:
             ws = _workspace(device, need, "logprobs", grows=True)
+    elif ws.dtype != torch.uint8 or ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the scores' device")
     st = lib().hd_logprobs(scores.data_ptr(), ld, mptr, ldm, yptr, scale,
                            at + 12 * N if yptr is not None else None, at + 8 * N, at,
                            at + 16 * N if each else None, at + 16 * N + 4 * each if each else None,

@@ -50,3 +50,16 @@ def test_results_of_split_rows():
         # |z| < 16, and the sum of K terms
         assert bool(((got.entropy.cpu().double() - ref[1]).abs()
                      <= 16 * (K / 64 + 72) * P.U32 * 2).all())
+
+
+def test_refused_workspaces():
+    """The kernels write to it: memory of the host, or of other tensors between, is refused."""
+    hd = hd_gpu()
+    s = torch.randn(2, 30000, generator=torch.Generator().manual_seed(1)).cuda()
+    need = hd.logprobs_workspace_bytes(2, 30000, F32)
+    assert need > 0
+    for bad in (torch.zeros(need, dtype=torch.uint8),
+                torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2],
+                torch.zeros(need, dtype=torch.int32, device="cuda")):
+        with pytest.raises(ValueError, match="workspace"):
+            hd.logprobs(s, workspace=bad)
