@@ -362,21 +362,18 @@ __device__ __forceinline__ void x_operands(const T* row, int64_t ch, int64_t I,
 }
 
 // X as operands in memory: [input tile][tile of 16 rows][step][part][lane]. Rows past N
-// are zero.
+// are zero. A workgroup lays out an input tile (x) of 16 rows (y).
 template <typename T>
 __global__ __launch_bounds__(256) void nibble_x_kernel(const T* __restrict__ X, int64_t ldx,
-                                                       int64_t N, int64_t I, int ntiles,
-                                                       int64_t total, bf16x8* out) {
+                                                       int64_t N, int64_t I, bf16x8* out) {
   constexpr int P = XLoad<T>::kParts;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const int lane = (int)at & 63, s = (int)(at >> 6) & 3;
-  const int64_t tile = at >> 8;
-  const int64_t n = tile % ntiles * 16 + lane % 16;
+  const int lane = threadIdx.x & 63, s = threadIdx.x >> 6;
+  const int64_t it = blockIdx.x, nt = blockIdx.y, n = nt * 16 + lane % 16;
   bf16x8 parts[P] = {};
-  if (n < N) x_operands(X + n * ldx, tile / ntiles * 16 + 4 * s + lane / 16, I, parts);
+  if (n < N) x_operands(X + n * ldx, it * 16 + 4 * s + lane / 16, I, parts);
 #pragma unroll
-  for (int p = 0; p < P; ++p) out[((at >> 6) * P + p) * 64 + lane] = parts[p];
+  for (int p = 0; p < P; ++p)
+    out[(((it * gridDim.y + nt) * 4 + s) * P + p) * 64 + lane] = parts[p];
 }
 
 // NT tiles of 16 rows of X, TD tiles of 16 outputs, GPT groups in an input tile.
@@ -604,6 +601,8 @@ struct ProductArgs {
   hipStream_t stream;
 };
 
+constexpr int64_t kMaxThreads = (int64_t(1) << 32) - 1;  // of a launch
+
 constexpr int parts_of(int x_dt) { return x_dt == 0 ? 3 : 1; }
 
 // Bytes of X as operands in LDS, up to 16 rows.
@@ -662,11 +661,24 @@ hipError_t launch_product_kernel(const ProductArgs& a) {
     });
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(cdiv(a.L.otiles, TD) * cdiv(ntiles, NT))),
-                     dim3(64 * waves), lds, a.stream, static_cast<const T*>(a.X), a.ldx, a.xop,
-                     ntiles, a.image, (int64_t)a.L.scales, (int64_t)a.L.zeros, a.Y, a.ldy, a.N,
-                     a.O, a.I, a.L.otiles, (int)a.L.itiles, a.y_dt, a.act);
-  return hipGetLastError();
+  // A launch holds fewer than 2^32 threads; outputs past those of the first take more. (The
+  // offsets of scales and zero points count from the codes that a launch begins at.)
+  const int64_t rows = cdiv(ntiles, NT), step = kMaxThreads / (64 * waves * rows) * TD;
+  for (int64_t t0 = 0; t0 < a.L.otiles; t0 += step) {
+    const int64_t tiles = t0 * a.L.itiles, left = a.L.otiles - t0;
+    const int64_t here = left < step ? left : step;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(cdiv(here, TD) * rows)), dim3(64 * waves), lds,
+                       a.stream, static_cast<const T*>(a.X), a.ldx, a.xop, ntiles,
+                       a.image + tiles * 1024,
+                       (int64_t)a.L.scales + tiles * (16 * GPT * 2 - 1024),
+                       (int64_t)a.L.zeros + tiles * (16 * GPT - 1024),
+                       static_cast<char*>(a.Y) + t0 * kTileO * (a.y_dt == 0 ? 4 : 2), a.ldy, a.N,
+                       a.O - t0 * kTileO < here * kTileO ? a.O - t0 * kTileO : here * kTileO, a.I,
+                       here, (int)a.L.itiles, a.y_dt, a.act);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, int GPT, bool ZERO, int NT, int TD, bool STREAM, bool XLDS>
@@ -806,14 +818,13 @@ hipError_t launch_nibble_product(const void* X, int64_t ldx, const void* image, 
   if (a.lds_tiles == 0) {
     bf16x8* xop = static_cast<bf16x8*>(workspace);
     const int ntiles = (int)cdiv(N, 16);
-    const int64_t total = a.L.itiles * ntiles * 256;
-    const dim3 grid((unsigned)cdiv(total, 256)), block(256);
+    const dim3 grid((unsigned)a.L.itiles, (unsigned)ntiles), block(256);
     if (x_dt == 0)
       hipLaunchKernelGGL(nibble_x_kernel<float>, grid, block, 0, stream,
-                         static_cast<const float*>(X), ldx, N, I, ntiles, total, xop);
+                         static_cast<const float*>(X), ldx, N, I, xop);
     else
       hipLaunchKernelGGL(nibble_x_kernel<bf16raw>, grid, block, 0, stream,
-                         static_cast<const bf16raw*>(X), ldx, N, I, ntiles, total, xop);
+                         static_cast<const bf16raw*>(X), ldx, N, I, xop);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.xop = xop;

@@ -122,3 +122,30 @@ def test_checkpoint_and_products_of_far_rows():
     del far
     far = far_rows(torch.zeros_like(H))
     assert same(hd.ckpt_load(near_kept, out=far), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_products_of_more_outputs_than_a_launch_holds(dtype):
+    """4096 rows and 4.2 million outputs: 2^32 threads and more, 34 GB of results. Whole numbers:
+    exact in every order of the sums, one rounding is left."""
+    hd = hd_gpu()
+    N, inner, group = 4096, 400, 32
+    outer = 16 * 4 * 65536 + 16 * 700 + 5      # 65536 workgroups of four tiles, and more
+    announce(f"nibble {N}x{outer}x{inner} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    codes = torch.randint(0, 256, (outer, inner // 2), dtype=torch.uint8, generator=g,
+                          device="cuda")
+    ngroups = -(-inner // group)
+    ones = torch.ones(outer, ngroups, dtype=BF16, device="cuda")
+    z = torch.randint(0, 16, (outer, ngroups), dtype=torch.uint8, generator=g, device="cuda")
+    X = torch.randint(-3, 4, (N, inner), generator=g, device="cuda").to(dtype)
+    for zeros in (z, None):
+        w = hd.nibble_pack(codes, ones, zeros, inner=inner, group=group)
+        Y = hd.nibble_product(X, w, dtype=BF16)
+        for o in list(range(0, outer, 524288)) + [outer - 20000]:
+            part = slice(o, min(outer, o + 20000))
+            W = hd.nibble_unpack(hd.nibble_pack(codes[part], ones[part],
+                                                None if zeros is None else zeros[part],
+                                                inner=inner, group=group))
+            assert torch.equal(Y[:, part], (X.float() @ W.t()).to(BF16))
+        del Y, w
