@@ -306,3 +306,35 @@ def test_refusals():
                 lambda: hd.ckpt_class_grad(dS.int(), kept)):
         with pytest.raises(TypeError):
             bad()
+
+
+# the three parts of fp32 as rows of their own, laid out in memory: four row tiles, and few
+# classes in a call that is too large for the workgroups to cut dS themselves
+@pytest.mark.parametrize("D,K", [(40, 33), (40, 37), (40, 42), (300, 42), ((1 << 24) + 70, 3),
+                                 ((1 << 24) + 70, 10), ((1 << 25) + 70, 26)])
+def test_fp32_gradients_laid_out_in_full(D, K):
+    """Every bit of an fp32 dS counts there too: one row, one group, q s = 127."""
+    hd = hd_gpu()
+    announce(f"class grad in full 1x{D}x{K}")
+    dS = torch.randn(1, K, generator=torch.Generator().manual_seed(K))
+    dS[0, 0], dS[0, 1], dS[0, 2] = 1.0 + 2.0 ** -23, 16777215.0, -1e-30
+    H = torch.full((1, D), 127.0, device="cuda")
+    got = hd.ckpt_class_grad(dS.cuda(), hd.ckpt_store(H))
+    # as above: each part times 127 is exact and the sum of three parts is rounded twice
+    ref = dS.double().t().cuda() * 127.0
+    assert bool(((got.double() - ref).abs() <= 2 * P.U32 * ref.abs()).all())
+
+
+@pytest.mark.parametrize("K", [3, 10, 26, 33, 42, 64])
+def test_fp32_gradients_of_whole_groups_in_full(K):
+    """One row of 64 holds something: the others add exact zeros, wherever it lies."""
+    hd = hd_gpu()
+    N, D = 200, 70
+    dS = torch.zeros(N, K)
+    at = (torch.arange(K) * 29 + 3) % N
+    v = torch.randn(K, generator=torch.Generator().manual_seed(K))
+    v[0], v[1], v[2] = 1.0 + 2.0 ** -23, 16777215.0, -1e-30
+    dS[at, torch.arange(K)] = v
+    got = hd.ckpt_class_grad(dS.cuda(), hd.ckpt_store(torch.full((N, D), 127.0).cuda())).cpu()
+    ref = v.double()[:, None] * 127.0
+    assert bool(((got.double() - ref).abs() <= 2 * P.U32 * ref.abs()).all())
