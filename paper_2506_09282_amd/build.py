@@ -8,6 +8,7 @@ from __future__ import annotations
 import concurrent.futures as cf
 import glob
 import os
+import re
 import subprocess
 import sys
 
@@ -29,9 +30,30 @@ CFLAGS = [
 ]
 
 
+# Kernels under csrc/ops keep their accumulators and loads in flight in registers. Instances that
+# did not fit (scratch memory in use) have given wrong sums with this compiler, without
+# an error, so a build in which one appears is refused.
+OPS = os.path.join(CSRC, "ops")
+RESOURCES = "-Rpass-analysis=kernel-resource-usage"
+
+
+def spilling(remarks: str) -> list:
+    """The kernels that use scratch memory, from the compiler's resource remarks."""
+    names, name = [], "?"
+    for line in remarks.splitlines():
+        m = re.search(r"Function Name: (\S+)", line)
+        if m:
+            name = m.group(1)
+        m = re.search(r"ScratchSize \[bytes/lane\]: (\d+)|Dynamic Stack: (True)", line)
+        if m and m.group(1) != "0":
+            names.append(name)
+    return names
+
+
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
-    cmd = [HIPCC, *CFLAGS, "-c", src, "-o", obj]
+    in_registers = os.path.dirname(os.path.abspath(src)) == OPS
+    cmd = [HIPCC, *CFLAGS, *([RESOURCES] if in_registers else []), "-c", src, "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -39,6 +61,12 @@ def _compile(src: str, verbose: bool) -> str:
                     if "packed-fp32-ops" not in l and "not a recognized feature" not in l)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{out}")
+    if in_registers:
+        spilled = spilling(out)
+        if spilled:
+            os.remove(obj)
+            raise RuntimeError(f"{src}: kernels that do not fit their registers: {spilled}")
+        out = "\n".join(l for l in out.splitlines() if "warning:" in l)  # (not the remarks)
     if verbose and out.strip():
         print(out, flush=True)
     return obj
