@@ -53,15 +53,22 @@ __device__ __forceinline__ float wave_sum(float v) {
 // Cross-workgroup hand-off without cache write-back.
 //
 // Data that one workgroup passes to another moves only through device-scope
-// atomic read-modify-writes, which are performed at a single coherence point
-// for each address. A workgroup publishes with no-return atomics, waits until
-// they are performed (s_waitcnt, all counters to zero) and only then takes a
-// ticket with a relaxed device-scope fetch-add; the workgroup that draws the
-// last ticket reads every published value with an atomic exchange against 0,
-// which both observes all performed atomics and leaves the slot zeroed for
-// the next call. A device-scope release fence would also work, but on gfx950
-// it writes back the whole L2 (buffer_wbl2) in every workgroup, which costs
-// tens of microseconds per launch.
+// atomic operations, which are performed at a single coherence point for each
+// address. A workgroup publishes, waits until that is performed (s_waitcnt, all
+// counters to zero) and only then takes a ticket with a relaxed device-scope
+// fetch-add; the workgroup that draws the last ticket reads what was published.
+// A device-scope release fence would also work, but on gfx950 it writes back
+// the whole L2 (buffer_wbl2) in every workgroup, which costs tens of
+// microseconds per launch.
+//
+// * Slots that several workgroups add to take no-return atomic adds and are read
+//   with an atomic exchange against 0, which leaves them zeroed for the next call.
+// * Slots of one writer (the parts of a split row of log probabilities) take
+//   atomic stores and are read with atomic loads, both relaxed and of device
+//   scope: they pass the caches of a single die, the wait covers the stores, and
+//   a load is issued only after the last ticket was drawn. Unlike exchanges, the
+//   loads are in flight together. What clears such slots afterwards may be plain
+//   stores: nobody reads them in the same launch, and its end makes them visible.
 __device__ __forceinline__ void wait_own_memory_ops() { __builtin_amdgcn_s_waitcnt(0); }
 __device__ __forceinline__ unsigned take_ticket(unsigned* counter) {
   return __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

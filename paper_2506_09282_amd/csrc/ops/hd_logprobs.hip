@@ -640,7 +640,8 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_long_kernel(LogprobsArgs 
         }
       }
     }
-    __syncthreads();  // all is read: left zeroed
+    // all is read: left zeroed (plain stores, which the end of the launch makes visible)
+    __syncthreads();
     for (int64_t i = threadIdx.x; i < (int64_t)sp.parts * kPartWords; i += kThreads)
       words[i] = 0;
   }
