@@ -303,7 +303,8 @@ const char *hd_infer_kernel(int64_t N, int64_t F, int64_t D, int64_t K, hd_dtype
  * that a part of a wider matrix can be passed. Their dtypes are HD_F32 and
  * HD_BF16 (HD_I8 gives HD_ERR_UNSUPPORTED). Results do not depend on the order of
  * execution: the same inputs give the same bits. Rows are independent: what
- * a row holds, NaN included, reaches no other row.
+ * a row holds, NaN included, reaches no other row (but for the 64 rows that share
+ * the scales of a checkpoint).
  *
  * Weights in 4 bits with group scales. A weight matrix of `outer` outputs and
  * `inner` inputs stands for
@@ -329,10 +330,10 @@ const char *hd_infer_kernel(int64_t N, int64_t F, int64_t D, int64_t K, hd_dtype
  * hd_nibble_product: Y[n][o] = act( sum_i X[n][i] w[o][i] ), X[N][inner] of x_dt,
  * Y[N][outer] of y_dt, sums in fp32 over the products x (code - zero), which are exact, one
  * rounding to y_dt; where X and Y are bf16 and act is the identity, the sums of x code and of
- * x zero are taken apart (which that rounding covers). An X of fp32 is used in full. `zeros` says whether the
- * image was made with zero points. Made for few rows, a single reading or a
- * request batch. workspace: hd_nibble_workspace_bytes(...) bytes (0 for a single row of
- * usual length), contents irrelevant before and undefined after the call.
+ * x zero are taken apart (which that rounding covers). An X of fp32 is used in full, but for
+ * bits below 2^-133. `zeros` says whether the image was made with zero points. Made for few
+ * rows, a single reading or a request batch. workspace: hd_nibble_workspace_bytes(...) bytes
+ * (0 for a single row of usual length), contents irrelevant before and undefined after the call.
  * Limits: outer, inner <= 2^30, ceil(outer/16) * ceil(inner/128) <= 2^24,
  * N <= 4096.
  */
@@ -386,7 +387,8 @@ hd_status hd_logprobs(const void *scores, int64_t ld, const uint8_t *mask, int64
  *   sum_n g_logp[n] logp[n] + g_entropy[n] entropy[n]:
  *   dscores[n][k] = scale ( g_logp (1[k = y] - p_k) - g_entropy p_k (t_k + entropy) ),
  * p_k = exp(t_k), from the scores, mask, y and scale of hd_logprobs and its stats and
- * entropy. Classes that take no part get 0 (NaN in a row whose stats are NaN);
+ * entropy. Classes that take no part get 0 (NaN in a row whose stats are NaN, or whose
+ * g_logp or g_entropy is not finite);
  * g_logp is read as 0 where no class is asked for. g_logp, g_entropy and y may be
  * NULL (0, 0, none). dscores has the scores' dtype and row stride ldd; it may be
  * the scores' own memory (same stride).
@@ -411,7 +413,8 @@ hd_status hd_logprobs_grad(const void *scores, int64_t ld, const uint8_t *mask, 
  * vectors, from the scores' gradient dS[N][K] (row stride lds) and the
  * checkpoint of H:
  *   dC[k][d] = sum_n dS[n][k] * (q s)[n][d]      fp32 [K][D], contiguous;
- * accumulate != 0 adds to what dC holds. Products are exact, sums fp32.
+ * accumulate != 0 adds to what dC holds. Products are exact (a dS of fp32 is used in
+ * full, but for bits below 2^-133), sums fp32.
  * workspace: hd_ckpt_class_grad_workspace_bytes(...) bytes (0 is possible), contents
  * irrelevant before and undefined after the call.
  * Limits: N <= 65535 * 64, D <= 2^30, K <= 2^20, and ceil(N/64) * ceil(K/32) < 2^23.

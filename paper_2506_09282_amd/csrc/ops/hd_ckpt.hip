@@ -20,13 +20,14 @@
 // operand (a small launch), so that the product's loop holds no transposition; in a short
 // call each workgroup does that for itself.
 //
-// Measured (kernels alone): 4096 x 10240 fp32 kept 33.5 us (212 MB, 6.3 TB/s) and taken back 30.6
-// (6.9 TB/s), as a copy with such loads and stores. Gradient, 65536 x 10240 x 26 fp32: 145-165 us,
+// Measured: 4096 x 10240 fp32 kept 33.9 us (kernel; 212 MB, 6.3 TB/s) and taken back 30.8 (6.9
+// TB/s), as a copy with such loads and stores. Gradient, 65536 x 10240 x 26 fp32: 164 to 177 us for
+// a call's three launches in a row of calls (the product alone 174 to 192 under the profiler),
 // where reading the 713 MB takes 100. Three matrix instructions for each step, a fifth of their
-// rows past the 26 classes, keep the matrix units busy for 46% of the time and the bytes' way
-// to bf16 the vector units for 47%: both run beside the loads, but hardly beside each other.
-// 2999 x 10000 x 100 bf16, 36 MB: 20 us; 24 MB of partial sums of six slices are written beside
-// them and read again by the join.
+// rows past the 26 classes, keep the matrix units busy for 44% of the time and the bytes' way
+// to bf16 the vector units for 44%: both run beside the loads, but hardly beside each other.
+// 2999 x 10000 x 100 bf16, 36 MB: 21 to 23 us, of 29 for the call; 24 MB of partial sums of six
+// slices are written beside them and read again by the join.
 #include <type_traits>
 
 #include "hd_ops.hpp"
@@ -557,7 +558,9 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t K, int dt) {
   // Three rows for each class where that is one tile instead of three parts of one
   // (65536 x 10240 x 10: 127 us instead of 151) or four tiles instead of six parts (32768 x
   // 10240 x 40: 136 instead of 147); two tiles instead of three parts lose (K = 20: 170 instead
-  // of 160).
+  // of 160), each side in the tiling that its count of parts and tiles gives it below: four waves
+  // of one column tile against eight of two. (Two tiles in the tiling of the other side were
+  // not measured.)
   p.fold = dt == 0 && (K <= 10 || (K > 32 && K <= 42));
   // A short call saves the launch that lays dS out; each workgroup then cuts all classes of its
   // groups by itself, which pays while there are few (K = 26, D = 10000, fp32: 1000 rows 15.0

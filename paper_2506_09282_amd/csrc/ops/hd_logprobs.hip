@@ -24,13 +24,14 @@
 // The gradient is a pass over the elements: statistics and entropy are its inputs, so it
 // reads each score once and needs no reduction.
 //
-// Measured (kernels alone): 65536 x 26 fp32 top 3, 9.7 MB: 6.6 us, launch and the selection of
-// three among eight lanes. 1 x 131072 fp32 top 20: 11.4 us, 64 parts of one step: a load,
-// a sort, a ticket and the join of 64 lists, each waiting for the one before. 2048 x 100003
-// bf16 top 8 with a mask of bytes, 615 MB: 126 us, 4.9 TB/s; the vector units, busy for 87% of
-// the time, bound it: 16 instructions an element, 9 where rows start at words and no mask is
-// given. Gradient, 4096 x 65536 bf16, 1.07 GB: 189 us, 5.7 TB/s, against 5.6 to 6.4 for a copy
-// with such loads and stores.
+// Measured: 65536 x 26 fp32 top 3, 9.7 MB: kernel 6.8 us, launch and the selection of
+// three among eight lanes. 1 x 131072 fp32 top 20: kernel 11 to 12 us, 64 parts of one step: a
+// load, a sort, a ticket and the join of 64 lists, each waiting for the one before. 2048 x 100003
+// bf16 top 8 with a mask of bytes, 615 MB: 127 to 136 us in a row of calls (138 to 150 under the
+// profiler), 4.5 to 4.9 TB/s; the vector units, busy for 86% of the time, bound it: 16
+// instructions an element, 9 where rows start at words and no mask is given. Gradient, 4096 x 65536
+// bf16, 1.07 GB: 193 to 199 us in a row of calls (193 to 211 under the profiler), 5.4 to 5.6
+// TB/s, against 5.6 to 6.4 for a copy with such loads and stores.
 #include "hd_ops.hpp"
 
 // A product that is rounded is meant to be (q = fl(c m) is taken off itself below); what is

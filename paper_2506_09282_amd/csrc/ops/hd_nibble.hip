@@ -32,11 +32,11 @@
 // one row of X leaves nothing else to fill the chip with: 57344 outputs are 1792 workgroups
 // at TD = 2, 1000 outputs 32.
 //
-// Measured (kernel alone): bf16 1 x 16384 x 57344, G = 128, 484 MB: 77 us, 6.3 TB/s, where
-// reading alone gives 7.1 (the vector units are busy for 58% of the time, the matrix units for
-// 26%; 57344 x 16384 codes are fetched once, 498 MB in all). fp32 1 x 561 x 10240, 3.3 MB: 5.3
-// us, a launch and one round of loads. bf16 32 x 3072 x 10240, 18 MB: 11.0 us, a launch, six
-// rounds of loads for each wave, and 63 MB of X from the L2.
+// Measured (kernel): bf16 1 x 16384 x 57344, G = 128, 484 MB: 77 to 80 us, 6.1 to 6.3 TB/s, where
+// reading alone gives 7.1 (the vector units are busy for 57% of the time, the matrix units for
+// 26%; 57344 x 16384 codes are fetched once, 497 MB in all); fp32 136 us a call. fp32
+// 1 x 561 x 10240, 3.3 MB: 5.4 us, a launch and one round of loads. bf16 32 x 3072 x 10240, 18
+// MB: 10.7 to 11.2 us, a launch, six rounds of loads for each wave, and 63 MB of X from the L2.
 #include "hd_ops.hpp"
 
 namespace hd {
@@ -615,15 +615,16 @@ bool x_in_lds(int64_t N, int64_t itiles, int x_dt) {
 
 // Output tiles of a workgroup that keeps X in LDS; 0: X is laid out in memory. Each workgroup
 // lays X out again, so where it fills half of the LDS (fp32; bf16 gains nothing) that pays if
-// all of them run at once (1 x 16384 x 700: 16.9 us, with X in memory 24.1; 4 x 4096 x 10240 in
-// three tiles: 10.5 and 13.3; but 4 x 4096 x 28672 in four: 22.4 and 20.6), and for one row always,
-// which X in memory holds sixteen times (1 x 16384 x 57344: 122 and 157).
+// all of them run at once (1 x 16384 x 700: 18.5 us, with X in memory 24.1; 4 x 4096 x 10240 in
+// three tiles: 11.6 and 14.4; but 4 x 4096 x 28672 in four: 26.3 and 21.6), and for one row always,
+// which X in memory holds sixteen times (1 x 16384 x 57344: 136 and 154).
 int lds_tiles(int64_t N, int64_t otiles, int64_t itiles, int x_dt) {
   if (x_in_lds(N, itiles, x_dt)) return 2;
   // More rows: each workgroup a tile of 16, where the workgroups run at once and together
-  // lay out little, for a launch less (20 x 1000 x 8192 bf16: 9.1 us, with X in memory 10.8; fp32
-  // 64 x 617 x 4096 9.1 and 10.8, 64 x 1280 x 2000 9.0 and 11.3; but 64 x 2000 x 4096 bf16 12.8
-  // and 11.4, 20 x 617 x 10240 fp32 13.0 and 11.8).
+  // lay out little, for a launch less of the host's time (20 x 1000 x 8192 bf16: 9.1 us a call,
+  // with X in memory 10.8; fp32 64 x 617 x 4096 8.9 and 11.1, 64 x 1280 x 2000 8.8 and 11.0, though
+  // inside a graph 8.7 and 7.4, 8.0 and 7.1; but 64 x 2000 x 4096 bf16 12.8 and 11.4,
+  // 20 x 617 x 10240 fp32 13.3 and 11.0).
   const size_t bytes = x_lds_bytes(N, itiles, x_dt);
   const int64_t cus = num_cus();
   if (N > 16) {
@@ -643,7 +644,7 @@ hipError_t launch_product_kernel(const ProductArgs& a) {
   // Eight waves share the input tiles; without X in LDS four where two row tiles or four output
   // tiles take more than 128 registers, so that two or three workgroups of them fit where one
   // of eight would (32 x 3072 x 10240: 12.4 us with eight, 11.2 with four; fp32 32 x 8192 x
-  // 16384, four output tiles: 40 and 36).
+  // 16384, four output tiles: 43.6 and 40.9).
   const int most = !XLDS && (NT == 2 || TD > 2) ? 4 : 8;
   const int waves = a.L.itiles < most ? (int)a.L.itiles : most;
   const int ntiles = (int)cdiv(a.N, 16);
@@ -697,8 +698,8 @@ constexpr size_t kStreamBytes = size_t(192) << 20;
 // X laid out in memory is read once for each workgroup's output tiles, and that weighs more
 // than the codes: four tiles (WIDE) instead of two halve it, but leave half the workgroups.
 // * fp32: where two tiles make more workgroups than compute units, of which each holds
-//   one (16 x 4096 x 10240: 13.6 us, with two tiles 18.0; 64 x 4096 x 16384: 43 and 67; but 16 x
-//   4096 x 8192, 256 workgroups: 14 and 12.9);
+//   one (16 x 4096 x 10240: 14.7 us, with two tiles 18.0; 64 x 4096 x 16384: 42 and 61; but 16 x
+//   4096 x 8192, 256 workgroups: 14.3 and 11.9);
 // * bf16: where four tiles leave 7/4 workgroups for each compute unit, and two input tiles for
 //   each wave (32 x 8192 x 28672: 32.7 us, with two 37.9; 64 x 8192 x 16384: 31.4 and 38.2; but 64
 //   x 8192 x 12288, 384 workgroups: 36 and 34).
