@@ -330,8 +330,9 @@ const char *hd_infer_kernel(int64_t N, int64_t F, int64_t D, int64_t K, hd_dtype
  * hd_nibble_product: Y[n][o] = act( sum_i X[n][i] w[o][i] ), X[N][inner] of x_dt,
  * Y[N][outer] of y_dt, sums in fp32 over the products x (code - zero), which are exact, one
  * rounding to y_dt; where X and Y are bf16 and act is the identity, the sums of x code and of
- * x zero are taken apart (which that rounding covers). An X of fp32 is used in full, but for
- * bits below 2^-133. `zeros` says whether the image was made with zero points. Made for few
+ * x zero are taken apart, whose roundings (about 2^-26 of sum |x zero scale|) can be seen beside
+ * that one only where all codes of a row are at their zero point. An X of fp32 is used in full,
+ * but for bits below 2^-133. `zeros` says whether the image was made with zero points. Made for few
  * rows, a single reading or a request batch. workspace: hd_nibble_workspace_bytes(...) bytes
  * (0 for a single row of usual length), contents irrelevant before and undefined after the call.
  * Limits: outer, inner <= 2^30, ceil(outer/16) * ceil(inner/128) <= 2^24,

@@ -13,10 +13,12 @@
 //   and a shift split eight codes and four conversions make eight bf16 values, exact.
 //   sum x*q starts from -z * sum x, which a constant operand gives once for all tiles of
 //   outputs, in the lanes that need it. Over an X of one sign both are larger than their
-//   difference, by up to 16 times its products, and so are fp32's roundings: about 2^-19 of the
-//   products' sum, where the result's own rounding is 2^-9 of it. Results that stay in
-//   fp32, or whose sign is taken, do not go this way (1 x 16384 x 57344 bf16, G = 128: 90 us a
-//   call so, 94 with exact differences; G = 64 with zero points 95 and 109);
+//   difference, and so are fp32's roundings: measured, X uniform in 0..1, at most 2^-26 of
+//   sum |x| z s (784 inputs, G = 64; 2^-28 for 16384, G = 128). Of a result in bf16, whose own
+//   rounding is 2^-9, that is less from one code in 16384 on that is off its zero point; a row
+//   with none gives such a number instead of 0. Results that stay in fp32, or whose sign is
+//   taken, do not go this way (1 x 16384 x 57344 bf16, inside a graph: G = 128 79.6 us so, 85 with
+//   exact differences; G = 64 with zero points 96 and 109; 32 x 3072 x 10240 13.1 and 13.5);
 // * fp32 X is the exact sum of three bf16 values (its 24 bits cut in three), one
 //   matrix instruction each. Products of 4 and 8 bits are exact in fp32.
 //
