@@ -178,7 +178,7 @@ def prepare(case, seed):
         X, codes, scales = _int8_inputs(case, seed)
         st = {"case": case, "X": X}
         if own:  # the model, laid out once
-            st["w"] = hd.int8_pack(codes, scales)
+            st["w"] = hd.byte_pack(codes, scales)
         else:
             st.update(codes=codes, scales=scales)
         return st
@@ -271,7 +271,7 @@ def run(state):
         if op == "dropout":
             return hd.dropout(state["X"], c["p"], state["key"], step=state["step"])
         if op == "int8":
-            return hd.int8_product(state["X"], state["w"])
+            return hd.byte_product(state["X"], state["w"])
         if op == "class_loss":
             cl = hd.class_loss(state["H"], state["C"], state["y"], scale=state["scale"],
                                mask=state["mask"])
