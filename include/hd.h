@@ -430,6 +430,101 @@ hd_status hd_ckpt_class_grad(const void *dS, int64_t lds, const void *image, flo
                              int64_t D, int64_t K, hd_dtype dt, int accumulate, void *workspace,
                              size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * Products in 8-bit integers with a scale for each row and each output. A weight
+ * matrix of `outer` outputs and `inner` inputs stands for w[o][i] = scale[o] * code[o][i],
+ * code an int8, scale fp32. Unlike the int8 model variant (HD_I8 above), whose scales stay with
+ * the caller, this gives the product itself: it encodes (outer = D, inner = F) or scores
+ * (outer = K, inner = D), or is any layer of a model in 8 bits.
+ *
+ * hd_byte_pack lays given codes out once (hd_byte_bytes bytes, 256-byte aligned, opaque):
+ * codes [outer][inner], scales [outer].
+ * hd_byte_quantize takes a matrix of numbers: W[outer][inner], or with inner_rows != 0
+ * W[inner][outer] (B as it is); rows of stride ldw. An output's scale is max |w| * fl(1/127),
+ * its codes rint(w * fl(1/scale)) in -127..127. An output that holds an infinity or NaN stands
+ * for NaN throughout; one whose largest value is below about 2^-121 for 0.
+ * hd_byte_unpack writes the weights an image stands for, [outer][inner] fp32.
+ * hd_byte_rows does the same to rows of X: codes [N][inner], contiguous, and scales [N], by that rule.
+ *
+ * hd_byte_product: Y[n][o] = act( row_scale[n] scale[o] sum_i code[n][i] w_code[o][i] ), Y[N][outer]
+ * of y_dt. X of HD_F32 or HD_BF16 is taken to codes and row scales by the rule above, within the
+ * call (row_scales is then NULL); X of HD_I8 holds codes, row_scales[N] their scales (NULL: 1
+ * throughout). The sum is exact, the scales are applied in 64 bits, and the result is rounded to
+ * fp32 and from there to y_dt; HD_ACT_HARDSIGN takes the sign before any rounding. workspace:
+ * hd_byte_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant before and undefined after the call.
+ * Limits: inner <= 131071 (|sum| < 2^31), outer, N <= 2^23, N * outer <= 2^38, row strides of X
+ * up to 2^22, ceil(outer/32) * ceil(inner/128) <= 2^23.
+ */
+size_t hd_byte_bytes(int64_t outer, int64_t inner);
+hd_status hd_byte_pack(const int8_t *codes, const float *scales, int64_t outer, int64_t inner,
+                       void *image, size_t image_bytes, hipStream_t stream);
+hd_status hd_byte_quantize(const void *W, int64_t ldw, int inner_rows, int64_t outer,
+                           int64_t inner, hd_dtype dt, void *image, size_t image_bytes,
+                           hipStream_t stream);
+hd_status hd_byte_unpack(const void *image, float *W, int64_t outer, int64_t inner,
+                         hipStream_t stream);
+hd_status hd_byte_rows(const void *X, int64_t ldx, int64_t N, int64_t inner, hd_dtype dt,
+                       int8_t *codes, float *scales, hipStream_t stream);
+size_t hd_byte_workspace_bytes(int64_t N, int64_t outer, int64_t inner, hd_dtype x_dt);
+hd_status hd_byte_product(const void *X, int64_t ldx, const float *row_scales, const void *image,
+                          void *Y, int64_t ldy, int64_t N, int64_t outer, int64_t inner,
+                          hd_dtype x_dt, hd_dtype y_dt, hd_act act, void *workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Softmax cross entropy of the classes y[N] straight from encodings H[N][D] (or any layer's
+ * outputs) and class vectors C[K][D], without the scores S = H C^T being kept:
+ *   s_k = sum_d H[n][d] C[k][d],  m = max_k s_k,  L = log sum_k exp(scale (s_k - m)),
+ *   loss = L - scale (s_y - m),  stats = {m, L}          (loss = -logp of hd_logprobs)
+ * H and C are of dt, loss and stats fp32, sums fp32 (an H or C of fp32 is used in full). mask, if not
+ * NULL, is K bytes: classes whose byte is 0 take no part, and what their vectors hold is not
+ * looked at.
+ *   - y[n] outside [0, K): no class is asked for, loss = 0. Such rows have no gradient and pass none
+ *     on, whatever they hold (rows that fill up a batch).
+ *   - a class that takes no part has loss +inf. A score of -inf takes no part either.
+ *   - a row in which nothing takes part: loss +inf (0 where no class is asked for), stats
+ *     {-inf, 0}, gradient 0.
+ *   - a row with a score of NaN or +inf in a class that takes part: loss (where a class is asked
+ *     for) and stats NaN.
+ * workspace: hd_class_loss_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant before and
+ * undefined after the call.
+ * Limits: N, K <= 2^24, D <= 2^20, N * K, N * D and K * D <= 2^38, row strides up to 2^22.
+ */
+size_t hd_class_loss_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
+hd_status hd_class_loss(const void *H, int64_t ldh, const void *C, int64_t ldc,
+                        const uint8_t *mask, const int32_t *y, float scale, float *loss,
+                        float *stats, int64_t N, int64_t D, int64_t K, hd_dtype dt,
+                        void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The gradient of sum_n g_loss[n] loss[n] with respect to H and C, from what hd_class_loss was
+ * given and its stats:
+ *   dS[n][k] = g_loss[n] scale (p_k - 1[k = y]),  p_k = exp(scale (s_k - m) - L),
+ *   dH[n][d] = sum_k dS[n][k] C[k][d],   dC[k][d] = sum_n dS[n][k] H[n][d],
+ * both of dt, contiguous [N][D] and [K][D]; either may be NULL (not both). dS is 0 in classes that
+ * take no part and rows that ask for none, and those classes' vectors and rows' encodings count
+ * as 0. For HD_BF16 dS is rounded to bf16 before the two products; sums are fp32. N == 0 clears dC.
+ */
+size_t hd_class_loss_grad_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
+hd_status hd_class_loss_grad(const void *H, int64_t ldh, const void *C, int64_t ldc,
+                             const uint8_t *mask, const int32_t *y, float scale,
+                             const float *stats, const float *g_loss, void *dH, void *dC,
+                             int64_t N, int64_t D, int64_t K, hd_dtype dt, void *workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Dropout whose mask is a function of a key, a step and a value's place, and is never stored:
+ *   Y[n][d] = X[n][d] * fl(1 / (1 - p)) where r(n, d) >= round(p 2^32), else 0,
+ * r(n, d) word d % 4 of Philox 4x32 (10 rounds) of the counter {d / 4, n, step low, step high}
+ * under the key {seed low, seed high}. The backward pass is the same call on the gradient. What
+ * is dropped may be NaN. step_at, if not NULL, is a number in device memory that is added to step,
+ * so that a captured call draws another mask at each replay. Y may be X's own memory
+ * (same stride). 0 <= p <= 1. Limits: N, D <= 2^30.
+ */
+hd_status hd_dropout(const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t N, int64_t D,
+                     double p, uint64_t seed, uint64_t step, const uint64_t *step_at, hd_dtype dt,
+                     hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

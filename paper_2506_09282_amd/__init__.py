@@ -13,6 +13,10 @@ Behind an answer: products with 4-bit weights (``nibble_*``) and log
 probabilities with entropy and alternatives (``logprobs``). Behind learning:
 their gradient (``logprobs_grad``) and encodings kept in 8 bits, from which the
 class vectors' gradient is read (``ckpt_*``).
+
+Many classes and layers in 8 bits: the cross entropy of encodings and class vectors without the
+scores, with its gradient (``class_loss``, ``class_loss_grad``), products in 8-bit integers
+(``byte_*``), and dropout without a stored mask (``dropout``).
 """
 from __future__ import annotations
 
@@ -63,6 +67,18 @@ SYMBOLS = (
     "hd_ckpt_load",
     "hd_ckpt_class_grad_workspace_bytes",
     "hd_ckpt_class_grad",
+    "hd_byte_bytes",
+    "hd_byte_pack",
+    "hd_byte_quantize",
+    "hd_byte_unpack",
+    "hd_byte_rows",
+    "hd_byte_workspace_bytes",
+    "hd_byte_product",
+    "hd_class_loss_workspace_bytes",
+    "hd_class_loss",
+    "hd_class_loss_grad_workspace_bytes",
+    "hd_class_loss_grad",
+    "hd_dropout",
 )
 
 _lib = None
@@ -159,6 +175,34 @@ def lib():
         L.hd_ckpt_class_grad_workspace_bytes.restype = sz
         L.hd_ckpt_class_grad.argtypes = [vp, i64, vp, vp, i64, i64, i64, i32, i32, vp, sz, vp]
         L.hd_ckpt_class_grad.restype = i32
+        L.hd_byte_bytes.argtypes = [i64, i64]
+        L.hd_byte_bytes.restype = sz
+        L.hd_byte_pack.argtypes = [vp, vp, i64, i64, vp, sz, vp]
+        L.hd_byte_pack.restype = i32
+        L.hd_byte_quantize.argtypes = [vp, i64, i32, i64, i64, i32, vp, sz, vp]
+        L.hd_byte_quantize.restype = i32
+        L.hd_byte_unpack.argtypes = [vp, vp, i64, i64, vp]
+        L.hd_byte_unpack.restype = i32
+        L.hd_byte_rows.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp]
+        L.hd_byte_rows.restype = i32
+        L.hd_byte_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.hd_byte_workspace_bytes.restype = sz
+        L.hd_byte_product.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, vp,
+                                      sz, vp]
+        L.hd_byte_product.restype = i32
+        L.hd_class_loss_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.hd_class_loss_workspace_bytes.restype = sz
+        L.hd_class_loss.argtypes = [vp, i64, vp, i64, vp, vp, f32, vp, vp, i64, i64, i64, i32, vp,
+                                    sz, vp]
+        L.hd_class_loss.restype = i32
+        L.hd_class_loss_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.hd_class_loss_grad_workspace_bytes.restype = sz
+        L.hd_class_loss_grad.argtypes = [vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, vp, i64, i64,
+                                         i64, i32, vp, sz, vp]
+        L.hd_class_loss_grad.restype = i32
+        u64, f64 = ctypes.c_uint64, ctypes.c_double
+        L.hd_dropout.argtypes = [vp, i64, vp, i64, i64, i64, f64, u64, u64, vp, i32, vp]
+        L.hd_dropout.restype = i32
         _lib = L
         return L
 
@@ -879,4 +923,219 @@ def ckpt_class_grad(dS, kept: Checkpoint, out=None, accumulate: bool = False):
                                   dt, accumulate, ws.data_ptr() if need else None, need,
                                   _raw_stream(index))
     _raise(st, "hd_ckpt_class_grad")
+    return out
+
+
+class ByteWeights:
+    """A matrix in 8 bits with a scale for each output, laid out once (opaque device image)."""
+
+    def __init__(self, image, outer: int, inner: int):
+        self.image, self.outer, self.inner = image, outer, inner
+
+
+def _byte_image(outer: int, inner: int, device):
+    torch = _torch()
+    nbytes = int(lib().hd_byte_bytes(outer, inner))
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def byte_pack(codes, scales) -> ByteWeights:
+    """8-bit weights from given ``codes`` [outer, inner] int8 and ``scales`` [outer] float32."""
+    torch = _torch()
+    _check_dev(codes)
+    if codes.dtype != torch.int8:
+        raise TypeError("codes must be int8")
+    if codes.dim() != 2:
+        raise ValueError("codes must be a matrix")
+    outer, inner = codes.shape
+    index = codes.get_device()
+    sptr = _vec(scales, "scales", torch.float32, outer, index)
+    image, nbytes = _byte_image(outer, inner, codes.device)
+    st = lib().hd_byte_pack(codes.data_ptr(), sptr, outer, inner, image.data_ptr(), nbytes,
+                            _raw_stream(index))
+    _raise(st, "hd_byte_pack")
+    return ByteWeights(image, outer, inner)
+
+
+def byte_quantize(W, inner_rows: bool = False) -> ByteWeights:
+    """8-bit weights from numbers: ``W`` [outer, inner] (class hypervectors), or with
+    ``inner_rows`` [inner, outer] (base hypervectors B[F, D]); float32 or bfloat16."""
+    outer, inner, ld, dt, index = _rows(W, "W")
+    if inner_rows:
+        outer, inner = inner, outer
+    image, nbytes = _byte_image(outer, inner, W.device)
+    st = lib().hd_byte_quantize(W.data_ptr(), ld, int(inner_rows), outer, inner, dt,
+                                image.data_ptr(), nbytes, _raw_stream(index))
+    _raise(st, "hd_byte_quantize")
+    return ByteWeights(image, outer, inner)
+
+
+def byte_unpack(w: ByteWeights):
+    """The weights that ``w`` stands for: [outer, inner] float32."""
+    torch = _torch()
+    W = torch.empty((w.outer, w.inner), dtype=torch.float32, device=w.image.device)
+    st = lib().hd_byte_unpack(w.image.data_ptr(), W.data_ptr(), w.outer, w.inner,
+                              _raw_stream(w.image.get_device()))
+    _raise(st, "hd_byte_unpack")
+    return W
+
+
+def byte_rows(X):
+    """Rows of ``X`` [N, inner] (float32 or bfloat16) as codes [N, inner] int8 and scales [N]
+    float32: what ``byte_product`` does to them, for rows that several products take."""
+    torch = _torch()
+    N, inner, ld, dt, index = _rows(X, "X")
+    codes = torch.empty(N, inner, dtype=torch.int8, device=X.device)
+    scales = torch.empty(N, dtype=torch.float32, device=X.device)
+    st = lib().hd_byte_rows(X.data_ptr(), ld, N, inner, dt, codes.data_ptr(), scales.data_ptr(),
+                            _raw_stream(index))
+    _raise(st, "hd_byte_rows")
+    return codes, scales
+
+
+def byte_product(X, w: ByteWeights, act: str = "identity", dtype=None, out=None, row_scales=None):
+    """Y[N, outer] = act(X w^T) in 8-bit integers. ``X`` [N, inner] float32 or bfloat16 is taken
+    to codes with a scale for each row; int8 ``X`` holds codes, with ``row_scales`` [N] float32
+    (None: 1). ``dtype`` of Y defaults to X's (float32 for int8). ``act`` "hardsign" encodes."""
+    torch = _torch()
+    if X.dtype == torch.int8:
+        index = X.get_device()
+        if index < 0:
+            raise ValueError("tensors must be on the GPU")
+        if X.dim() != 2:
+            raise ValueError("X must be a matrix")
+        N, inner = X.shape
+        ldx, step = X.stride()
+        if step != 1 and inner > 1:
+            raise ValueError("X must have contiguous rows")
+        if ldx < inner:
+            if N > 1:
+                raise ValueError("X must not have overlapping rows")
+            ldx = inner
+        x_dt = HD_I8
+    else:
+        N, inner, ldx, x_dt, index = _rows(X, "X")
+        if row_scales is not None:
+            raise ValueError("row_scales are for X in int8")
+    sptr = _vec(row_scales, "row_scales", torch.float32, N, index) if row_scales is not None else None
+    outer, image = w.outer, w.image
+    if inner != w.inner:
+        raise ValueError("shape mismatch")
+    if image.get_device() != index:
+        raise ValueError("X and the weights must be on one device")
+    if out is None:
+        if dtype is None:
+            dtype = torch.float32 if x_dt == HD_I8 else X.dtype
+        y_dt = (_codes or _float_codes()).get(dtype)
+        if y_dt is None:
+            raise TypeError("dtype must be float32 or bfloat16")
+        out, ldy = torch.empty(N, outer, dtype=dtype, device=X.device), outer
+    else:
+        _, _, ldy, y_dt, out_index = _rows(out, "out")
+        if out_index != index or out.shape != (N, outer):
+            raise ValueError("out must be [N, outer] on X's device")
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError("out has another dtype")
+    need = _need("hd_byte_workspace_bytes", index, N, outer, inner, x_dt)
+    ws = torch.empty(need, dtype=torch.uint8, device=X.device) if need else None
+    st = lib().hd_byte_product(X.data_ptr(), ldx, sptr, image.data_ptr(), out.data_ptr(), ldy, N,
+                               outer, inner, x_dt, y_dt, ACTS[act], _ptr(ws), need,
+                               _raw_stream(index))
+    _raise(st, "hd_byte_product")
+    return out
+
+
+class ClassLoss(NamedTuple):
+    """What ``class_loss`` gives for N rows: ``loss`` [N] and ``stats`` [N, 2] (the largest score m,
+    and log sum exp scale (s - m)). They are parts of one allocation."""
+    loss: object
+    stats: object
+
+
+def _class_args(H, C, y, mask):
+    torch = _torch()
+    N, D, ldh, dt, index = _rows(H, "H")
+    K, D2, ldc, c_dt, c_index = _rows(C, "C")
+    if c_dt != dt:
+        raise TypeError("H and C must share a dtype")
+    if D2 != D:
+        raise ValueError("shape mismatch")
+    if c_index != index:
+        raise ValueError("H and C must be on one device")
+    yptr = _vec(y, "y", torch.int32, N, index)
+    mptr = None
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError("mask must be bool or uint8")
+        mptr = _vec(mask, "mask", mask.dtype, K, index)
+    return N, D, K, ldh, ldc, dt, index, yptr, mptr
+
+
+def class_loss(H, C, y, scale: float = 1.0, mask=None) -> ClassLoss:
+    """Softmax cross entropy of the classes ``y`` [N] int32 (outside [0, K): none asked for, loss 0)
+    under softmax(scale * H C^T), for encodings ``H`` [N, D] and class vectors ``C`` [K, D], both
+    float32 or both bfloat16, without the scores being kept. ``mask`` [K]: classes that are False
+    take no part."""
+    torch = _torch()
+    N, D, K, ldh, ldc, dt, index, yptr, mptr = _class_args(H, C, y, mask)
+    buf = torch.empty(3 * N, dtype=torch.float32, device=H.device)
+    at = buf.data_ptr()  # stats, loss
+    need = _need("hd_class_loss_workspace_bytes", index, N, D, K, dt)
+    ws = torch.empty(need, dtype=torch.uint8, device=H.device) if need else None
+    st = lib().hd_class_loss(H.data_ptr(), ldh, C.data_ptr(), ldc, mptr, yptr, scale, at + 8 * N,
+                             at, N, D, K, dt, _ptr(ws), need, _raw_stream(index))
+    _raise(st, "hd_class_loss")
+    stats, loss = buf.split_with_sizes((2 * N, N))
+    return ClassLoss(loss, stats.view(N, 2))
+
+
+def class_loss_grad(H, C, y, cl: ClassLoss, g_loss, scale: float = 1.0, mask=None,
+                    wrt: str = "both"):
+    """The gradient of sum(g_loss * loss) (``g_loss`` [N] float32): (dH [N, D], dC [K, D]) of H's
+    dtype; ``cl`` is what ``class_loss`` gave for the same H, C, y, scale and mask. ``wrt``: "both",
+    "encodings" or "classes"; what is not asked for is None and costs nothing."""
+    torch = _torch()
+    if wrt not in ("both", "encodings", "classes"):
+        raise ValueError('wrt must be "both", "encodings" or "classes"')
+    N, D, K, ldh, ldc, dt, index, yptr, mptr = _class_args(H, C, y, mask)
+    gptr, stats = _vec(g_loss, "g_loss", torch.float32, N, index), cl.stats
+    if (stats.shape != (N, 2) or stats.dtype != torch.float32 or not stats.is_contiguous()
+            or stats.get_device() != index):
+        raise ValueError("stats must be float32 [N, 2] on the encodings' device")
+    dH = torch.empty(N, D, dtype=H.dtype, device=H.device) if wrt != "classes" else None
+    dC = torch.empty(K, D, dtype=H.dtype, device=H.device) if wrt != "encodings" else None
+    need = _need("hd_class_loss_grad_workspace_bytes", index, N, D, K, dt)
+    ws = torch.empty(need, dtype=torch.uint8, device=H.device) if need else None
+    st = lib().hd_class_loss_grad(H.data_ptr(), ldh, C.data_ptr(), ldc, mptr, yptr, scale,
+                                  stats.data_ptr(), gptr, _ptr(dH), _ptr(dC), N, D, K, dt,
+                                  _ptr(ws), need, _raw_stream(index))
+    _raise(st, "hd_class_loss_grad")
+    return dH, dC
+
+
+def dropout(X, p: float, seed: int, step=0, out=None):
+    """``X`` [N, D] (float32 or bfloat16) with values dropped with probability ``p`` and the others
+    times 1 / (1 - p). Which ones is a function of ``seed`` and ``step`` (64 bits each) and a
+    value's place: the same call on the gradient is the backward pass. ``step`` may be an int64
+    tensor of one element on the GPU, which a graph's replays read. ``out`` may be X itself."""
+    torch = _torch()
+    N, D, ldx, dt, index = _rows(X, "X")
+    at = None
+    if isinstance(step, torch.Tensor):
+        if step.dtype != torch.int64 or step.numel() != 1:
+            raise TypeError("step must be a number or an int64 tensor of one element")
+        if step.get_device() != index:
+            raise ValueError("step must be on X's device")
+        at, step = step.data_ptr(), 0
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64):
+        raise ValueError("seed and step must be in [0, 2^64)")
+    if out is None:
+        out, ldy = torch.empty(N, D, dtype=X.dtype, device=X.device), D
+    else:
+        _, _, ldy, out_dt, out_index = _rows(out, "out")
+        if out.shape != (N, D) or out_dt != dt or out_index != index:
+            raise ValueError("out must have X's shape, dtype and device")
+    st = lib().hd_dropout(X.data_ptr(), ldx, out.data_ptr(), ldy, N, D, p, seed, step, at, dt,
+                          _raw_stream(index))
+    _raise(st, "hd_dropout")
     return out

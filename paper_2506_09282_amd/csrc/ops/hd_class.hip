@@ -1,0 +1,686 @@
+// Softmax cross entropy of given classes straight from encodings H[N][D] and class vectors
+// C[K][D], and its gradient, without the scores S = H C^T ever being kept:
+//
+//   s_k = <H_n, C_k>,  m = max s_k,  L = log sum exp(scale (s_k - m)),
+//   loss = L - scale (s_y - m)
+//   dS = g scale (p - 1[k = y]),  p = exp(scale (s_k - m) - L);   dH = dS C,  dC = dS^T H
+//
+// A tile of scores stays in its workgroup's registers: the forward pass leaves of it each row's
+// maximum and sum over the tile's classes (joined by a second launch) and the score asked for; the
+// backward pass computes it again and leaves dS, of as many classes at a time as fit
+// kPieceBytes, which the two products then read. Classes are the instruction's rows, so
+// that a lane holds 16 classes of one sample and most of a row's maximum and sum needs no
+// exchange between lanes.
+//
+// Where there are too few tiles for the chip (few rows and classes), the reduction over D is
+// split and the parts of the (then small) score matrix go through the workspace.
+#include "hd_tile.hpp"
+
+namespace hd {
+namespace ops {
+
+namespace {
+
+using tile::Bf16;
+using tile::die_order;
+using tile::F32;
+using tile::kCols;
+using tile::kRows;
+using tile::Operand;
+using tile::Plan;
+using tile::Tile;
+using tile::tile_at;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kThreads = 256;
+
+// Scores' gradients kept at a time. 128 MiB stay in the last cache (256 MB) between the launch
+// that writes them and the two that read them.
+constexpr int64_t kPieceBytes = int64_t(128) << 20;
+
+struct Scores {  // of the classes [0, K) of a piece
+  Operand H, C;
+  const int32_t* y;
+  const uint64_t* open;  // a bit for each class (null: all are open)
+  float scale;
+  int64_t N, D, K;
+  int64_t first;  // the piece's first class (of y)
+  uint32_t mt, nt;
+};
+
+// Of 32 classes from k on, those that take part.
+__device__ __forceinline__ uint32_t open_bits(const Scores& a, int64_t k) {
+  const int64_t left = a.K - k;
+  if (left <= 0) return 0u;
+  uint32_t bits = left < 32 ? (1u << left) - 1u : ~0u;
+  if (a.open) bits &= (uint32_t)(a.open[k >> 6] >> (k & 32));
+  return bits;
+}
+
+__device__ __forceinline__ bool asked(int32_t y, int64_t K) { return y >= 0 && y < K; }
+
+// A row's maximum and sum of exp2(c (s - m)) over two sets of classes.
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
+  const float top = fmaxf(m, m2);
+  const float at = top == -INFINITY ? 0.0f : top;  // (nothing takes part: sums of 0 stay 0)
+  s = s * exp2f(c * (m - at)) + s2 * exp2f(c * (m2 - at));
+  m = top;
+}
+
+// m and log of the sum to what the caller gets; NaN and +inf among the scores give NaN.
+__device__ __forceinline__ void finish_row(float m, float s, float target, bool asks, float scale,
+                                           float* loss, float* stats) {
+  float L = logf(s), at = m;
+  if (m == -INFINITY && s == 0.0f) {  // no class
+    L = 0.0f;
+    *loss = asks ? INFINITY : 0.0f;
+  } else {
+    if (s != s || m == INFINITY) at = L = NAN;
+    *loss = asks ? L - scale * (target - at) : 0.0f;
+  }
+  stats[0] = at;
+  stats[1] = L;
+}
+
+// ---- forward ----------------------------------------------------------------------
+
+// parts[n][class tile] = {maximum, sum}, target[n] = the score asked for.
+template <class TL>
+__global__ __launch_bounds__(TL::T, 2) void class_loss_kernel(
+    Scores a, float2* __restrict__ parts, float* __restrict__ target) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  uint32_t mi, ni;
+  tile_at(die_order(blockIdx.x, gridDim.x), a.mt, a.nt, mi, ni);
+  const int64_t m0 = (int64_t)mi * TL::BM, n0 = (int64_t)ni * TL::BN;
+  typename TL::Acc c[TL::MT][TL::NT];
+  TL::product(a.C, a.H, m0, n0, 0, a.D, lds, c);
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
+  const float scale2 = a.scale * kLog2e;
+  const bool all_open = !a.open && m0 + TL::BM <= a.K;
+  float2* part = reinterpret_cast<float2*>(lds);  // [WM][BN]
+#pragma unroll
+  for (int j = 0; j < TL::NT; ++j) {
+    const int col = (wn * TL::NT + j) * 32 + (lane & 31);
+    const int64_t n = n0 + col;
+    const int32_t y = n < a.N ? a.y[n] : -1;
+    const int64_t at = (int64_t)y - m0 - wm * TL::MT * 32;
+    const bool here = y >= 0 && y < a.K && at >= 0 && at < TL::MT * 32;
+    if (!all_open) {
+#pragma unroll
+      for (int i = 0; i < TL::MT; ++i) {
+        uint32_t bits = open_bits(a, m0 + (wm * TL::MT + i) * 32) >> (4 * half);
+        // (worked out for each column again: kept, the lanes' conditions fill the registers)
+        asm volatile("" : "+v"(bits));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!(bits >> ((r / 4) * 8 + r % 4) & 1)) c[i][j][r] = -INFINITY;
+      }
+    }
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < TL::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) m = fmaxf(m, c[i][j][r]);
+    if (here) {  // one of the two lanes of a sample holds the score asked for
+      int place = (int)at;
+      place = ((place >> 2) & 1) == half ? (place >> 5) * 16 + ((place & 31) >> 3) * 4 + (place & 3)
+                                         : -1;
+      asm volatile("" : "+v"(place));
+      float t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TL::MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) t = place == i * 16 + r ? c[i][j][r] : t;
+      if (place >= 0) target[n] = t;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TL::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s += exp2f(scale2 * (c[i][j][r] - base));
+    join(m, s, lane_xor<32>(m), lane_xor<32>(s), scale2);
+    if (half == 0) part[wm * TL::BN + col] = make_float2(m, s);
+  }
+  __syncthreads();
+  for (int col = threadIdx.x; col < TL::BN; col += TL::T) {
+    float2 x = part[col];
+#pragma unroll
+    for (int w = 1; w < TL::WM; ++w) {
+      const float2 z = part[w * TL::BN + col];
+      join(x.x, x.y, z.x, z.y, scale2);
+    }
+    if (n0 + col < a.N) parts[(n0 + col) * a.mt + mi] = x;
+  }
+}
+
+// A wave joins the parts of a row.
+__global__ __launch_bounds__(kThreads) void class_join_kernel(
+    const float2* __restrict__ parts, const float* __restrict__ target,
+    const int32_t* __restrict__ y, int64_t N, int64_t K, int tiles, float scale,
+    float* __restrict__ loss, float* __restrict__ stats) {
+  const int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (n >= N) return;
+  const int lane = threadIdx.x & 63;
+  const float scale2 = scale * kLog2e;
+  float m = -INFINITY, s = 0.0f;
+  for (int t = lane; t < tiles; t += 64) {
+    const float2 x = parts[n * tiles + t];
+    join(m, s, x.x, x.y, scale2);
+  }
+  join(m, s, lane_xor<1>(m), lane_xor<1>(s), scale2);
+  join(m, s, lane_xor<2>(m), lane_xor<2>(s), scale2);
+  join(m, s, lane_xor<4>(m), lane_xor<4>(s), scale2);
+  join(m, s, lane_xor<8>(m), lane_xor<8>(s), scale2);
+  join(m, s, lane_xor<16>(m), lane_xor<16>(s), scale2);
+  join(m, s, lane_xor<32>(m), lane_xor<32>(s), scale2);
+  if (lane == 0) {
+    const bool asks = asked(y[n], K);
+    finish_row(m, s, asks ? target[n] : 0.0f, asks, scale, loss + n, stats + 2 * n);
+  }
+}
+
+// ---- the scores in parts of D, where there are few ----------------------------------
+
+// out[part][n][class], rows of mt * BM classes.
+template <class TL>
+__global__ __launch_bounds__(TL::T, 2) void class_scores_kernel(Scores a, int64_t each,
+                                                                float* __restrict__ out) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const uint32_t tiles = a.mt * a.nt;
+  const uint32_t id = die_order(blockIdx.x, gridDim.x), part = id / tiles;
+  uint32_t mi, ni;
+  tile_at(id % tiles, a.mt, a.nt, mi, ni);
+  const int64_t m0 = (int64_t)mi * TL::BM, n0 = (int64_t)ni * TL::BN;
+  const int64_t k0 = part * each, k1 = k0 + each < a.D ? k0 + each : a.D;
+  typename TL::Acc c[TL::MT][TL::NT];
+  TL::product(a.C, a.H, m0, n0, k0, k1, lds, c);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
+  const int64_t ld = (int64_t)a.mt * TL::BM;
+#pragma unroll
+  for (int j = 0; j < TL::NT; ++j) {
+    const int64_t n = n0 + (wn * TL::NT + j) * 32 + (lane & 31);
+    if (n >= a.N) continue;
+    float* row = out + ((int64_t)part * a.N + n) * ld + m0 + wm * TL::MT * 32 + half * 4;
+#pragma unroll
+    for (int i = 0; i < TL::MT; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(row + i * 32 + q * 8) =
+            f32x4{c[i][j][4 * q], c[i][j][4 * q + 1], c[i][j][4 * q + 2], c[i][j][4 * q + 3]};
+  }
+}
+
+struct Parts {
+  const float* p;  // [parts][N][ld]
+  int64_t ld, N;
+  int count;
+};
+__device__ __forceinline__ float score_of(const Parts& s, int64_t n, int64_t k) {
+  float v = 0.0f;
+  for (int i = 0; i < s.count; ++i) v += s.p[((int64_t)i * s.N + n) * s.ld + k];
+  return v;
+}
+
+// W waves to a row.
+template <int W>
+__global__ __launch_bounds__(kThreads) void class_rows_kernel(
+    Parts sc, const int32_t* __restrict__ y, const uint64_t* __restrict__ open, int64_t K,
+    float scale, float* __restrict__ loss, float* __restrict__ stats) {
+  __shared__ float2 part[kThreads / 64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * (4 / W) + wave / W;
+  const bool there = row < sc.N;  // (all threads meet at the barrier)
+  const int64_t n = there ? row : sc.N - 1;
+  const float scale2 = scale * kLog2e;
+  float m = -INFINITY, s = 0.0f;
+  for (int64_t k = (wave % W) * 64 + lane; k < K; k += 64 * W) {
+    if (open && !(open[k >> 6] >> (k & 63) & 1)) continue;
+    const float v = score_of(sc, n, k);
+    // (a score of NaN is no maximum, and makes the sum NaN)
+    if (v > m) {
+      s = m == -INFINITY ? s + 1.0f : s * exp2f(scale2 * (m - v)) + 1.0f;
+      if (v == INFINITY) s = NAN;
+      m = v;
+    } else if (v != -INFINITY) {
+      s += exp2f(scale2 * (v - (m == -INFINITY ? 0.0f : m)));
+    }
+  }
+  join(m, s, lane_xor<1>(m), lane_xor<1>(s), scale2);
+  join(m, s, lane_xor<2>(m), lane_xor<2>(s), scale2);
+  join(m, s, lane_xor<4>(m), lane_xor<4>(s), scale2);
+  join(m, s, lane_xor<8>(m), lane_xor<8>(s), scale2);
+  join(m, s, lane_xor<16>(m), lane_xor<16>(s), scale2);
+  join(m, s, lane_xor<32>(m), lane_xor<32>(s), scale2);
+  if constexpr (W > 1) {
+    if (lane == 0) part[wave] = make_float2(m, s);
+    __syncthreads();
+    m = part[0].x;
+    s = part[0].y;
+    for (int w = 1; w < W; ++w) join(m, s, part[w].x, part[w].y, scale2);
+  }
+  if (there && lane == 0 && wave % W == 0) {
+    const bool asks = asked(y[n], K);
+    float t = 0.0f;
+    if (asks)
+      t = open && !(open[y[n] >> 6] >> (y[n] & 63) & 1) ? -INFINITY : score_of(sc, n, y[n]);
+    finish_row(m, s, t, asks, scale, loss + n, stats + 2 * n);
+  }
+}
+
+// ---- backward: the scores' gradient ---------------------------------------------------
+
+struct RowGrad {
+  float m, shift, g;  // p = exp2(c (s - m) - shift), dS = g (p - 1[k = y])
+  int64_t y;          // of the piece; far outside where no class is asked for
+  bool on;
+};
+__device__ __forceinline__ RowGrad row_grad(const Scores& a, const float* stats, const float* g,
+                                            int64_t K_all, int64_t n) {
+  RowGrad r;
+  const float m = stats[2 * n];
+  r.on = asked(a.y[n], K_all);
+  r.m = m == -INFINITY ? 0.0f : m;
+  r.shift = stats[2 * n + 1] * kLog2e;
+  r.g = g[n] * a.scale;
+  r.y = (int64_t)a.y[n] - a.first;
+  return r;
+}
+__device__ __forceinline__ float score_grad(const RowGrad& r, float s, int64_t k, bool open,
+                                            float scale2) {
+  // a score of -inf takes no part: its p is 0, also where it is asked for
+  float p = exp2f(scale2 * (s - r.m) - r.shift);
+  if (k == r.y && s != -INFINITY) p -= 1.0f;
+  return r.on && open ? r.g * p : 0.0f;
+}
+
+// dS[n][class] of a piece, rows of ld elements.
+template <class TL>
+__global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
+    Scores a, int64_t K_all, const float* __restrict__ stats, const float* __restrict__ g,
+    typename TL::P::elem* __restrict__ dS, int64_t ld) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  uint32_t mi, ni;
+  tile_at(die_order(blockIdx.x, gridDim.x), a.mt, a.nt, mi, ni);
+  const int64_t m0 = (int64_t)mi * TL::BM, n0 = (int64_t)ni * TL::BN;
+  typename TL::Acc c[TL::MT][TL::NT];
+  TL::product(a.C, a.H, m0, n0, 0, a.D, lds, c);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
+  const float scale2 = a.scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < TL::NT; ++j) {
+    const int64_t n = n0 + (wn * TL::NT + j) * 32 + (lane & 31);
+    if (n >= a.N) continue;
+    const RowGrad row = row_grad(a, stats, g, K_all, n);
+#pragma unroll
+    for (int i = 0; i < TL::MT; ++i) {
+      const int64_t k0 = m0 + (wm * TL::MT + i) * 32;
+      const uint32_t bits = open_bits(a, k0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = q * 8 + half * 4 + e;
+          v[e] = score_grad(row, c[i][j][4 * q + e], k0 + at, bits >> at & 1, scale2);
+        }
+        const int64_t k = k0 + q * 8 + half * 4;
+        if (k >= ld) continue;  // (ld is a multiple of 8, so four values fit or none)
+        if constexpr (TL::P::kEs == 4) {
+          *reinterpret_cast<f32x4*>(dS + n * ld + k) = f32x4{v[0], v[1], v[2], v[3]};
+        } else {
+          u32x2 w;
+          w[0] = to_bf16(v[0]) | (uint32_t)to_bf16(v[1]) << 16;
+          w[1] = to_bf16(v[2]) | (uint32_t)to_bf16(v[3]) << 16;
+          *reinterpret_cast<u32x2*>(dS + n * ld + k) = w;
+        }
+      }
+    }
+  }
+}
+
+// The same from the parts of the scores; a thread takes a class of a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void class_dscores_parts_kernel(
+    Scores a, int64_t K_all, Parts sc, const float* __restrict__ stats,
+    const float* __restrict__ g, T* __restrict__ dS, int64_t ld) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t n = i / ld, k = i - n * ld;
+  if (n >= a.N) return;
+  const bool open = k < a.K && (!a.open || (a.open[k >> 6] >> (k & 63) & 1));
+  float v = 0.0f;
+  if (open)
+    v = score_grad(row_grad(a, stats, g, K_all, n), score_of(sc, n, k), k, true,
+                   a.scale * kLog2e);
+  store_elem(dS, i, v);
+}
+
+// ---- backward: the products -------------------------------------------------------------
+
+// Where a product goes: its part of the reduction to parts[part][M][N], or, added to
+// `before` where there is one, to sums (fp32) or out. All are contiguous.
+struct Out {
+  void* out;
+  float *sums, *parts;
+  const float* before;
+  int64_t M, N;
+};
+
+template <typename T>
+__device__ __forceinline__ void put(const Out& o, int64_t at, float v) {
+  if (o.before) v += o.before[at];
+  if (o.sums)
+    o.sums[at] = v;
+  else
+    store_elem(reinterpret_cast<T*>(o.out), at, v);
+}
+
+template <class TL>
+__global__ __launch_bounds__(TL::T, 2) void class_product_kernel(
+    Operand a, Operand b, int64_t K, int64_t each, uint32_t mt, uint32_t nt, Out o) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const uint32_t tiles = mt * nt;
+  const uint32_t id = die_order(blockIdx.x, gridDim.x), part = id / tiles;
+  uint32_t mi, ni;
+  tile_at(id % tiles, mt, nt, mi, ni);
+  const int64_t m0 = (int64_t)mi * TL::BM, n0 = (int64_t)ni * TL::BN;
+  const int64_t k0 = part * each, k1 = k0 + each < K ? k0 + each : K;
+  typename TL::Acc c[TL::MT][TL::NT];
+  TL::product(a, b, m0, n0, k0, k1, lds, c);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
+#pragma unroll
+  for (int i = 0; i < TL::MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int64_t m = m0 + (wm * TL::MT + i) * 32 + (r / 4) * 8 + half * 4 + r % 4;
+      if (m >= o.M) continue;
+#pragma unroll
+      for (int j = 0; j < TL::NT; ++j) {
+        const int64_t n = n0 + (wn * TL::NT + j) * 32 + (lane & 31);
+        if (n >= o.N) continue;
+        if (o.parts)
+          o.parts[((int64_t)part * o.M + m) * o.N + n] = c[i][j][r];
+        else
+          put<typename TL::P::elem>(o, m * o.N + n, c[i][j][r]);
+      }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void class_sum_kernel(Out o, int count) {
+  const int64_t each = o.M * o.N;
+  const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (at >= each) return;
+  float v = 0.0f;
+  for (int i = 0; i < count; ++i) v += o.parts[i * each + at];
+  put<T>(o, at, v);
+}
+
+// Bits of the rows that ask for a class, and of the open classes.
+__global__ __launch_bounds__(kThreads) void class_bits_kernel(const int32_t* __restrict__ y,
+                                                              int64_t N, uint64_t* rows,
+                                                              const uint8_t* __restrict__ mask,
+                                                              int64_t K, uint64_t* classes) {
+  const int64_t row_words = rows ? cdiv(N, 64) : 0;
+  int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (w < row_words) {
+    const int64_t n = w * 64 + lane;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(n < N && asked(y[n], K));
+    if (lane == 0) rows[w] = b;
+    return;
+  }
+  w -= row_words;
+  if (!mask || w >= cdiv(K, 64)) return;
+  const int64_t k = w * 64 + lane;
+  const uint64_t b = __builtin_amdgcn_ballot_w64(k < K && mask[k] != 0);
+  if (lane == 0) classes[w] = b;
+}
+
+// ---- host -------------------------------------------------------------------------------
+
+hipError_t last_error() { return hipGetLastError(); }
+
+template <auto KERNEL>
+hipError_t allow_lds(int bytes) {
+  static PerDeviceOnce once;
+  return once_per_device(once, [&] {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  });
+}
+
+template <auto KERNEL, class TL, typename... A>
+hipError_t launch_tiles(int64_t blocks, hipStream_t stream, A... args) {
+  const hipError_t e = allow_lds<KERNEL>(TL::kLds);
+  if (e != hipSuccess) return e;
+  KERNEL<<<dim3((uint32_t)blocks), dim3(TL::T), TL::kLds, stream>>>(args...);
+  return last_error();
+}
+
+// f is called with the tile of a plan.
+template <class P, int AK, int BK, class F>
+hipError_t with_tile(tile::Shape s, F f) {
+  switch (s) {
+    case tile::k256: return f(Tile<P, AK, BK, 256, 256, 2, 4>());
+    case tile::k128: return f(Tile<P, AK, BK, 128, 128, 2, 2>());
+    case tile::k32x128: return f(Tile<P, AK, BK, 32, 128, 1, 4>());
+    default: return f(Tile<P, AK, BK, 128, 32, 4, 1>());
+  }
+}
+
+int64_t tile_m(const Plan& p) {
+  return p.shape == tile::k256 ? 256 : p.shape == tile::k32x128 ? 32 : 128;
+}
+
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+// How a call cuts its classes: one piece where the scores go through the workspace in
+// parts, else as many classes as kPieceBytes hold.
+int64_t piece_of(int64_t N, int64_t K, int64_t es) {
+  int64_t k = kPieceBytes / (N * es) / 256 * 256;
+  if (k < 256) k = 256;
+  return k < K ? k : K;
+}
+
+struct LossPlace {
+  Plan s;
+  size_t open, parts, target, total;
+};
+LossPlace loss_place(int64_t N, int64_t D, int64_t K) {
+  LossPlace w;
+  w.s = tile::plan(K, N, D);
+  w.open = 0;
+  w.parts = up((size_t)cdiv(K, 64) * 8);
+  if (w.s.splits > 1) {
+    w.target = w.total = w.parts + up((size_t)w.s.splits * N * w.s.mt * tile_m(w.s) * 4);
+  } else {
+    w.target = w.parts + up((size_t)N * w.s.mt * 8);
+    w.total = w.target + up((size_t)N * 4);
+  }
+  return w;
+}
+
+struct GradPlace {
+  int64_t piece, ld;  // classes at a time, and of a row of dS
+  size_t rows, open, dS, scores, sums, parts, total;
+};
+GradPlace grad_place(int64_t N, int64_t D, int64_t K, int64_t es) {
+  GradPlace w;
+  const Plan s = tile::plan(K, N, D);
+  w.piece = s.splits > 1 ? K : piece_of(N, K, es);
+  w.ld = cdiv(w.piece, 8) * 8;
+  w.rows = 0;
+  w.open = up((size_t)cdiv(N, 64) * 8);
+  w.dS = w.open + up((size_t)cdiv(K, 64) * 8);
+  w.scores = w.dS + up((size_t)N * w.ld * es);
+  size_t at = w.scores;
+  if (s.splits > 1) at += up((size_t)s.splits * N * s.mt * tile_m(s) * 4);
+  w.sums = at;
+  if (w.piece < K) at += up((size_t)N * D * 4);
+  w.parts = at;
+  // (the last piece may be short, and its products split further)
+  size_t most = 0;
+  for (int64_t k : {w.piece, K - (K - 1) / w.piece * w.piece}) {
+    const Plan h = tile::plan(N, D, k), c = tile::plan(k, D, N);
+    if (h.splits > 1) most = std::max(most, (size_t)(h.splits * N * D) * 4);
+    if (c.splits > 1) most = std::max(most, (size_t)(c.splits * k * D) * 4);
+  }
+  w.total = at + up(most);
+  return w;
+}
+
+template <class P>
+hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hipStream_t stream) {
+  const LossPlace w = loss_place(c.N, c.D, c.K);
+  uint64_t* open = nullptr;
+  hipError_t e;
+  if (c.mask) {
+    open = reinterpret_cast<uint64_t*>(ws + w.open);
+    class_bits_kernel<<<dim3((uint32_t)cdiv(cdiv(c.K, 64), kThreads / 64)), dim3(kThreads), 0,
+                        stream>>>(nullptr, 0, nullptr, c.mask, c.K, open);
+    if ((e = last_error()) != hipSuccess) return e;
+  }
+  const Scores a{{c.H, c.ldh, c.N, nullptr}, {c.C, c.ldc, c.K, nullptr}, c.y, open, c.scale,
+                 c.N, c.D, c.K, 0, (uint32_t)w.s.mt, (uint32_t)w.s.nt};
+  const int64_t tiles = w.s.mt * w.s.nt;
+  float* parts = reinterpret_cast<float*>(ws + w.parts);
+  if (w.s.splits == 1) {
+    float* target = reinterpret_cast<float*>(ws + w.target);
+    e = with_tile<P, kRows, kRows>(w.s.shape, [&](auto t) {
+      typedef decltype(t) TL;
+      return launch_tiles<class_loss_kernel<TL>, TL>(tiles, stream, a,
+                                                     reinterpret_cast<float2*>(parts), target);
+    });
+    if (e != hipSuccess) return e;
+    class_join_kernel<<<dim3((uint32_t)cdiv(c.N, kThreads / 64)), dim3(kThreads), 0, stream>>>(
+        reinterpret_cast<const float2*>(parts), target, c.y, c.N, c.K, (int)w.s.mt, c.scale, loss,
+        stats);
+    return last_error();
+  }
+  e = with_tile<P, kRows, kRows>(w.s.shape, [&](auto t) {
+    typedef decltype(t) TL;
+    if constexpr (TL::BM * TL::BN > 128 * 128)
+      return hipErrorInvalidValue;  // (the large tile is not split)
+    else
+      return launch_tiles<class_scores_kernel<TL>, TL>(tiles * w.s.splits, stream, a, w.s.each,
+                                                       parts);
+  });
+  if (e != hipSuccess) return e;
+  const Parts sc{parts, w.s.mt * tile_m(w.s), c.N, (int)w.s.splits};
+  if (c.K <= 512)
+    class_rows_kernel<1><<<dim3((uint32_t)cdiv(c.N, 4)), dim3(kThreads), 0, stream>>>(
+        sc, c.y, open, c.K, c.scale, loss, stats);
+  else
+    class_rows_kernel<4><<<dim3((uint32_t)c.N), dim3(kThreads), 0, stream>>>(
+        sc, c.y, open, c.K, c.scale, loss, stats);
+  return last_error();
+}
+
+template <class P, int AK, int BK>
+hipError_t run_product(const Operand& a, const Operand& b, int64_t K, Out o, float* parts,
+                       hipStream_t stream) {
+  const Plan p = tile::plan(o.M, o.N, K);
+  if (p.splits > 1) o.parts = parts;
+  const hipError_t e = with_tile<P, AK, BK>(p.shape, [&](auto t) {
+    typedef decltype(t) TL;
+    return launch_tiles<class_product_kernel<TL>, TL>(p.mt * p.nt * p.splits, stream, a, b, K,
+                                                      p.each, (uint32_t)p.mt, (uint32_t)p.nt, o);
+  });
+  if (e != hipSuccess || p.splits == 1) return e;
+  class_sum_kernel<typename P::elem>
+      <<<dim3((uint32_t)cdiv(o.M * o.N, kThreads)), dim3(kThreads), 0, stream>>>(o, (int)p.splits);
+  return last_error();
+}
+
+template <class P>
+hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void* dH, void* dC,
+                    char* ws, hipStream_t stream) {
+  typedef typename P::elem T;
+  const GradPlace w = grad_place(c.N, c.D, c.K, P::kEs);
+  uint64_t* rows = reinterpret_cast<uint64_t*>(ws + w.rows);
+  uint64_t* open = reinterpret_cast<uint64_t*>(ws + w.open);
+  hipError_t e;
+  class_bits_kernel<<<dim3((uint32_t)cdiv(cdiv(c.N, 64) + cdiv(c.K, 64), kThreads / 64)),
+                      dim3(kThreads), 0, stream>>>(c.y, c.N, rows, c.mask, c.K, open);
+  if ((e = last_error()) != hipSuccess) return e;
+  T* dS = reinterpret_cast<T*>(ws + w.dS);
+  float* sums = reinterpret_cast<float*>(ws + w.sums);
+  float* parts = reinterpret_cast<float*>(ws + w.parts);
+  for (int64_t first = 0; first < c.K; first += w.piece) {
+    const int64_t K = std::min(w.piece, c.K - first);
+    const bool last = first + K == c.K;
+    const uint64_t* part_open = c.mask ? open + first / 64 : nullptr;
+    const T* C = reinterpret_cast<const T*>(c.C) + first * c.ldc;
+    Plan s = tile::plan(K, c.N, c.D);
+    const int64_t tiles = s.mt * s.nt;
+    if (w.piece < c.K) s.splits = 1;  // (a short last piece is computed whole)
+    const Scores a{{c.H, c.ldh, c.N, nullptr}, {C, c.ldc, K, nullptr}, c.y, part_open, c.scale,
+                   c.N, c.D, K, first, (uint32_t)s.mt, (uint32_t)s.nt};
+    if (s.splits == 1) {
+      e = with_tile<P, kRows, kRows>(s.shape, [&](auto t) {
+        typedef decltype(t) TL;
+        return launch_tiles<class_dscores_kernel<TL>, TL>(tiles, stream, a, c.K, stats, g, dS,
+                                                          w.ld);
+      });
+    } else {
+      float* scores = reinterpret_cast<float*>(ws + w.scores);
+      e = with_tile<P, kRows, kRows>(s.shape, [&](auto t) {
+        typedef decltype(t) TL;
+        if constexpr (TL::BM * TL::BN > 128 * 128)
+          return hipErrorInvalidValue;
+        else
+          return launch_tiles<class_scores_kernel<TL>, TL>(tiles * s.splits, stream, a, s.each,
+                                                           scores);
+      });
+      if (e != hipSuccess) return e;
+      const Parts sc{scores, s.mt * tile_m(s), c.N, (int)s.splits};
+      class_dscores_parts_kernel<T>
+          <<<dim3((uint32_t)cdiv(c.N * w.ld, kThreads)), dim3(kThreads), 0, stream>>>(
+              a, c.K, sc, stats, g, dS, w.ld);
+      e = last_error();
+    }
+    if (e != hipSuccess) return e;
+    if (dC) {
+      const Out o{reinterpret_cast<T*>(dC) + first * c.D, nullptr, nullptr, nullptr, K, c.D};
+      e = run_product<P, kCols, kCols>({dS, w.ld, K, nullptr}, {c.H, c.ldh, c.D, rows}, c.N, o,
+                                       parts, stream);
+      if (e != hipSuccess) return e;
+    }
+    if (dH) {
+      const Out o{dH, last ? nullptr : sums, nullptr, first ? sums : nullptr, c.N, c.D};
+      e = run_product<P, kRows, kCols>({dS, w.ld, c.N, nullptr}, {C, c.ldc, c.D, part_open}, K, o,
+                                       parts, stream);
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t class_loss_ws_bytes(int64_t N, int64_t D, int64_t K) { return loss_place(N, D, K).total; }
+size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt) {
+  return grad_place(N, D, K, dt == 0 ? 4 : 2).total;
+}
+
+hipError_t launch_class_loss(const ClassArgs& a, float* loss, float* stats, void* workspace,
+                             hipStream_t stream) {
+  char* ws = reinterpret_cast<char*>(workspace);
+  return a.dt == 0 ? run_loss<F32>(a, loss, stats, ws, stream)
+                   : run_loss<Bf16>(a, loss, stats, ws, stream);
+}
+hipError_t launch_class_loss_grad(const ClassArgs& a, const float* stats, const float* g_loss,
+                                  void* dH, void* dC, void* workspace, hipStream_t stream) {
+  char* ws = reinterpret_cast<char*>(workspace);
+  return a.dt == 0 ? run_grad<F32>(a, stats, g_loss, dH, dC, ws, stream)
+                   : run_grad<Bf16>(a, stats, g_loss, dH, dC, ws, stream);
+}
+
+}  // namespace ops
+}  // namespace hd

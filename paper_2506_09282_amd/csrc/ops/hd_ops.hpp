@@ -105,5 +105,46 @@ hipError_t launch_ckpt_class_grad(const void* dS, int64_t lds, const void* image
                                   int64_t N, int64_t D, int64_t K, int dt, bool accumulate,
                                   void* workspace, hipStream_t stream);
 
+// ---- cross entropy of class scores that are never kept (hd_class.hip) ---------
+struct ClassArgs {
+  const void* H;
+  int64_t ldh;
+  const void* C;
+  int64_t ldc;
+  const uint8_t* mask;  // [K], may be null
+  const int32_t* y;
+  float scale;
+  int64_t N, D, K;
+  int dt;
+};
+size_t class_loss_ws_bytes(int64_t N, int64_t D, int64_t K);
+hipError_t launch_class_loss(const ClassArgs& a, float* loss, float* stats, void* workspace,
+                             hipStream_t stream);
+size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt);
+hipError_t launch_class_loss_grad(const ClassArgs& a, const float* stats, const float* g_loss,
+                                  void* dH, void* dC, void* workspace, hipStream_t stream);
+
+// ---- products with 8-bit weights (hd_byte.hip) --------------------------------
+size_t byte_image_bytes(int64_t O, int64_t I);
+hipError_t launch_byte_pack(const int8_t* codes, const float* scales, int64_t O, int64_t I,
+                            void* image, hipStream_t stream);
+hipError_t launch_byte_quantize(const void* W, int64_t ldw, bool in_rows, int64_t O, int64_t I,
+                                int dt, void* image, hipStream_t stream);
+hipError_t launch_byte_unpack(const void* image, float* W, int64_t O, int64_t I,
+                              hipStream_t stream);
+hipError_t launch_byte_rows(const void* X, int64_t ldx, int64_t N, int64_t I, int dt,
+                            int8_t* codes, float* scales, hipStream_t stream);
+size_t byte_ws_bytes(int64_t N, int64_t O, int64_t I, int x_dt);
+hipError_t launch_byte_product(const void* X, int64_t ldx, const float* row_scales,
+                               const void* image, void* Y, int64_t ldy, int64_t N, int64_t O,
+                               int64_t I, int x_dt, int y_dt, int act, void* workspace,
+                               hipStream_t stream);
+
+// ---- dropout (hd_dropout.hip) ----------------------------------------------------
+// Values whose random word is under `below` (up to 2^32: all) are dropped.
+hipError_t launch_dropout(const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t N, int64_t D,
+                          uint64_t below, float scale, uint64_t seed, uint64_t step,
+                          const uint64_t* step_at, int dt, hipStream_t stream);
+
 }  // namespace ops
 }  // namespace hd

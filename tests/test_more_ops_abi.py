@@ -1,0 +1,162 @@
+"""The C entry points of the cross entropy of class scores, of products with 8-bit weights and of
+dropout, without a GPU: sizes, and every refusal on the host before anything is enqueued; and the
+generator's published outputs."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import learn_plain as P
+import paper_2506_09282_amd as hd
+
+FAKE = 0x10000  # never dereferenced: validation fails first
+ARG, UNSUP, WS, OK = hd.HD_ERR_ARG, hd.HD_ERR_UNSUPPORTED, hd.HD_ERR_WORKSPACE, hd.HD_OK
+F32, BF16, I8 = hd.HD_F32, hd.HD_BF16, hd.HD_I8
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def L():
+    return hd.lib()
+
+
+def test_class_loss_refusals(L):
+    need = L.hd_class_loss_workspace_bytes(4, 8, 10, F32)
+    assert need > 0
+    for bad in ((0, 8, 10, F32), (4, 0, 10, F32), (4, 8, 0, F32), (4, 8, 10, I8), (4, 8, 10, 9),
+                ((1 << 24) + 1, 8, 10, F32), (4, (1 << 20) + 1, 10, F32)):
+        assert L.hd_class_loss_workspace_bytes(*bad) == 0
+        assert L.hd_class_loss_grad_workspace_bytes(*bad) == 0
+
+    def f(H=FAKE, ldh=8, C=FAKE, ldc=8, mask=None, y=FAKE, scale=1.0, loss=FAKE, st=FAKE, N=4,
+          D=8, K=10, dt=F32, ws=FAKE, b=need):
+        return L.hd_class_loss(H, ldh, C, ldc, mask, y, scale, loss, st, N, D, K, dt, ws, b, None)
+
+    assert f(H=None) == ARG and f(C=None) == ARG and f(y=None) == ARG and f(loss=None) == ARG
+    assert f(st=None) == ARG and f(ws=None) == ARG and f(ws=FAKE + 8) == ARG
+    assert f(N=-1) == ARG and f(D=0) == ARG and f(K=0) == ARG and f(dt=7) == ARG
+    assert f(ldh=7) == ARG and f(ldc=7) == ARG
+    for scale in (0.0, -1.0, math.inf, math.nan):
+        assert f(scale=scale) == ARG
+    assert f(H=FAKE + 2) == ARG and f(C=FAKE + 1) == ARG and f(y=FAKE + 2) == ARG
+    assert f(loss=FAKE + 2) == ARG and f(st=FAKE + 1) == ARG
+    assert f(dt=I8) == UNSUP and f(ldh=(1 << 22) + 1) == UNSUP and f(ldc=BIG) == UNSUP
+    assert f(N=1 << 20, K=1 << 20) == UNSUP and f(K=(1 << 24) + 1) == UNSUP
+    assert f(D=(1 << 20) + 1, ldh=1 << 21, ldc=1 << 21) == UNSUP
+    assert f(b=need - 1) == WS
+    assert f(N=0, H=None, y=None, ws=None) == OK
+
+
+def test_class_loss_grad_refusals(L):
+    need = L.hd_class_loss_grad_workspace_bytes(4, 8, 10, BF16)
+
+    def f(H=FAKE, ldh=8, C=FAKE, ldc=8, mask=None, y=FAKE, scale=1.0, st=FAKE, g=FAKE, dH=FAKE,
+          dC=FAKE, N=4, D=8, K=10, dt=BF16, ws=FAKE, b=need):
+        return L.hd_class_loss_grad(H, ldh, C, ldc, mask, y, scale, st, g, dH, dC, N, D, K, dt,
+                                    ws, b, None)
+
+    assert f(H=None) == ARG and f(C=None) == ARG and f(y=None) == ARG and f(st=None) == ARG
+    assert f(g=None) == ARG and f(dH=None, dC=None) == ARG and f(ws=None) == ARG
+    assert f(dH=FAKE + 1) == ARG and f(dC=FAKE + 1) == ARG and f(g=FAKE + 2) == ARG
+    assert f(scale=math.nan) == ARG and f(ldh=3) == ARG and f(N=-2) == ARG
+    assert f(dt=I8) == UNSUP and f(b=need - 1) == WS
+    assert f(N=0, H=None, dC=None) == OK
+
+
+def test_workspaces_grow_with_the_rows_not_the_scores(L):
+    """4096 rows by 131072 classes: the scores would be 2 GiB in fp32."""
+    fwd = L.hd_class_loss_workspace_bytes(4096, 4096, 131072, BF16)
+    bwd = L.hd_class_loss_grad_workspace_bytes(4096, 4096, 131072, BF16)
+    assert fwd < 64 << 20 and bwd < 320 << 20
+
+
+def test_byte_refusals(L):
+    n = L.hd_byte_bytes(40, 130)
+    assert n == 2 * 2 * 4096 + 256  # stages of 128 inputs of 32 outputs, then the scales
+    for bad in ((0, 8), (8, 0), ((1 << 23) + 1, 8), (8, 131072), (1 << 23, 131071)):
+        assert L.hd_byte_bytes(*bad) == 0
+
+    def pack(c=FAKE, s=FAKE, o=40, i=130, im=FAKE, b=n):
+        return L.hd_byte_pack(c, s, o, i, im, b, None)
+
+    assert pack(c=None) == ARG and pack(s=None) == ARG and pack(im=None) == ARG
+    assert pack(s=FAKE + 2) == ARG and pack(im=FAKE + 16) == ARG and pack(o=0) == ARG
+    assert pack(i=131072) == UNSUP and pack(b=n - 1) == WS
+
+    def quant(W=FAKE, ld=130, rows=0, o=40, i=130, dt=F32, im=FAKE, b=n):
+        return L.hd_byte_quantize(W, ld, rows, o, i, dt, im, b, None)
+
+    assert quant(W=None) == ARG and quant(ld=129) == ARG and quant(dt=9) == ARG
+    assert quant(rows=1, ld=39) == ARG and quant(W=FAKE + 2) == ARG and quant(im=FAKE + 4) == ARG
+    assert quant(dt=I8) == UNSUP and quant(b=0) == WS
+    assert L.hd_byte_unpack(None, FAKE, 40, 130, None) == ARG
+    assert L.hd_byte_unpack(FAKE, FAKE + 2, 40, 130, None) == ARG
+
+    def rows(X=FAKE, ld=130, N=4, i=130, dt=BF16, c=FAKE, s=FAKE):
+        return L.hd_byte_rows(X, ld, N, i, dt, c, s, None)
+
+    assert rows(X=None) == ARG and rows(c=None) == ARG and rows(s=FAKE + 1) == ARG
+    assert rows(ld=129) == ARG and rows(N=-1) == ARG and rows(dt=I8) == UNSUP
+    assert rows(i=131072, ld=131072) == UNSUP and rows(N=0, X=None) == OK
+
+
+def test_byte_product_refusals(L):
+    need = L.hd_byte_workspace_bytes(4, 40, 130, F32)
+    assert need > 0 and L.hd_byte_workspace_bytes(0, 40, 130, F32) == 0
+
+    def f(X=FAKE, ldx=130, rs=None, im=FAKE, Y=FAKE, ldy=40, N=4, o=40, i=130, xdt=F32, ydt=F32,
+          act=1, ws=FAKE, b=need):
+        return L.hd_byte_product(X, ldx, rs, im, Y, ldy, N, o, i, xdt, ydt, act, ws, b, None)
+
+    assert f(X=None) == ARG and f(im=None) == ARG and f(Y=None) == ARG and f(ws=None) == ARG
+    assert f(ldx=129) == ARG and f(ldy=39) == ARG and f(N=-1) == ARG and f(act=2) == ARG
+    assert f(rs=FAKE) == ARG  # X in fp32 brings no scales
+    assert f(xdt=I8, rs=FAKE + 2) == ARG and f(X=FAKE + 2) == ARG and f(Y=FAKE + 1) == ARG
+    assert f(im=FAKE + 64) == ARG and f(ws=FAKE + 64) == ARG and f(xdt=5) == ARG and f(ydt=5) == ARG
+    assert f(ydt=I8) == UNSUP and f(N=(1 << 23) + 1) == UNSUP and f(ldx=BIG) == UNSUP
+    assert f(N=1 << 23, o=1 << 16, ldy=1 << 16) == UNSUP
+    assert f(b=need - 1) == WS and f(N=0, X=None, Y=None, ws=None) == OK
+
+
+def test_dropout_refusals(L):
+    def f(X=FAKE, ldx=8, Y=2 * FAKE, ldy=8, N=4, D=8, p=0.5, seed=1, step=0, at=None, dt=F32):
+        return L.hd_dropout(X, ldx, Y, ldy, N, D, p, seed, step, at, dt, None)
+
+    assert f(X=None) == ARG and f(Y=None) == ARG and f(ldx=7) == ARG and f(ldy=7) == ARG
+    assert f(N=-1) == ARG and f(D=0) == ARG and f(dt=8) == ARG and f(at=FAKE + 4) == ARG
+    for p in (-0.1, 1.1, math.nan, math.inf):
+        assert f(p=p) == ARG
+    assert f(X=FAKE + 2) == ARG and f(Y=2 * FAKE + 1) == ARG
+    assert f(Y=FAKE, ldy=9) == ARG  # in place with another stride
+    assert f(dt=I8) == UNSUP and f(N=(1 << 30) + 1) == UNSUP and f(ldx=BIG + 1) == UNSUP
+    assert f(N=0, X=None, Y=None) == OK
+
+
+def test_binding_refusals():
+    x = torch.zeros(2, 8)
+    y = torch.zeros(2, dtype=torch.int32)
+    for call in (lambda: hd.class_loss(x, x, y), lambda: hd.byte_quantize(x),
+                 lambda: hd.byte_rows(x), lambda: hd.dropout(x, 0.5, 1),
+                 lambda: hd.byte_pack(x.to(torch.int8), torch.ones(2)),
+                 lambda: hd.byte_product(x.to(torch.int8), None)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_philox_published_outputs():
+    """The generator's known answers (Random123's kat_vectors, philox4x32 10)."""
+    ones = 0xFFFFFFFF
+    for counter, key, want in (
+            ((0, 0, 0, 0), (0, 0), (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+            ((ones,) * 4, (ones,) * 2, (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+            ((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0),
+             (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1))):
+        assert tuple(int(v) for v in P.philox([np.uint64(c) for c in counter], key)) == want
+
+
+def test_int8_rule():
+    X = torch.tensor([[127.0, -63.5, 0.4, math.nan], [0.0, 0.0, 0.0, 0.0], [254.0, 1.0, 3.0, -5.0]])
+    q, s = P.int8_codes(X)
+    assert q.tolist() == [[0, 0, 0, 0], [0, 0, 0, 0], [127, 0, 2, -2]] and math.isnan(s[0])
+    assert float(s[1]) == 0 and abs(float(s[2]) - 2) < 1e-6
