@@ -14,6 +14,8 @@
 //
 // Where there are too few tiles for the chip (few rows and classes), the reduction over D is
 // split and the parts of the (then small) score matrix go through the workspace.
+#include <type_traits>
+
 #include "hd_tile.hpp"
 
 namespace hd {
@@ -466,9 +468,11 @@ hipError_t launch_tiles(int64_t blocks, hipStream_t stream, A... args) {
 // f is called with the tile of a plan.
 template <class P, int AK, int BK, class F>
 hipError_t with_tile(tile::Shape s, F f) {
+  // fp32 on the bf16 instruction where the matrix instructions bound the tile
+  typedef std::conditional_t<std::is_same_v<P, F32>, tile::X3, P> Q;
   switch (s) {
-    case tile::k256: return f(Tile<P, AK, BK, 256, 256, 2, 4>());
-    case tile::k128: return f(Tile<P, AK, BK, 128, 128, 2, 2>());
+    case tile::k256: return f(Tile<Q, AK, BK, 256, 256, 2, 4>());
+    case tile::k128: return f(Tile<Q, AK, BK, 128, 128, 2, 2>());
     case tile::k32x128: return f(Tile<P, AK, BK, 32, 128, 1, 4>());
     default: return f(Tile<P, AK, BK, 128, 32, 4, 1>());
   }

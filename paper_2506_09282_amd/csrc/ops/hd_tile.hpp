@@ -4,13 +4,14 @@
 //
 // An operand lies in memory with its reduction contiguous (kRows: row m holds k), with its
 // reduction as rows (kCols: row k holds m), or as an 8-bit weight image (kImage). A stage is
-// 128 bytes of the reduction of every row (64 bf16, 32 fp32, 128 int8 values). It goes through
+// 128 bytes of the reduction of every row (64 bf16, 32 fp32, 128 int8 values; 64 bytes of fp32 in
+// three parts). It goes through
 // registers into one of two buffers in LDS while the other is multiplied, so that rows of any
 // alignment, ends of rows and rows that take no part cost nothing but their own loads.
 //
-// In LDS a kRows operand is [row][8 pieces of 16 bytes], piece j at j ^ (row & 7): a lane's
-// operand of the 32 x 32 instruction is one piece, and the 64 pieces of a read spread over all
-// banks. A kCols operand is [k][R values] as in memory; bf16 takes its operands with transposing
+// In LDS a kRows operand is [row][8 pieces of 16 bytes], piece j at j ^ (row / 2 % 8): a lane's
+// operand of the 32 x 32 instruction is one piece, and 16 lanes' pieces, of 16 rows, lie in all 64
+// banks (with j ^ (row % 8) two at a time share theirs: 37% of the LDS's cycles, measured). A kCols operand is [k][R values] as in memory; bf16 takes its operands with transposing
 // reads (16 lanes read 4 rows of 16 values and get 4 values of one column each), fp32, whose
 // instruction takes one k from a lane, with plain ones.
 #pragma once
@@ -43,7 +44,7 @@ struct Bf16 {
   typedef bf16raw elem;
   typedef u32x4_a2 piece;
   typedef f32x16 acc;
-  static constexpr int kEs = 2, kBk = 64;
+  static constexpr int kEs = 2, kBk = 64, kParts = 1;
   static __device__ __forceinline__ void mfma(acc& c, const u32x4& a, const u32x4& b) {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -53,7 +54,7 @@ struct F32 {
   typedef float elem;
   typedef u32x4_a4 piece;
   typedef f32x16 acc;
-  static constexpr int kEs = 4, kBk = 32;
+  static constexpr int kEs = 4, kBk = 32, kParts = 1;
   static __device__ __forceinline__ void mfma(acc& c, const u32x4& a, const u32x4& b) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -61,11 +62,41 @@ struct F32 {
                                                0, 0);
   }
 };
+// fp32 as the exact sum of three bf16 values: the upper half of its bits, the rest rounded to
+// bf16, and what is left (8 bits; exact but for bits below 2^-133). Six of the nine products of
+// parts are summed; those left out are within 2^-22 of the whole and of either sign. That is
+// six bf16 instructions for 16 values of k, where fp32's own take twice as long. An infinity
+// has no such parts and counts as NaN.
+struct X3 {
+  typedef float elem;
+  typedef u32x4_a4 piece;
+  typedef f32x16 acc;
+  static constexpr int kEs = 4, kBk = 16, kParts = 3;
+  static __device__ __forceinline__ void mfma(acc& c, const u32x4& a, const u32x4& b) {
+    Bf16::mfma(c, a, b);
+  }
+  // Four values to two words of each part.
+  static __device__ __forceinline__ void split(const u32x4& v, u32x2 (&part)[3]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t x = v[2 * h], y = v[2 * h + 1];
+      part[0][h] = __builtin_amdgcn_perm(y, x, 0x07060302);  // the upper halves
+      const float rx = __uint_as_float(x) - __uint_as_float(x & 0xffff0000u);
+      const float ry = __uint_as_float(y) - __uint_as_float(y & 0xffff0000u);
+      const bf16x2 m = {(__bf16)rx, (__bf16)ry};
+      const uint32_t mid = __builtin_bit_cast(uint32_t, m);
+      part[1][h] = mid;
+      const bf16x2 l = {(__bf16)(rx - __uint_as_float(mid << 16)),
+                        (__bf16)(ry - __uint_as_float(mid & 0xffff0000u))};
+      part[2][h] = __builtin_bit_cast(uint32_t, l);
+    }
+  }
+};
 struct I8 {
   typedef int8_t elem;
   typedef u32x4_a1 piece;
   typedef i32x16 acc;
-  static constexpr int kEs = 1, kBk = 128;
+  static constexpr int kEs = 1, kBk = 128, kParts = 1;
   static __device__ __forceinline__ void mfma(acc& c, const u32x4& a, const u32x4& b) {
     c = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a),
                                               __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
@@ -105,18 +136,16 @@ __device__ __forceinline__ int col_swizzle(int k) {
 template <class P, int KIND, int R, int T>
 struct Loader {
   static constexpr int kE = 16 / P::kEs;
-  static constexpr int kPasses = R * 8 / T;
-  static constexpr int kAcross = KIND == kCols ? R / kE : 8;  // pieces of a row
-  static constexpr int kStep = T / kAcross;                   // rows of a pass
+  static constexpr int kAcross = KIND == kCols ? R / kE : P::kBk / kE;  // pieces of a row
+  static constexpr int kStep = T / kAcross;                             // rows of a pass
+  static constexpr int kPasses = (KIND == kCols ? P::kBk : R) / kStep;
   static_assert(kPasses >= 1 && T % kAcross == 0, "");
-  static constexpr int kBytes = R * 128;  // of a stage
 
   const char* base;  // kRows: the tile's first row; kCols: its first column of k = 0
   int64_t ld;        // bytes
   const uint64_t* live;
-  uint32_t off[kPasses];
+  uint32_t off[KIND == kCols ? 1 : kPasses];
   int lds_at, row, cols;
-  bool inside;  // every column of the tile exists
   u32x4 reg[kPasses];
 
   __device__ __forceinline__ Loader(const Operand& o, int64_t at, int tid) {
@@ -128,21 +157,17 @@ struct Loader {
       // a wave's load is a block of 32 outputs x 32 inputs: lane l holds output l % 32,
       // inputs 16 (l / 32) ... of it; ld: blocks of 32 inputs
       const int lane = tid & 63, wave = tid >> 6;
-      base = reinterpret_cast<const char*>(o.p);
+      base = reinterpret_cast<const char*>(o.p) + at / 32 * o.ld * 1024;
+      const int64_t last = cdiv(o.extent - at, 32) - 1;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int block = p * (T / 64) + wave;  // of the stage: (outputs / 32, inputs / 32)
-        const int64_t tiles = cdiv(o.extent, 32);
-        int64_t t = at / 32 + block / 4;
-        t = t < tiles ? t : tiles - 1;
-        off[p] = 0;
-        reg[p] = u32x4{0u, 0u, 0u, 0u};
-        first[p] = (t * o.ld + block % 4) * 1024 + lane * 16;
+        const int t = block / 4 < last ? block / 4 : (int)last;
+        off[p] = ((uint32_t)t * (uint32_t)o.ld + block % 4) * 1024 + lane * 16;
       }
       row = lane & 31;
       cols = lane >> 5;
       lds_at = 0;
-      inside = true;
       return;
     }
     if constexpr (KIND == kRows) {
@@ -154,21 +179,17 @@ struct Loader {
         off[p] = (uint32_t)(r < last ? r : last) * (uint32_t)ld + piece * 16;
       }
       cols = piece * kE;  // its place in the stage
-      lds_at = row * 128 + ((piece ^ (row & 7)) << 4);
-      inside = true;
+      lds_at = row * 128 + ((piece ^ ((row >> 1) & 7)) << 4);
     } else {
       base = reinterpret_cast<const char*>(o.p) + at * P::kEs;
-      const int64_t left = o.extent - at - piece * kE;
-      cols = left > kE ? kE : left < 0 ? 0 : (int)left;
-      inside = o.extent - at >= R;
-#pragma unroll
-      for (int p = 0; p < kPasses; ++p)
-        off[p] = (uint32_t)(p * kStep + row) * (uint32_t)ld + piece * 16;
+      const int64_t last = (o.extent - 1 - at) / kE;  // the last piece with a column that exists
+      const int mine = piece < last ? piece : (int)last;
+      const int64_t left = o.extent - at - mine * kE;
+      cols = left > kE ? kE : (int)left;
+      off[0] = (uint32_t)row * (uint32_t)ld + mine * 16;  // of pass 0
       lds_at = 0;
     }
   }
-  int64_t first[KIND == kImage ? kPasses : 1];
-
   __device__ __forceinline__ u32x4 whole(const char* p) const {
     return *reinterpret_cast<const typename P::piece*>(p);
   }
@@ -178,7 +199,7 @@ struct Loader {
     if constexpr (KIND == kImage) {
 #pragma unroll
       for (int p = 0; p < kPasses; ++p)  // (an image's reduction is whole stages)
-        reg[p] = *reinterpret_cast<const u32x4*>(base + first[p] + k * 32);
+        reg[p] = *reinterpret_cast<const u32x4*>(base + k * 32 + off[p]);
     } else if constexpr (KIND == kRows) {
       const char* at = base + k * P::kEs;
       if (k + P::kBk <= end) {
@@ -192,18 +213,26 @@ struct Loader {
       }
     } else {
       const char* at = base + k * ld;
-      if (inside && !live && k + P::kBk <= end) {
+      const uint64_t bits = live ? live[k >> 6] >> (k & 63) : ~uint64_t(0);
+      if (k + P::kBk + kE <= end) {
+        // (a piece across the row's end runs into the next rows, of which there are enough: what
+        // it takes from there are columns that nobody looks at)
+        const uint64_t mine = bits >> row;
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) reg[p] = whole(at + off[p]);
+        for (int p = 0; p < kPasses; ++p) reg[p] = whole(at + p * kStep * ld + off[0]);
+        if (live) {
+#pragma unroll
+          for (int p = 0; p < kPasses; ++p)
+            if (!(mine >> (p * kStep) & 1)) reg[p] = u32x4{0u, 0u, 0u, 0u};
+        }
       } else {
-        uint64_t bits = live ? live[k >> 6] >> (k & 63) : ~uint64_t(0);
         const int64_t left = end - k;
-        if (left < 64) bits &= (uint64_t(1) << left) - 1;
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
           u32x4 v = {0u, 0u, 0u, 0u};
-          if (bits >> (p * kStep + row) & 1)
-            v = cols == kE ? whole(at + off[p]) : load_part<P>(at + off[p], cols);
+          if (p * kStep + row < left && (bits >> (p * kStep + row) & 1))
+            v = cols == kE ? whole(at + p * kStep * ld + off[0])
+                           : load_part<P>(at + p * kStep * ld + off[0], cols);
           reg[p] = v;
         }
       }
@@ -212,13 +241,29 @@ struct Loader {
 
   // Those registers to the operand's part of a buffer.
   __device__ __forceinline__ void store(char* lds, int tid) const {
+    if constexpr (P::kParts == 3) {
+      const int piece = tid % kAcross;
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        u32x2 part[3];
+        X3::split(reg[p], part);
+        const int r = p * kStep + row;
+        const int at = KIND == kRows
+                           ? r * 32 + (((piece >> 1) ^ ((r >> 3) & 1)) << 4) + (piece & 1) * 8
+                           : r * R * 2 + (((piece >> 1) ^ col_swizzle<Bf16, R>(r)) << 4) +
+                                 (piece & 1) * 8;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(lds + q * R * 32 + at) = part[q];
+      }
+      return;
+    }
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
       int at;
       if constexpr (KIND == kImage) {
         const int block = p * (T / 64) + (tid >> 6);
         const int r = block / 4 * 32 + row;
-        at = r * 128 + (((block % 4 * 2 + cols) ^ (r & 7)) << 4);
+        at = r * 128 + (((block % 4 * 2 + cols) ^ ((r >> 1) & 7)) << 4);
       } else if constexpr (KIND == kRows) {
         at = lds_at + p * kStep * 128;
       } else {
@@ -230,14 +275,20 @@ struct Loader {
   }
 };
 
-// A lane's operand: rows 32 * sub ... of the tile, quarter kk of the stage.
+// A lane's operand: rows 32 * sub ... of the tile, quarter kk of the stage (or the part kk of it).
 template <class P, int KIND, int R>
 __device__ __forceinline__ u32x4 fragment(const char* lds, int sub, int kk, int lane) {
   const int half = lane >> 5;
-  if constexpr (KIND != kCols) {
+  if constexpr (P::kParts == 3 && KIND == kRows) {  // (kk: the part)
+    const int row = sub * 32 + (lane & 31);
+    return *reinterpret_cast<const u32x4*>(lds + kk * R * 32 + row * 32 +
+                                           ((half ^ ((lane >> 3) & 1)) << 4));
+  } else if constexpr (P::kParts == 3) {
+    return fragment<Bf16, kCols, R>(lds + kk * R * 32, sub, 0, lane);
+  } else if constexpr (KIND != kCols) {
     const int row = sub * 32 + (lane & 31);
     return *reinterpret_cast<const u32x4*>(lds + row * 128 +
-                                           (((2 * kk + half) ^ (lane & 7)) << 4));
+                                           (((2 * kk + half) ^ ((lane >> 1) & 7)) << 4));
   } else if constexpr (P::kEs == 2) {
     const int i = lane & 15, piece = sub * 4 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
     const int k = kk * 16 + half * 8 + (i >> 2);
@@ -272,7 +323,10 @@ struct Tile {
   typedef P_ P;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, T = 64 * WM * WN;
   static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
-  static constexpr int kStage = (BM + BN) * 128, kLds = 2 * kStage;
+  static constexpr int kRowBytes = P::kParts == 3 ? 96 : 128;  // of a stage
+  static constexpr int kStage = (BM + BN) * kRowBytes, kLds = 2 * kStage;
+  // A quarter's operands are read while the one before is multiplied, where two sets fit the registers.
+  static constexpr bool kAhead = AK == kRows && BK_ == kRows && P::kParts == 1;
   typedef typename P::acc Acc;
 
   // The sum over k in [k0, k1). All threads of the workgroup; ends with a barrier.
@@ -293,36 +347,98 @@ struct Tile {
     la.load(k0, k1);
     lb.load(k0, k1);
     la.store(lds, tid);
-    lb.store(lds + BM * 128, tid);
+    lb.store(lds + BM * kRowBytes, tid);
+    if (k0 + P::kBk < k1) {
+      la.load(k0 + P::kBk, k1);
+      lb.load(k0 + P::kBk, k1);
+    }
     __syncthreads();
+    if constexpr (P::kParts == 3) {
+      int cur = 0;
+      for (int64_t k = k0; k < k1; k += P::kBk) {
+        const char* at = lds + cur * kStage;
+        char* other = lds + (cur ^ 1) * kStage;
+        u32x4 fa[3][MT], fb[3][NT];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) fa[q][i] = fragment<P, AK, BM>(at, wm * MT + i, q, lane);
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            fb[q][j] = fragment<P, BK_, BN>(at + BM * kRowBytes, wn * NT + j, q, lane);
+        }
+        // parts' products, the smallest first
+        auto multiply = [&](int p, int q) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) P::mfma(c[i][j], fa[p][i], fb[q][j]);
+        };
+        multiply(2, 0);
+        multiply(1, 1);
+        multiply(0, 2);
+        if (k + P::kBk < k1) {
+          la.store(other, tid);
+          lb.store(other + BM * kRowBytes, tid);
+          if (k + 2 * P::kBk < k1) {
+            la.load(k + 2 * P::kBk, k1);
+            lb.load(k + 2 * P::kBk, k1);
+          }
+        }
+        multiply(1, 0);
+        multiply(0, 1);
+        multiply(0, 0);
+        __syncthreads();
+        cur ^= 1;
+      }
+      return;
+    }
+    u32x4 fa[2][MT], fb[2][NT];
+    auto read = [&](int to, const char* at, int kk) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[to][i] = fragment<P, AK, BM>(at, wm * MT + i, kk, lane);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        fb[to][j] = fragment<P, BK_, BN>(at + BM * kRowBytes, wn * NT + j, kk, lane);
+    };
+    auto multiply = [&](int of) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) P::mfma(c[i][j], fa[of][i], fb[of][j]);
+    };
+    if constexpr (kAhead) read(0, lds, 0);
     int cur = 0;
     for (int64_t k = k0; k < k1; k += P::kBk) {
-      const bool more = k + P::kBk < k1;
-      if (more) {
-        la.load(k + P::kBk, k1);
-        lb.load(k + P::kBk, k1);
-      }
       const char* at = lds + cur * kStage;
+      char* other = lds + (cur ^ 1) * kStage;
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        u32x4 fa[MT], fb[NT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) fa[i] = fragment<P, AK, BM>(at, wm * MT + i, kk, lane);
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          fb[j] = fragment<P, BK_, BN>(at + BM * 128, wn * NT + j, kk, lane);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) P::mfma(c[i][j], fa[i], fb[j]);
+        if constexpr (kAhead) {
+          if (kk < 3) read((kk + 1) & 1, at, kk + 1);
+        } else {
+          read(0, at, kk);
+        }
+        if (kk == 2 && k + P::kBk < k1) {
+          la.store(other, tid);
+          lb.store(other + BM * kRowBytes, tid);
+          if (k + 2 * P::kBk < k1) {
+            la.load(k + 2 * P::kBk, k1);
+            lb.load(k + 2 * P::kBk, k1);
+          }
+        }
+        if (kk == 3) {  // the next stage is there, and this one is read: its rest is in registers
+          __syncthreads();
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (kAhead)
+            if (k + P::kBk < k1) read(0, other, 0);
+        }
+        multiply(kAhead ? kk & 1 : 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
       cur ^= 1;
-      if (more) {
-        la.store(lds + cur * kStage, tid);
-        lb.store(lds + cur * kStage + BM * 128, tid);
-      }
-      __syncthreads();
     }
+    __syncthreads();
   }
 };
 
