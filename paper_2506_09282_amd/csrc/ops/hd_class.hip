@@ -217,60 +217,111 @@ __global__ __launch_bounds__(TL::T, 2) void class_scores_kernel(Scores a, int64_
 }
 
 struct Parts {
-  const float* p;  // [parts][N][ld]
+  const float* p;  // [count][N][ld], ld a multiple of 4
   int64_t ld, N;
   int count;
 };
-__device__ __forceinline__ float score_of(const Parts& s, int64_t n, int64_t k) {
-  float v = 0.0f;
-  for (int i = 0; i < s.count; ++i) v += s.p[((int64_t)i * s.N + n) * s.ld + k];
+// Four scores of a row, of every `step`-th part from `first` on.
+__device__ __forceinline__ f32x4 scores_of(const Parts& s, int64_t n, int64_t k, int first,
+                                           int step) {
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  const float* at = s.p + (first * s.N + n) * s.ld + k;
+#pragma unroll 8
+  for (int i = first; i < s.count; i += step, at += step * s.N * s.ld)
+    v += *reinterpret_cast<const f32x4*>(at);
+  return v;
+}
+// The sum over PG groups of threads that each hold every PG-th part; `lane` of `lanes` in a
+// group. All threads call it; the first group has the sums.
+template <int PG>
+__device__ __forceinline__ f32x4 join_groups(f32x4 v, int group, int lane, int lanes, f32x4* lds) {
+  if constexpr (PG > 1) {
+    lds[group * lanes + lane] = v;
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+      for (int g = 1; g < PG; ++g) v += lds[g * lanes + lane];
+    }
+  }
   return v;
 }
 
-// W waves to a row.
-template <int W>
+// A bit for each of four classes from k on that takes part. (Without a branch: this compiler has
+// lost the values of short-circuited conditions that write parts of a vector.)
+__device__ __forceinline__ uint32_t open4(const uint8_t* mask, int64_t k, int64_t K) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t at = k + e < K ? k + e : K - 1;
+    const uint32_t open = mask ? (uint32_t)(mask[at] != 0) : 1u;
+    bits |= (open & (uint32_t)(k + e < K)) << e;
+  }
+  return bits;
+}
+
+// m and s of a row over 2^x neighbouring lanes.
+template <int LANES>
+__device__ __forceinline__ void join_lanes(float& m, float& s, float c) {
+  join(m, s, lane_xor<1>(m), lane_xor<1>(s), c);
+  join(m, s, lane_xor<2>(m), lane_xor<2>(s), c);
+  join(m, s, lane_xor<4>(m), lane_xor<4>(s), c);
+  if constexpr (LANES > 8) {
+    join(m, s, lane_xor<8>(m), lane_xor<8>(s), c);
+    join(m, s, lane_xor<16>(m), lane_xor<16>(s), c);
+    join(m, s, lane_xor<32>(m), lane_xor<32>(s), c);
+  }
+}
+
+// A row's loss from the parts of its scores. G lanes take four classes each (G = 256: again and
+// again, else G lanes cover the row), PG groups of them share the parts.
+template <int G, int PG>
 __global__ __launch_bounds__(kThreads) void class_rows_kernel(
-    Parts sc, const int32_t* __restrict__ y, const uint64_t* __restrict__ open, int64_t K,
+    Parts sc, const int32_t* __restrict__ y, const uint8_t* __restrict__ mask, int64_t K,
     float scale, float* __restrict__ loss, float* __restrict__ stats) {
+  constexpr int kRowsOf = kThreads / (G * PG);
+  __shared__ f32x4 sums[PG > 1 ? kThreads : 1];
   __shared__ float2 part[kThreads / 64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (4 / W) + wave / W;
-  const bool there = row < sc.N;  // (all threads meet at the barrier)
-  const int64_t n = there ? row : sc.N - 1;
+  __shared__ float target[kRowsOf];
+  const int lane = threadIdx.x % G, group = threadIdx.x / G % PG, row = threadIdx.x / (G * PG);
+  const int64_t at = (int64_t)blockIdx.x * kRowsOf + row;
+  const bool there = at < sc.N;  // (all threads meet at the barriers)
+  const int64_t n = there ? at : sc.N - 1;
+  const int32_t yn = y[n];
+  const bool asks = asked(yn, K);
   const float scale2 = scale * kLog2e;
   float m = -INFINITY, s = 0.0f;
-  for (int64_t k = (wave % W) * 64 + lane; k < K; k += 64 * W) {
-    if (open && !(open[k >> 6] >> (k & 63) & 1)) continue;
-    const float v = score_of(sc, n, k);
-    // (a score of NaN is no maximum, and makes the sum NaN)
-    if (v > m) {
-      s = m == -INFINITY ? s + 1.0f : s * exp2f(scale2 * (m - v)) + 1.0f;
-      if (v == INFINITY) s = NAN;
-      m = v;
-    } else if (v != -INFINITY) {
-      s += exp2f(scale2 * (v - (m == -INFINITY ? 0.0f : m)));
+  for (int64_t k0 = 0; k0 < K; k0 += 4 * G) {
+    const int64_t k = k0 + 4 * lane;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (k < K) v = scores_of(sc, n, k, group, PG);
+    v = join_groups<PG>(v, group, lane, G, sums);
+    const uint32_t bits = open4(mask, k, K);
+    float x[4], top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = bits >> e & 1 ? v[e] : -INFINITY;
+      top = fmaxf(top, x[e]);
     }
+    const int64_t place = (int64_t)yn - k;
+    if (asks & (group == 0) & (place >= 0) & (place < 4))
+      target[row] = place < 2 ? (place == 0 ? x[0] : x[1]) : (place == 2 ? x[2] : x[3]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += exp2f(scale2 * (x[e] - base));
+    join(m, s, top, sum, scale2);
   }
-  join(m, s, lane_xor<1>(m), lane_xor<1>(s), scale2);
-  join(m, s, lane_xor<2>(m), lane_xor<2>(s), scale2);
-  join(m, s, lane_xor<4>(m), lane_xor<4>(s), scale2);
-  join(m, s, lane_xor<8>(m), lane_xor<8>(s), scale2);
-  join(m, s, lane_xor<16>(m), lane_xor<16>(s), scale2);
-  join(m, s, lane_xor<32>(m), lane_xor<32>(s), scale2);
-  if constexpr (W > 1) {
-    if (lane == 0) part[wave] = make_float2(m, s);
-    __syncthreads();
+  join_lanes<(G < 64 ? G : 64)>(m, s, scale2);
+  if constexpr (G > 64)
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(m, s);
+  __syncthreads();
+  if constexpr (G > 64) {
     m = part[0].x;
     s = part[0].y;
-    for (int w = 1; w < W; ++w) join(m, s, part[w].x, part[w].y, scale2);
+    for (int w = 1; w < kThreads / 64; ++w) join(m, s, part[w].x, part[w].y, scale2);
   }
-  if (there && lane == 0 && wave % W == 0) {
-    const bool asks = asked(y[n], K);
-    float t = 0.0f;
-    if (asks)
-      t = open && !(open[y[n] >> 6] >> (y[n] & 63) & 1) ? -INFINITY : score_of(sc, n, y[n]);
-    finish_row(m, s, t, asks, scale, loss + n, stats + 2 * n);
-  }
+  if (there && lane == 0 && group == 0)
+    finish_row(m, s, asks ? target[row] : 0.0f, asks, scale, loss + n, stats + 2 * n);
 }
 
 // ---- backward: the scores' gradient ---------------------------------------------------
@@ -345,20 +396,59 @@ __global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
   }
 }
 
-// The same from the parts of the scores; a thread takes a class of a row.
-template <typename T>
+// Bits of the rows that ask for a class (word w of them), then of the open classes; a wave to a
+// word. Either may be null.
+__device__ __forceinline__ void write_bits(int64_t w, const int32_t* y, int64_t N, uint64_t* rows,
+                                           const uint8_t* mask, int64_t K, uint64_t* classes) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row_words = rows ? cdiv(N, 64) : 0;
+  if (w < row_words) {
+    const int64_t n = w * 64 + lane;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(n < N && asked(y[n], K));
+    if (lane == 0) rows[w] = b;
+    return;
+  }
+  w -= row_words;
+  if (!classes || w >= cdiv(K, 64)) return;
+  const int64_t k = w * 64 + lane;
+  const uint64_t b = __builtin_amdgcn_ballot_w64(k < K && mask[k] != 0);
+  if (lane == 0) classes[w] = b;
+}
+__global__ __launch_bounds__(kThreads) void class_bits_kernel(const int32_t* __restrict__ y,
+                                                              int64_t N, uint64_t* rows,
+                                                              const uint8_t* __restrict__ mask,
+                                                              int64_t K, uint64_t* classes) {
+  write_bits((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), y, N, rows, mask, K,
+             classes);
+}
+
+// dS from the parts of the scores (all classes); a thread takes four classes of a row, PG groups
+// of threads share the parts. The blocks behind them write the bits.
+template <typename T, int PG>
 __global__ __launch_bounds__(kThreads) void class_dscores_parts_kernel(
-    Scores a, int64_t K_all, Parts sc, const float* __restrict__ stats,
-    const float* __restrict__ g, T* __restrict__ dS, int64_t ld) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t n = i / ld, k = i - n * ld;
-  if (n >= a.N) return;
-  const bool open = k < a.K && (!a.open || (a.open[k >> 6] >> (k & 63) & 1));
-  float v = 0.0f;
-  if (open)
-    v = score_grad(row_grad(a, stats, g, K_all, n), score_of(sc, n, k), k, true,
-                   a.scale * kLog2e);
-  store_elem(dS, i, v);
+    Scores a, Parts sc, const float* __restrict__ stats, const float* __restrict__ g,
+    T* __restrict__ dS, int64_t ld, const uint8_t* __restrict__ mask, uint32_t blocks,
+    uint64_t* rows, uint64_t* classes) {
+  constexpr int kLanes = kThreads / PG;
+  __shared__ f32x4 sums[PG > 1 ? kThreads : 1];
+  if (blockIdx.x >= blocks) {
+    write_bits((int64_t)(blockIdx.x - blocks) * (kThreads / 64) + (threadIdx.x >> 6), a.y, a.N,
+               rows, mask, a.K, classes);
+    return;
+  }
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const int64_t at = (int64_t)blockIdx.x * kLanes + lane, quads = ld / 4;
+  const int64_t n = at / quads, k = (at - n * quads) * 4;
+  const bool there = n < a.N;
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (there && k < a.K) v = scores_of(sc, n, k, group, PG);
+  v = join_groups<PG>(v, group, lane, kLanes, sums);
+  if (!there || group != 0) return;
+  const RowGrad row = row_grad(a, stats, g, a.K, n);
+  const uint32_t bits = open4(mask, k, a.K);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    store_elem(dS, n * ld + k + e, score_grad(row, v[e], k + e, bits >> e & 1, a.scale * kLog2e));
 }
 
 // ---- backward: the products -------------------------------------------------------------
@@ -423,30 +513,7 @@ __global__ __launch_bounds__(kThreads) void class_sum_kernel(Out o, int count) {
   put<T>(o, at, v);
 }
 
-// Bits of the rows that ask for a class, and of the open classes.
-__global__ __launch_bounds__(kThreads) void class_bits_kernel(const int32_t* __restrict__ y,
-                                                              int64_t N, uint64_t* rows,
-                                                              const uint8_t* __restrict__ mask,
-                                                              int64_t K, uint64_t* classes) {
-  const int64_t row_words = rows ? cdiv(N, 64) : 0;
-  int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (w < row_words) {
-    const int64_t n = w * 64 + lane;
-    const uint64_t b = __builtin_amdgcn_ballot_w64(n < N && asked(y[n], K));
-    if (lane == 0) rows[w] = b;
-    return;
-  }
-  w -= row_words;
-  if (!mask || w >= cdiv(K, 64)) return;
-  const int64_t k = w * 64 + lane;
-  const uint64_t b = __builtin_amdgcn_ballot_w64(k < K && mask[k] != 0);
-  if (lane == 0) classes[w] = b;
-}
-
 // ---- host -------------------------------------------------------------------------------
-
-hipError_t last_error() { return hipGetLastError(); }
 
 template <auto KERNEL>
 hipError_t allow_lds(int bytes) {
@@ -462,7 +529,7 @@ hipError_t launch_tiles(int64_t blocks, hipStream_t stream, A... args) {
   const hipError_t e = allow_lds<KERNEL>(TL::kLds);
   if (e != hipSuccess) return e;
   KERNEL<<<dim3((uint32_t)blocks), dim3(TL::T), TL::kLds, stream>>>(args...);
-  return last_error();
+  return hipGetLastError();
 }
 
 // f is called with the tile of a plan.
@@ -540,15 +607,27 @@ GradPlace grad_place(int64_t N, int64_t D, int64_t K, int64_t es) {
 }
 
 template <class P>
+hipError_t run_scores(const Scores& a, const Plan& p, float* parts, hipStream_t stream) {
+  return with_tile<P, kRows, kRows>(p.shape, [&](auto t) {
+    typedef decltype(t) TL;
+    if constexpr (TL::BM * TL::BN > 128 * 128)
+      return hipErrorInvalidValue;  // (the large tile is not split)
+    else
+      return launch_tiles<class_scores_kernel<TL>, TL>(p.mt * p.nt * p.splits, stream, a, p.each,
+                                                       parts);
+  });
+}
+
+template <class P>
 hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hipStream_t stream) {
   const LossPlace w = loss_place(c.N, c.D, c.K);
-  uint64_t* open = nullptr;
   hipError_t e;
-  if (c.mask) {
+  uint64_t* open = nullptr;
+  if (c.mask && w.s.splits == 1) {
     open = reinterpret_cast<uint64_t*>(ws + w.open);
     class_bits_kernel<<<dim3((uint32_t)cdiv(cdiv(c.K, 64), kThreads / 64)), dim3(kThreads), 0,
                         stream>>>(nullptr, 0, nullptr, c.mask, c.K, open);
-    if ((e = last_error()) != hipSuccess) return e;
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   const Scores a{{c.H, c.ldh, c.N, nullptr}, {c.C, c.ldc, c.K, nullptr}, c.y, open, c.scale,
                  c.N, c.D, c.K, 0, (uint32_t)w.s.mt, (uint32_t)w.s.nt};
@@ -565,25 +644,22 @@ hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hip
     class_join_kernel<<<dim3((uint32_t)cdiv(c.N, kThreads / 64)), dim3(kThreads), 0, stream>>>(
         reinterpret_cast<const float2*>(parts), target, c.y, c.N, c.K, (int)w.s.mt, c.scale, loss,
         stats);
-    return last_error();
+    return hipGetLastError();
   }
-  e = with_tile<P, kRows, kRows>(w.s.shape, [&](auto t) {
-    typedef decltype(t) TL;
-    if constexpr (TL::BM * TL::BN > 128 * 128)
-      return hipErrorInvalidValue;  // (the large tile is not split)
-    else
-      return launch_tiles<class_scores_kernel<TL>, TL>(tiles * w.s.splits, stream, a, w.s.each,
-                                                       parts);
-  });
-  if (e != hipSuccess) return e;
+  if ((e = run_scores<P>(a, w.s, parts, stream)) != hipSuccess) return e;
   const Parts sc{parts, w.s.mt * tile_m(w.s), c.N, (int)w.s.splits};
-  if (c.K <= 512)
-    class_rows_kernel<1><<<dim3((uint32_t)cdiv(c.N, 4)), dim3(kThreads), 0, stream>>>(
-        sc, c.y, open, c.K, c.scale, loss, stats);
-  else
-    class_rows_kernel<4><<<dim3((uint32_t)c.N), dim3(kThreads), 0, stream>>>(
-        sc, c.y, open, c.K, c.scale, loss, stats);
-  return last_error();
+  auto rows = [&](auto* kernel, int each) {
+    kernel<<<dim3((uint32_t)cdiv(c.N, each)), dim3(kThreads), 0, stream>>>(
+        sc, c.y, c.mask, c.K, c.scale, loss, stats);
+    return hipGetLastError();
+  };
+  // Many parts are those of few rows: a workgroup to a row shares them.
+  const bool many = sc.count > 8;
+  if (c.K <= 32)
+    return many ? rows(class_rows_kernel<8, 32>, 1) : rows(class_rows_kernel<8, 1>, 32);
+  if (c.K <= 256)
+    return many ? rows(class_rows_kernel<64, 4>, 1) : rows(class_rows_kernel<64, 1>, 4);
+  return rows(class_rows_kernel<256, 1>, 1);
 }
 
 template <class P, int AK, int BK>
@@ -599,7 +675,7 @@ hipError_t run_product(const Operand& a, const Operand& b, int64_t K, Out o, flo
   if (e != hipSuccess || p.splits == 1) return e;
   class_sum_kernel<typename P::elem>
       <<<dim3((uint32_t)cdiv(o.M * o.N, kThreads)), dim3(kThreads), 0, stream>>>(o, (int)p.splits);
-  return last_error();
+  return hipGetLastError();
 }
 
 template <class P>
@@ -609,17 +685,25 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
   const GradPlace w = grad_place(c.N, c.D, c.K, P::kEs);
   uint64_t* rows = reinterpret_cast<uint64_t*>(ws + w.rows);
   uint64_t* open = reinterpret_cast<uint64_t*>(ws + w.open);
+  if (!dC) rows = nullptr;
+  if (!c.mask) open = nullptr;
+  // (in one piece the scores' parts may be summed by a launch that writes the bits too)
+  const Plan whole = tile::plan(c.K, c.N, c.D);
+  const uint32_t bit_blocks = (uint32_t)cdiv((rows ? cdiv(c.N, 64) : 0) + (open ? cdiv(c.K, 64) : 0),
+                                             kThreads / 64);
   hipError_t e;
-  class_bits_kernel<<<dim3((uint32_t)cdiv(cdiv(c.N, 64) + cdiv(c.K, 64), kThreads / 64)),
-                      dim3(kThreads), 0, stream>>>(c.y, c.N, rows, c.mask, c.K, open);
-  if ((e = last_error()) != hipSuccess) return e;
+  if (whole.splits == 1 && bit_blocks) {
+    class_bits_kernel<<<dim3(bit_blocks), dim3(kThreads), 0, stream>>>(c.y, c.N, rows, c.mask, c.K,
+                                                                       open);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   T* dS = reinterpret_cast<T*>(ws + w.dS);
   float* sums = reinterpret_cast<float*>(ws + w.sums);
   float* parts = reinterpret_cast<float*>(ws + w.parts);
   for (int64_t first = 0; first < c.K; first += w.piece) {
     const int64_t K = std::min(w.piece, c.K - first);
     const bool last = first + K == c.K;
-    const uint64_t* part_open = c.mask ? open + first / 64 : nullptr;
+    const uint64_t* part_open = open ? open + first / 64 : nullptr;
     const T* C = reinterpret_cast<const T*>(c.C) + first * c.ldc;
     Plan s = tile::plan(K, c.N, c.D);
     const int64_t tiles = s.mt * s.nt;
@@ -634,20 +718,16 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
       });
     } else {
       float* scores = reinterpret_cast<float*>(ws + w.scores);
-      e = with_tile<P, kRows, kRows>(s.shape, [&](auto t) {
-        typedef decltype(t) TL;
-        if constexpr (TL::BM * TL::BN > 128 * 128)
-          return hipErrorInvalidValue;
-        else
-          return launch_tiles<class_scores_kernel<TL>, TL>(tiles * s.splits, stream, a, s.each,
-                                                           scores);
-      });
-      if (e != hipSuccess) return e;
+      if ((e = run_scores<P>(a, s, scores, stream)) != hipSuccess) return e;
       const Parts sc{scores, s.mt * tile_m(s), c.N, (int)s.splits};
-      class_dscores_parts_kernel<T>
-          <<<dim3((uint32_t)cdiv(c.N * w.ld, kThreads)), dim3(kThreads), 0, stream>>>(
-              a, c.K, sc, stats, g, dS, w.ld);
-      e = last_error();
+      auto sum = [&](auto* kernel, int groups) {
+        const uint32_t blocks = (uint32_t)cdiv(c.N * w.ld / 4, kThreads / groups);
+        kernel<<<dim3(blocks + bit_blocks), dim3(kThreads), 0, stream>>>(
+            a, sc, stats, g, dS, w.ld, c.mask, blocks, rows, open);
+        return hipGetLastError();
+      };
+      e = sc.count > 8 ? sum(class_dscores_parts_kernel<T, 8>, 8)
+                       : sum(class_dscores_parts_kernel<T, 1>, 1);
     }
     if (e != hipSuccess) return e;
     if (dC) {

@@ -133,7 +133,7 @@ __device__ __forceinline__ int col_swizzle(int k) {
 }
 
 // One operand's way from memory to LDS: R rows (or columns) by T threads.
-template <class P, int KIND, int R, int T>
+template <class P, int KIND, int R, int T, int RING>
 struct Loader {
   static constexpr int kE = 16 / P::kEs;
   static constexpr int kAcross = KIND == kCols ? R / kE : P::kBk / kE;  // pieces of a row
@@ -146,7 +146,7 @@ struct Loader {
   const uint64_t* live;
   uint32_t off[KIND == kCols ? 1 : kPasses];
   int lds_at, row, cols;
-  u32x4 reg[kPasses];
+  u32x4 ring[RING][kPasses];  // stages on their way
 
   __device__ __forceinline__ Loader(const Operand& o, int64_t at, int tid) {
     ld = o.ld * P::kEs;
@@ -194,8 +194,9 @@ struct Loader {
     return *reinterpret_cast<const typename P::piece*>(p);
   }
 
-  // Stage [k, min(k + kBk, end)) to registers.
-  __device__ __forceinline__ void load(int64_t k, int64_t end) {
+  // Stage [k, min(k + kBk, end)) to a slot of the ring.
+  __device__ __forceinline__ void load(int64_t k, int64_t end, int slot) {
+    u32x4(&reg)[kPasses] = ring[slot];
     if constexpr (KIND == kImage) {
 #pragma unroll
       for (int p = 0; p < kPasses; ++p)  // (an image's reduction is whole stages)
@@ -230,7 +231,8 @@ struct Loader {
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
           u32x4 v = {0u, 0u, 0u, 0u};
-          if (p * kStep + row < left && (bits >> (p * kStep + row) & 1))
+          const bool there = (p * kStep + row < left) & (bits >> (p * kStep + row) & 1);
+          if (there)
             v = cols == kE ? whole(at + p * kStep * ld + off[0])
                            : load_part<P>(at + p * kStep * ld + off[0], cols);
           reg[p] = v;
@@ -240,7 +242,8 @@ struct Loader {
   }
 
   // Those registers to the operand's part of a buffer.
-  __device__ __forceinline__ void store(char* lds, int tid) const {
+  __device__ __forceinline__ void store(char* lds, int tid, int slot) const {
+    const u32x4(&reg)[kPasses] = ring[slot];
     if constexpr (P::kParts == 3) {
       const int piece = tid % kAcross;
 #pragma unroll
@@ -327,6 +330,12 @@ struct Tile {
   static constexpr int kStage = (BM + BN) * kRowBytes, kLds = 2 * kStage;
   // A quarter's operands are read while the one before is multiplied, where two sets fit the registers.
   static constexpr bool kAhead = AK == kRows && BK_ == kRows && P::kParts == 1;
+  static constexpr int kSets = P::kParts == 3 ? 3 : kAhead ? 2 : 1;
+  // Stages loaded ahead: as many as the registers hold. The large tile has the time of a whole
+  // stage (over 2000 cycles) for each load; smaller ones, and short reductions, wait for memory.
+  static constexpr int kRing = BM * BN > 128 * 128                       ? 1
+                               : BM * BN == 128 * 128 && P::kParts == 1 ? 2
+                                                                        : 3;
   typedef typename P::acc Acc;
 
   // The sum over k in [k0, k1). All threads of the workgroup; ends with a barrier.
@@ -342,58 +351,19 @@ struct Tile {
 #pragma unroll
         for (int r = 0; r < 16; ++r) c[i][j][r] = 0;
     if (k0 >= k1) return;
-    Loader<P, AK, BM, T> la(a, m0, tid);
-    Loader<P, BK_, BN, T> lb(b, n0, tid);
-    la.load(k0, k1);
-    lb.load(k0, k1);
-    la.store(lds, tid);
-    lb.store(lds + BM * kRowBytes, tid);
-    if (k0 + P::kBk < k1) {
-      la.load(k0 + P::kBk, k1);
-      lb.load(k0 + P::kBk, k1);
-    }
-    __syncthreads();
-    if constexpr (P::kParts == 3) {
-      int cur = 0;
-      for (int64_t k = k0; k < k1; k += P::kBk) {
-        const char* at = lds + cur * kStage;
-        char* other = lds + (cur ^ 1) * kStage;
-        u32x4 fa[3][MT], fb[3][NT];
-#pragma unroll
-        for (int q = 0; q < 3; ++q) {
-#pragma unroll
-          for (int i = 0; i < MT; ++i) fa[q][i] = fragment<P, AK, BM>(at, wm * MT + i, q, lane);
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            fb[q][j] = fragment<P, BK_, BN>(at + BM * kRowBytes, wn * NT + j, q, lane);
-        }
-        // parts' products, the smallest first
-        auto multiply = [&](int p, int q) {
-#pragma unroll
-          for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) P::mfma(c[i][j], fa[p][i], fb[q][j]);
-        };
-        multiply(2, 0);
-        multiply(1, 1);
-        multiply(0, 2);
-        if (k + P::kBk < k1) {
-          la.store(other, tid);
-          lb.store(other + BM * kRowBytes, tid);
-          if (k + 2 * P::kBk < k1) {
-            la.load(k + 2 * P::kBk, k1);
-            lb.load(k + 2 * P::kBk, k1);
-          }
-        }
-        multiply(1, 0);
-        multiply(0, 1);
-        multiply(0, 0);
-        __syncthreads();
-        cur ^= 1;
-      }
-      return;
-    }
-    u32x4 fa[2][MT], fb[2][NT];
+    Loader<P, AK, BM, T, kRing> la(a, m0, tid);
+    Loader<P, BK_, BN, T, kRing> lb(b, n0, tid);
+    // (stages are counted in 32 bits: a reduction is far shorter)
+    const int stages = (int)((k1 - k0 + P::kBk - 1) / P::kBk);
+    auto load = [&](int s, int slot) {
+      la.load(k0 + (int64_t)s * P::kBk, k1, slot);
+      lb.load(k0 + (int64_t)s * P::kBk, k1, slot);
+    };
+    auto store = [&](char* to, int slot) {
+      la.store(to, tid, slot);
+      lb.store(to + BM * kRowBytes, tid, slot);
+    };
+    u32x4 fa[kSets][MT], fb[kSets][NT];
     auto read = [&](int to, const char* at, int kk) {
 #pragma unroll
       for (int i = 0; i < MT; ++i) fa[to][i] = fragment<P, AK, BM>(at, wm * MT + i, kk, lane);
@@ -401,42 +371,68 @@ struct Tile {
       for (int j = 0; j < NT; ++j)
         fb[to][j] = fragment<P, BK_, BN>(at + BM * kRowBytes, wn * NT + j, kk, lane);
     };
-    auto multiply = [&](int of) {
+    auto multiply = [&](int of_a, int of_b) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) P::mfma(c[i][j], fa[of][i], fb[of][j]);
+        for (int j = 0; j < NT; ++j) P::mfma(c[i][j], fa[of_a][i], fb[of_b][j]);
     };
-    if constexpr (kAhead) read(0, lds, 0);
-    int cur = 0;
-    for (int64_t k = k0; k < k1; k += P::kBk) {
-      const char* at = lds + cur * kStage;
-      char* other = lds + (cur ^ 1) * kStage;
+    // Stage s goes to LDS from slot s % kRing while stage s - 1 is multiplied, and stage
+    // s + kRing is then loaded into that slot.
+    load(0, 0);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        if constexpr (kAhead) {
-          if (kk < 3) read((kk + 1) & 1, at, kk + 1);
-        } else {
-          read(0, at, kk);
+    for (int u = 1; u < kRing; ++u)
+      if (u < stages) load(u, u);
+    store(lds, 0);
+    if (kRing < stages) load(kRing, 0);
+    __syncthreads();
+    if constexpr (kAhead) read(0, lds, 0);
+    auto step = [&](int s, int u) {
+      const char* at = lds + (s & 1) * kStage;
+      char* other = lds + ((s & 1) ^ 1) * kStage;
+      const int slot = (u + 1) % kRing;
+      auto next = [&] {
+        if (s + 1 < stages) {
+          store(other, slot);
+          if (s + 1 + kRing < stages) load(s + 1 + kRing, slot);
         }
-        if (kk == 2 && k + P::kBk < k1) {
-          la.store(other, tid);
-          lb.store(other + BM * kRowBytes, tid);
-          if (k + 2 * P::kBk < k1) {
-            la.load(k + 2 * P::kBk, k1);
-            lb.load(k + 2 * P::kBk, k1);
+      };
+      if constexpr (P::kParts == 3) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) read(q, at, q);
+        multiply(2, 0);  // parts' products, the smallest first
+        multiply(1, 1);
+        multiply(0, 2);
+        next();
+        multiply(1, 0);
+        multiply(0, 1);
+        multiply(0, 0);
+        __syncthreads();
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          if constexpr (kAhead) {
+            if (kk < 3) read((kk + 1) & 1, at, kk + 1);
+          } else {
+            read(0, at, kk);
           }
-        }
-        if (kk == 3) {  // the next stage is there, and this one is read: its rest is in registers
-          __syncthreads();
+          if (kk == 2) next();
+          if (kk == 3) {  // the next stage is there, and the rest of this one is in registers
+            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kAhead)
+              if (s + 1 < stages) read(0, other, 0);
+          }
+          multiply(kAhead ? kk & 1 : 0, kAhead ? kk & 1 : 0);
           __builtin_amdgcn_sched_barrier(0);
-          if constexpr (kAhead)
-            if (k + P::kBk < k1) read(0, other, 0);
         }
-        multiply(kAhead ? kk & 1 : 0);
-        __builtin_amdgcn_sched_barrier(0);
       }
-      cur ^= 1;
+    };
+    // (no way out of a round: its last steps are passed over)
+    for (int s0 = 0; s0 < stages; s0 += kRing) {
+#pragma unroll
+      for (int u = 0; u < kRing; ++u)
+        if (s0 + u < stages) step(s0 + u, u);
     }
     __syncthreads();
   }
@@ -489,7 +485,7 @@ inline Plan plan(int64_t M, int64_t N, int64_t K) {
     slots = 512;
   }
   const int64_t tiles = p.mt * p.nt;
-  const int64_t most = cdiv(K, 256);  // at least two stages or so to a part
+  const int64_t most = cdiv(K, 128);
   if (2 * tiles <= slots && p.shape != k256) {
     p.splits = slots / tiles;
     if (p.splits > most) p.splits = most;
