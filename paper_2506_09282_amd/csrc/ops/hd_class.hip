@@ -272,12 +272,16 @@ __device__ __forceinline__ void join_lanes(float& m, float& s, float c) {
   }
 }
 
-// A row's loss from the parts of its scores. G lanes take four classes each (G = 256: again and
-// again, else G lanes cover the row), PG groups of them share the parts.
+// A row's loss from the parts of its scores. G lanes take four classes each (G = 256: kChunk classes
+// of the row, one of gridDim.y pieces that class_join_kernel joins; else G lanes cover the row), PG
+// groups of them share the parts.
+constexpr int64_t kChunk = 4096;
+
 template <int G, int PG>
 __global__ __launch_bounds__(kThreads) void class_rows_kernel(
     Parts sc, const int32_t* __restrict__ y, const uint8_t* __restrict__ mask, int64_t K,
-    float scale, float* __restrict__ loss, float* __restrict__ stats) {
+    float scale, float* __restrict__ loss, float* __restrict__ stats, float2* __restrict__ pieces,
+    float* __restrict__ targets) {
   constexpr int kRowsOf = kThreads / (G * PG);
   __shared__ f32x4 sums[PG > 1 ? kThreads : 1];
   __shared__ float2 part[kThreads / 64];
@@ -290,7 +294,8 @@ __global__ __launch_bounds__(kThreads) void class_rows_kernel(
   const bool asks = asked(yn, K);
   const float scale2 = scale * kLog2e;
   float m = -INFINITY, s = 0.0f;
-  for (int64_t k0 = 0; k0 < K; k0 += 4 * G) {
+  const int64_t k1 = G > 64 && (blockIdx.y + 1) * kChunk < K ? (blockIdx.y + 1) * kChunk : K;
+  for (int64_t k0 = G > 64 ? blockIdx.y * kChunk : 0; k0 < k1; k0 += 4 * G) {
     const int64_t k = k0 + 4 * lane;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (k < K) v = scores_of(sc, n, k, group, PG);
@@ -303,8 +308,13 @@ __global__ __launch_bounds__(kThreads) void class_rows_kernel(
       top = fmaxf(top, x[e]);
     }
     const int64_t place = (int64_t)yn - k;
-    if (asks & (group == 0) & (place >= 0) & (place < 4))
-      target[row] = place < 2 ? (place == 0 ? x[0] : x[1]) : (place == 2 ? x[2] : x[3]);
+    if (asks & (group == 0) & (place >= 0) & (place < 4)) {
+      const float t = place < 2 ? (place == 0 ? x[0] : x[1]) : (place == 2 ? x[2] : x[3]);
+      if (G > 64 && pieces)
+        targets[n] = t;
+      else
+        target[row] = t;
+    }
     const float base = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f;
 #pragma unroll
@@ -320,7 +330,9 @@ __global__ __launch_bounds__(kThreads) void class_rows_kernel(
     s = part[0].y;
     for (int w = 1; w < kThreads / 64; ++w) join(m, s, part[w].x, part[w].y, scale2);
   }
-  if (there && lane == 0 && group == 0)
+  if (G > 64 && pieces) {
+    if (threadIdx.x == 0) pieces[n * gridDim.y + blockIdx.y] = make_float2(m, s);
+  } else if (there && lane == 0 && group == 0)
     finish_row(m, s, asks ? target[row] : 0.0f, asks, scale, loss + n, stats + 2 * n);
 }
 
@@ -361,36 +373,57 @@ __global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
   const int64_t m0 = (int64_t)mi * TL::BM, n0 = (int64_t)ni * TL::BN;
   typename TL::Acc c[TL::MT][TL::NT];
   TL::product(a.C, a.H, m0, n0, 0, a.D, lds, c);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // (nothing of what follows is worked out before the product)
+  const int lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int wm = wave / TL::WN, wn = wave % TL::WN;
   const float scale2 = a.scale * kLog2e;
+  typedef typename TL::P::elem T;
+  // [32 samples][up to 256 bytes of the wave's classes], so that the stores run along the rows
+  constexpr int kTiles = TL::MT * 32 * sizeof(T) > 256 ? 256 / (32 * sizeof(T)) : TL::MT;
+  constexpr int kAcross = kTiles * 32, kPitch = kAcross + 16 / sizeof(T);
+  static_assert(TL::WM * TL::WN * 32 * kPitch * sizeof(T) <= TL::kLds, "");
+  T* mine = reinterpret_cast<T*>(lds) + wave * 32 * kPitch;
 #pragma unroll
   for (int j = 0; j < TL::NT; ++j) {
-    const int64_t n = n0 + (wn * TL::NT + j) * 32 + (lane & 31);
-    if (n >= a.N) continue;
-    const RowGrad row = row_grad(a, stats, g, K_all, n);
+    const int64_t nw = n0 + (wn * TL::NT + j) * 32, n = nw + (lane & 31);
+    const RowGrad row = row_grad(a, stats, g, K_all, n < a.N ? n : a.N - 1);
 #pragma unroll
-    for (int i = 0; i < TL::MT; ++i) {
-      const int64_t k0 = m0 + (wm * TL::MT + i) * 32;
-      const uint32_t bits = open_bits(a, k0);
+    for (int i0 = 0; i0 < TL::MT; i0 += kTiles) {
+      const int64_t first = m0 + (wm * TL::MT + i0) * 32;
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[4];
+      for (int i = 0; i < kTiles; ++i) {
+        uint32_t bits = open_bits(a, first + i * 32);
+        asm volatile("" : "+v"(bits));  // (worked out for each column again)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = q * 8 + half * 4 + e;
-          v[e] = score_grad(row, c[i][j][4 * q + e], k0 + at, bits >> at & 1, scale2);
+        for (int q = 0; q < 4; ++q) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int at = q * 8 + half * 4 + e;
+            v[e] = score_grad(row, c[i0 + i][j][4 * q + e], first + i * 32 + at, bits >> at & 1,
+                              scale2);
+          }
+          store_four(mine, (lane & 31) * kPitch + i * 32 + q * 8 + half * 4, v, 4);
+          __builtin_amdgcn_sched_barrier(0);  // (four at a time: the registers hold the sums)
         }
-        const int64_t k = k0 + q * 8 + half * 4;
-        if (k >= ld) continue;  // (ld is a multiple of 8, so four values fit or none)
-        if constexpr (TL::P::kEs == 4) {
-          *reinterpret_cast<f32x4*>(dS + n * ld + k) = f32x4{v[0], v[1], v[2], v[3]};
-        } else {
-          u32x2 w;
-          w[0] = to_bf16(v[0]) | (uint32_t)to_bf16(v[1]) << 16;
-          w[1] = to_bf16(v[2]) | (uint32_t)to_bf16(v[3]) << 16;
-          *reinterpret_cast<u32x2*>(dS + n * ld + k) = w;
-        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      // (ld is a multiple of 8: a piece of 16 bytes fits or begins past it)
+      constexpr int kE = 16 / sizeof(T), kPieces = kAcross / kE;
+      int q0 = threadIdx.x & 63;
+      asm volatile("" : "+v"(q0));
+#pragma unroll 1
+      for (int q = q0; q < 32 * kPieces; q += 64) {
+        const int r = q / kPieces, k = q % kPieces * kE;
+        if (nw + r < a.N && first + k < ld)
+          *reinterpret_cast<u32x4*>(dS + (nw + r) * ld + first + k) =
+              *reinterpret_cast<const u32x4*>(mine + r * kPitch + k);
       }
     }
   }
@@ -463,12 +496,15 @@ struct Out {
 };
 
 template <typename T>
-__device__ __forceinline__ void put(const Out& o, int64_t at, float v) {
-  if (o.before) v += o.before[at];
+__device__ __forceinline__ void put(const Out& o, int64_t at, f32x4 v, int64_t n) {
+  if (o.before) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += o.before[e < n ? at + e : at];
+  }
   if (o.sums)
-    o.sums[at] = v;
+    store_four(o.sums, at, v, n);
   else
-    store_elem(reinterpret_cast<T*>(o.out), at, v);
+    store_four(reinterpret_cast<T*>(o.out), at, v, n);
 }
 
 template <class TL>
@@ -483,34 +519,37 @@ __global__ __launch_bounds__(TL::T, 2) void class_product_kernel(
   const int64_t k0 = part * each, k1 = k0 + each < K ? k0 + each : K;
   typename TL::Acc c[TL::MT][TL::NT];
   TL::product(a, b, m0, n0, k0, k1, lds, c);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const int wm = wave / TL::WN, wn = wave % TL::WN;
-#pragma unroll
-  for (int i = 0; i < TL::MT; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t m = m0 + (wm * TL::MT + i) * 32 + (r / 4) * 8 + half * 4 + r % 4;
-      if (m >= o.M) continue;
-#pragma unroll
-      for (int j = 0; j < TL::NT; ++j) {
-        const int64_t n = n0 + (wn * TL::NT + j) * 32 + (lane & 31);
-        if (n >= o.N) continue;
-        if (o.parts)
-          o.parts[((int64_t)part * o.M + m) * o.N + n] = c[i][j][r];
-        else
-          put<typename TL::P::elem>(o, m * o.N + n, c[i][j][r]);
-      }
-    }
+  float* to = o.parts ? o.parts + (int64_t)part * o.M * o.N : nullptr;
+  TL::rows_out(c, lds, m0, n0, [&](int64_t m, int64_t n, const f32x4& v) {
+    if (m >= o.M || n >= o.N) return;
+    if (to)
+      store_four(to, m * o.N + n, v, o.N - n);
+    else
+      put<typename TL::P::elem>(o, m * o.N + n, v, o.N - n);
+  });
 }
 
-template <typename T>
+// The parts' sum, four values to a thread, the parts shared by PG groups of threads.
+template <typename T, int PG>
 __global__ __launch_bounds__(kThreads) void class_sum_kernel(Out o, int count) {
-  const int64_t each = o.M * o.N;
-  const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (at >= each) return;
-  float v = 0.0f;
-  for (int i = 0; i < count; ++i) v += o.parts[i * each + at];
-  put<T>(o, at, v);
+  constexpr int kLanes = kThreads / PG;
+  __shared__ f32x4 sums[PG > 1 ? kThreads : 1];
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const int64_t each = o.M * o.N, at = ((int64_t)blockIdx.x * kLanes + lane) * 4;
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (at + 4 <= each) {
+    const float* p = o.parts + group * each + at;
+#pragma unroll 8
+    for (int i = group; i < count; i += PG, p += PG * each)
+      v += *reinterpret_cast<const f32x4_a4*>(p);
+  } else if (at < each) {
+    for (int i = group; i < count; i += PG) {
+      const float* p = o.parts + i * each + at;
+      v += f32x4{p[0], at + 1 < each ? p[1] : 0.0f, at + 2 < each ? p[2] : 0.0f, 0.0f};
+    }
+  }
+  v = join_groups<PG>(v, group, lane, kLanes, sums);
+  if (group == 0 && at < each) put<T>(o, at, v, each - at);
 }
 
 // ---- host -------------------------------------------------------------------------------
@@ -540,13 +579,13 @@ hipError_t with_tile(tile::Shape s, F f) {
   switch (s) {
     case tile::k256: return f(Tile<Q, AK, BK, 256, 256, 2, 4>());
     case tile::k128: return f(Tile<Q, AK, BK, 128, 128, 2, 2>());
-    case tile::k32x128: return f(Tile<P, AK, BK, 32, 128, 1, 4>());
-    default: return f(Tile<P, AK, BK, 128, 32, 4, 1>());
+    case tile::k32x256: return f(Tile<P, AK, BK, 32, 256, 1, 4>());
+    default: return f(Tile<P, AK, BK, 256, 32, 4, 1>());
   }
 }
 
 int64_t tile_m(const Plan& p) {
-  return p.shape == tile::k256 ? 256 : p.shape == tile::k32x128 ? 32 : 128;
+  return p.shape == tile::k32x256 ? 32 : p.shape == tile::k128 ? 128 : 256;
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -561,7 +600,7 @@ int64_t piece_of(int64_t N, int64_t K, int64_t es) {
 
 struct LossPlace {
   Plan s;
-  size_t open, parts, target, total;
+  size_t open, parts, pieces, target, total;
 };
 LossPlace loss_place(int64_t N, int64_t D, int64_t K) {
   LossPlace w;
@@ -569,9 +608,11 @@ LossPlace loss_place(int64_t N, int64_t D, int64_t K) {
   w.open = 0;
   w.parts = up((size_t)cdiv(K, 64) * 8);
   if (w.s.splits > 1) {
-    w.target = w.total = w.parts + up((size_t)w.s.splits * N * w.s.mt * tile_m(w.s) * 4);
+    w.pieces = w.parts + up((size_t)w.s.splits * N * w.s.mt * tile_m(w.s) * 4);
+    w.target = w.pieces + up((size_t)N * cdiv(K, kChunk) * 8);
+    w.total = w.target + up((size_t)N * 4);
   } else {
-    w.target = w.parts + up((size_t)N * w.s.mt * 8);
+    w.pieces = w.target = w.parts + up((size_t)N * w.s.mt * 8);
     w.total = w.target + up((size_t)N * 4);
   }
   return w;
@@ -648,9 +689,12 @@ hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hip
   }
   if ((e = run_scores<P>(a, w.s, parts, stream)) != hipSuccess) return e;
   const Parts sc{parts, w.s.mt * tile_m(w.s), c.N, (int)w.s.splits};
+  const int chunks = c.K > 256 ? (int)cdiv(c.K, kChunk) : 1;
+  float2* pieces = chunks > 1 ? reinterpret_cast<float2*>(ws + w.pieces) : nullptr;
+  float* targets = reinterpret_cast<float*>(ws + w.target);
   auto rows = [&](auto* kernel, int each) {
-    kernel<<<dim3((uint32_t)cdiv(c.N, each)), dim3(kThreads), 0, stream>>>(
-        sc, c.y, c.mask, c.K, c.scale, loss, stats);
+    kernel<<<dim3((uint32_t)cdiv(c.N, each), (uint32_t)chunks), dim3(kThreads), 0, stream>>>(
+        sc, c.y, c.mask, c.K, c.scale, loss, stats, pieces, targets);
     return hipGetLastError();
   };
   // Many parts are those of few rows: a workgroup to a row shares them.
@@ -659,7 +703,11 @@ hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hip
     return many ? rows(class_rows_kernel<8, 32>, 1) : rows(class_rows_kernel<8, 1>, 32);
   if (c.K <= 256)
     return many ? rows(class_rows_kernel<64, 4>, 1) : rows(class_rows_kernel<64, 1>, 4);
-  return rows(class_rows_kernel<256, 1>, 1);
+  e = rows(class_rows_kernel<256, 1>, 1);
+  if (e != hipSuccess || chunks == 1) return e;
+  class_join_kernel<<<dim3((uint32_t)cdiv(c.N, kThreads / 64)), dim3(kThreads), 0, stream>>>(
+      pieces, targets, c.y, c.N, c.K, chunks, c.scale, loss, stats);
+  return hipGetLastError();
 }
 
 template <class P, int AK, int BK>
@@ -673,9 +721,13 @@ hipError_t run_product(const Operand& a, const Operand& b, int64_t K, Out o, flo
                                                       p.each, (uint32_t)p.mt, (uint32_t)p.nt, o);
   });
   if (e != hipSuccess || p.splits == 1) return e;
-  class_sum_kernel<typename P::elem>
-      <<<dim3((uint32_t)cdiv(o.M * o.N, kThreads)), dim3(kThreads), 0, stream>>>(o, (int)p.splits);
-  return hipGetLastError();
+  auto sum = [&](auto* kernel, int groups) {
+    kernel<<<dim3((uint32_t)cdiv(o.M * o.N, 4 * kThreads / groups)), dim3(kThreads), 0, stream>>>(
+        o, (int)p.splits);
+    return hipGetLastError();
+  };
+  typedef typename P::elem T;
+  return p.splits > 8 ? sum(class_sum_kernel<T, 8>, 8) : sum(class_sum_kernel<T, 1>, 1);
 }
 
 template <class P>

@@ -24,6 +24,28 @@ __device__ __forceinline__ bf16raw to_bf16(float v) {
 __device__ __forceinline__ void store_elem(float* p, int64_t i, float v) { p[i] = v; }
 __device__ __forceinline__ void store_elem(bf16raw* p, int64_t i, float v) { p[i] = to_bf16(v); }
 
+// Up to four values of a row from place i on (n of them), wherever rows start.
+__device__ __forceinline__ void store_four(float* p, int64_t i, const f32x4& v, int64_t n) {
+  if (n >= 4) {
+    *reinterpret_cast<f32x4_a4*>(p + i) = v;
+  } else {
+    if (n > 0) p[i] = v[0];
+    if (n > 1) p[i + 1] = v[1];
+    if (n > 2) p[i + 2] = v[2];
+  }
+}
+__device__ __forceinline__ void store_four(bf16raw* p, int64_t i, const f32x4& v, int64_t n) {
+  typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+  if (n >= 4) {
+    *reinterpret_cast<u32x2_a2*>(p + i) = u32x2{to_bf16(v[0]) | (uint32_t)to_bf16(v[1]) << 16,
+                                                to_bf16(v[2]) | (uint32_t)to_bf16(v[3]) << 16};
+  } else {
+    if (n > 0) p[i] = to_bf16(v[0]);
+    if (n > 1) p[i + 1] = to_bf16(v[1]);
+    if (n > 2) p[i + 2] = to_bf16(v[2]);
+  }
+}
+
 // The value of lane ^ OFF, in the vector ALU alone (a shuffle through LDS takes several
 // times as long, and the sorts and sums across lanes are chains of these).
 template <int OFF>

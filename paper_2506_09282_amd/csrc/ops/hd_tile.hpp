@@ -16,6 +16,8 @@
 // instruction takes one k from a lane, with plain ones.
 #pragma once
 
+#include <type_traits>
+
 #include "hd_ops.hpp"
 
 namespace hd {
@@ -103,14 +105,31 @@ struct I8 {
   }
 };
 
-// The first `valid` elements at p, zeros behind them.
-template <class P>
-__device__ __forceinline__ u32x4 load_part(const char* p, int valid) {
-  u32x4 v = {0u, 0u, 0u, 0u};
+// The first `valid` elements at p, zeros behind them. With `back`, the elements before p are there
+// too, and one load takes those that end with the last valid one (BACK: not in the large tile, whose
+// registers are full).
+template <class P, bool BACK>
+__device__ __forceinline__ u32x4 load_part(const char* p, int valid, bool back) {
   constexpr int kE = 16 / P::kEs;
-#pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    if (e >= valid) break;
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (valid <= 0) return v;
+  if (BACK && back) {
+    const int bytes = (kE - valid) * P::kEs;  // under 16
+    v = *reinterpret_cast<const typename P::piece*>(p - bytes);
+    uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+    const int s = 8 * (bytes & 7);
+    if (bytes & 8) {
+      lo = hi;
+      hi = 0;
+    }
+    lo = lo >> s | (s ? hi << (64 - s) : 0);
+    hi >>= s;
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  }
+  // (a loop, not 16 bytes' worth of straight code: it is rare, and short kernels wait for their code)
+  uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+  for (int e = valid - 1; e >= 0; --e) {
     uint32_t x;
     if constexpr (P::kEs == 4)
       x = reinterpret_cast<const uint32_t*>(p)[e];
@@ -118,9 +137,10 @@ __device__ __forceinline__ u32x4 load_part(const char* p, int valid) {
       x = reinterpret_cast<const uint16_t*>(p)[e];
     else
       x = reinterpret_cast<const uint8_t*>(p)[e];
-    v[e * P::kEs / 4] |= x << (8 * (e * P::kEs % 4));
+    hi = hi << (8 * P::kEs) | lo >> (64 - 8 * P::kEs);
+    lo = lo << (8 * P::kEs) | x;
   }
-  return v;
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
 // How pieces of a kCols row k are moved, so that rows read together use different banks.
@@ -132,8 +152,10 @@ __device__ __forceinline__ int col_swizzle(int k) {
     return R >= 128 ? (k & 3) * 4 : R == 64 ? ((k >> 1) & 1) * 4 : 0;
 }
 
-// One operand's way from memory to LDS: R rows (or columns) by T threads.
-template <class P, int KIND, int R, int T, int RING>
+// One operand's way from memory to LDS: R rows (or columns) by T threads. ONCE: each value passes
+// one workgroup only, so that whole lines go past the caches (16384 x 10240 fp32 under 26 classes:
+// 121 us instead of 130; rows of 2000 bytes, whose lines two stages share, 73 instead of 59).
+template <class P, int KIND, int R, int T, int RING, bool ONCE>
 struct Loader {
   static constexpr int kE = 16 / P::kEs;
   static constexpr int kAcross = KIND == kCols ? R / kE : P::kBk / kE;  // pieces of a row
@@ -146,11 +168,14 @@ struct Loader {
   const uint64_t* live;
   uint32_t off[KIND == kCols ? 1 : kPasses];
   int lds_at, row, cols;
+  bool back;   // kCols: the elements before a piece are the row's
+  bool lines;  // rows are whole cache lines
   u32x4 ring[RING][kPasses];  // stages on their way
 
   __device__ __forceinline__ Loader(const Operand& o, int64_t at, int tid) {
     ld = o.ld * P::kEs;
     live = o.live;
+    lines = ((uint64_t)o.p | (uint64_t)ld) % 128 == 0;
     row = tid / kAcross;
     const int piece = tid % kAcross;
     if constexpr (KIND == kImage) {
@@ -186,12 +211,16 @@ struct Loader {
       const int mine = piece < last ? piece : (int)last;
       const int64_t left = o.extent - at - mine * kE;
       cols = left > kE ? kE : (int)left;
+      back = at + mine * kE >= kE;
       off[0] = (uint32_t)row * (uint32_t)ld + mine * 16;  // of pass 0
       lds_at = 0;
     }
   }
   __device__ __forceinline__ u32x4 whole(const char* p) const {
-    return *reinterpret_cast<const typename P::piece*>(p);
+    const typename P::piece* at = reinterpret_cast<const typename P::piece*>(p);
+    if constexpr (ONCE)
+      if (lines) return __builtin_nontemporal_load(at);
+    return *at;
   }
 
   // Stage [k, min(k + kBk, end)) to a slot of the ring.
@@ -210,7 +239,8 @@ struct Loader {
         const int64_t left = end - k - cols;
 #pragma unroll
         for (int p = 0; p < kPasses; ++p)
-          reg[p] = left >= kE ? whole(at + off[p]) : load_part<P>(at + off[p], (int)left);
+          reg[p] = left >= kE ? whole(at + off[p])
+                             : load_part<P, (RING > 1)>(at + off[p], (int)left, k + cols >= kE);
       }
     } else {
       const char* at = base + k * ld;
@@ -227,14 +257,14 @@ struct Loader {
             if (!(mine >> (p * kStep) & 1)) reg[p] = u32x4{0u, 0u, 0u, 0u};
         }
       } else {
-        const int64_t left = end - k;
+        const int left = end - k < 64 ? (int)(end - k) : 64;
+        const uint64_t mine = (left < 64 ? bits & ((uint64_t(1) << left) - 1) : bits) >> row;
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
           u32x4 v = {0u, 0u, 0u, 0u};
-          const bool there = (p * kStep + row < left) & (bits >> (p * kStep + row) & 1);
-          if (there)
+          if (mine >> (p * kStep) & 1)
             v = cols == kE ? whole(at + p * kStep * ld + off[0])
-                           : load_part<P>(at + p * kStep * ld + off[0], cols);
+                           : load_part<P, (RING > 1)>(at + p * kStep * ld + off[0], cols, back);
           reg[p] = v;
         }
       }
@@ -328,14 +358,12 @@ struct Tile {
   static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
   static constexpr int kRowBytes = P::kParts == 3 ? 96 : 128;  // of a stage
   static constexpr int kStage = (BM + BN) * kRowBytes, kLds = 2 * kStage;
-  // A quarter's operands are read while the one before is multiplied, where two sets fit the registers.
-  static constexpr bool kAhead = AK == kRows && BK_ == kRows && P::kParts == 1;
-  static constexpr int kSets = P::kParts == 3 ? 3 : kAhead ? 2 : 1;
+  // Operands in registers: the parts, or a quarter of a stage (reading one quarter while another
+  // is multiplied took as many registers again and gained nothing: two waves share a SIMD).
+  static constexpr int kSets = P::kParts;
   // Stages loaded ahead: as many as the registers hold. The large tile has the time of a whole
   // stage (over 2000 cycles) for each load; smaller ones, and short reductions, wait for memory.
-  static constexpr int kRing = BM * BN > 128 * 128                       ? 1
-                               : BM * BN == 128 * 128 && P::kParts == 1 ? 2
-                                                                        : 3;
+  static constexpr int kRing = BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128 && P::kParts == 3 ? 3 : 2;
   typedef typename P::acc Acc;
 
   // The sum over k in [k0, k1). All threads of the workgroup; ends with a barrier.
@@ -351,8 +379,8 @@ struct Tile {
 #pragma unroll
         for (int r = 0; r < 16; ++r) c[i][j][r] = 0;
     if (k0 >= k1) return;
-    Loader<P, AK, BM, T, kRing> la(a, m0, tid);
-    Loader<P, BK_, BN, T, kRing> lb(b, n0, tid);
+    Loader<P, AK, BM, T, kRing, (BN == 32)> la(a, m0, tid);
+    Loader<P, BK_, BN, T, kRing, (BM == 32)> lb(b, n0, tid);
     // (stages are counted in 32 bits: a reduction is far shorter)
     const int stages = (int)((k1 - k0 + P::kBk - 1) / P::kBk);
     auto load = [&](int s, int slot) {
@@ -386,7 +414,6 @@ struct Tile {
     store(lds, 0);
     if (kRing < stages) load(kRing, 0);
     __syncthreads();
-    if constexpr (kAhead) read(0, lds, 0);
     auto step = [&](int s, int u) {
       const char* at = lds + (s & 1) * kStage;
       char* other = lds + ((s & 1) ^ 1) * kStage;
@@ -411,19 +438,11 @@ struct Tile {
       } else {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-          if constexpr (kAhead) {
-            if (kk < 3) read((kk + 1) & 1, at, kk + 1);
-          } else {
-            read(0, at, kk);
-          }
+          read(0, at, kk);
           if (kk == 2) next();
-          if (kk == 3) {  // the next stage is there, and the rest of this one is in registers
-            __syncthreads();
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (kAhead)
-              if (s + 1 < stages) read(0, other, 0);
-          }
-          multiply(kAhead ? kk & 1 : 0, kAhead ? kk & 1 : 0);
+          // (the next stage is there, and the rest of this one is in registers)
+          if (kk == 3) __syncthreads();
+          multiply(0, 0);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -435,6 +454,40 @@ struct Tile {
         if (s0 + u < stages) step(s0 + u, u);
     }
     __syncthreads();
+  }
+
+  // f(m, n, four values of row m from column n on) for all of the tile, a wave's lanes side by side
+  // along the rows. The sums change lanes through the wave's own part of LDS.
+  template <class F>
+  static __device__ __forceinline__ void rows_out(const Acc (&c)[MT][NT], char* lds, int64_t m0,
+                                                  int64_t n0, F f) {
+    typedef std::remove_reference_t<decltype(c[0][0][0] + 0)> E;
+    typedef E Four __attribute__((ext_vector_type(4)));
+    constexpr int kPitch = NT * 32 + 8;  // (rows four apart lie half the banks apart)
+    static_assert(WM * WN * 32 * kPitch * 4 <= kLds, "");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    E* mine = reinterpret_cast<E*>(lds) + wave * 32 * kPitch;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      // (a wave's LDS accesses are done in order)
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          mine[((r / 4) * 8 + half * 4 + r % 4) * kPitch + j * 32 + (lane & 31)] = c[i][j][r];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const int64_t m = m0 + (wave / WN * MT + i) * 32, n = n0 + wave % WN * NT * 32;
+#pragma unroll 2
+      for (int q = lane; q < 32 * NT * 8; q += 64) {
+        const int row = q / (NT * 8), col = q % (NT * 8) * 4;
+        f(m + row, n + col, *reinterpret_cast<const Four*>(mine + row * kPitch + col));
+      }
+    }
   }
 };
 
@@ -457,7 +510,7 @@ __device__ __forceinline__ void tile_at(uint32_t id, uint32_t mt, uint32_t nt, u
 }
 
 // ---- host: which tile, and how many parts of the reduction -----------------------
-enum Shape { k256, k128, k32x128, k128x32 };
+enum Shape { k256, k128, k32x256, k256x32 };
 
 struct Plan {
   Shape shape;
@@ -472,11 +525,11 @@ inline Plan plan(int64_t M, int64_t N, int64_t K) {
   Plan p;
   int64_t slots;  // workgroups that the chip holds at once
   if (M <= 32) {
-    p = {k32x128, 1, cdiv(N, 128), 1, 0};
-    slots = 768;
+    p = {k32x256, 1, cdiv(N, 256), 1, 0};
+    slots = 512;
   } else if (N <= 32) {
-    p = {k128x32, cdiv(M, 128), 1, 1, 0};
-    slots = 768;
+    p = {k256x32, cdiv(M, 256), 1, 1, 0};
+    slots = 512;
   } else if (cdiv(M, 256) * cdiv(N, 256) >= 192) {
     p = {k256, cdiv(M, 256), cdiv(N, 256), 1, 0};
     slots = 256;

@@ -102,10 +102,11 @@ def test_byte_refusals(L):
 
 
 def test_byte_product_refusals(L):
-    need = L.hd_byte_workspace_bytes(4, 40, 130, F32)
+    need = L.hd_byte_workspace_bytes(70, 40, 130, F32)
     assert need > 0 and L.hd_byte_workspace_bytes(0, 40, 130, F32) == 0
+    assert L.hd_byte_workspace_bytes(1, 40, 130, F32) == 0  # each workgroup codes a short X itself
 
-    def f(X=FAKE, ldx=130, rs=None, im=FAKE, Y=FAKE, ldy=40, N=4, o=40, i=130, xdt=F32, ydt=F32,
+    def f(X=FAKE, ldx=130, rs=None, im=FAKE, Y=FAKE, ldy=40, N=70, o=40, i=130, xdt=F32, ydt=F32,
           act=1, ws=FAKE, b=need):
         return L.hd_byte_product(X, ldx, rs, im, Y, ldy, N, o, i, xdt, ydt, act, ws, b, None)
 
