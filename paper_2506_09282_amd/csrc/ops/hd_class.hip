@@ -573,14 +573,17 @@ hipError_t launch_tiles(int64_t blocks, hipStream_t stream, A... args) {
 
 // f is called with the tile of a plan.
 template <class P, int AK, int BK, class F>
-hipError_t with_tile(tile::Shape s, F f) {
+hipError_t with_tile(const Plan& p, const Operand& a, const Operand& b, F f) {
   // fp32 on the bf16 instruction where the matrix instructions bound the tile
   typedef std::conditional_t<std::is_same_v<P, F32>, tile::X3, P> Q;
-  switch (s) {
+  const bool once = tile::once(p, a, b, P::kEs);
+  switch (p.shape) {
     case tile::k256: return f(Tile<Q, AK, BK, 256, 256, 2, 4>());
     case tile::k128: return f(Tile<Q, AK, BK, 128, 128, 2, 2>());
-    case tile::k32x256: return f(Tile<P, AK, BK, 32, 256, 1, 4>());
-    default: return f(Tile<P, AK, BK, 256, 32, 4, 1>());
+    case tile::k32x256:
+      return once ? f(Tile<P, AK, BK, 32, 256, 1, 4, true>()) : f(Tile<P, AK, BK, 32, 256, 1, 4>());
+    default:
+      return once ? f(Tile<P, AK, BK, 256, 32, 4, 1, true>()) : f(Tile<P, AK, BK, 256, 32, 4, 1>());
   }
 }
 
@@ -649,7 +652,7 @@ GradPlace grad_place(int64_t N, int64_t D, int64_t K, int64_t es) {
 
 template <class P>
 hipError_t run_scores(const Scores& a, const Plan& p, float* parts, hipStream_t stream) {
-  return with_tile<P, kRows, kRows>(p.shape, [&](auto t) {
+  return with_tile<P, kRows, kRows>(p, a.C, a.H, [&](auto t) {
     typedef decltype(t) TL;
     if constexpr (TL::BM * TL::BN > 128 * 128)
       return hipErrorInvalidValue;  // (the large tile is not split)
@@ -676,7 +679,7 @@ hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hip
   float* parts = reinterpret_cast<float*>(ws + w.parts);
   if (w.s.splits == 1) {
     float* target = reinterpret_cast<float*>(ws + w.target);
-    e = with_tile<P, kRows, kRows>(w.s.shape, [&](auto t) {
+    e = with_tile<P, kRows, kRows>(w.s, a.C, a.H, [&](auto t) {
       typedef decltype(t) TL;
       return launch_tiles<class_loss_kernel<TL>, TL>(tiles, stream, a,
                                                      reinterpret_cast<float2*>(parts), target);
@@ -715,7 +718,7 @@ hipError_t run_product(const Operand& a, const Operand& b, int64_t K, Out o, flo
                        hipStream_t stream) {
   const Plan p = tile::plan(o.M, o.N, K);
   if (p.splits > 1) o.parts = parts;
-  const hipError_t e = with_tile<P, AK, BK>(p.shape, [&](auto t) {
+  const hipError_t e = with_tile<P, AK, BK>(p, a, b, [&](auto t) {
     typedef decltype(t) TL;
     return launch_tiles<class_product_kernel<TL>, TL>(p.mt * p.nt * p.splits, stream, a, b, K,
                                                       p.each, (uint32_t)p.mt, (uint32_t)p.nt, o);
@@ -763,7 +766,7 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
     const Scores a{{c.H, c.ldh, c.N, nullptr}, {C, c.ldc, K, nullptr}, c.y, part_open, c.scale,
                    c.N, c.D, K, first, (uint32_t)s.mt, (uint32_t)s.nt};
     if (s.splits == 1) {
-      e = with_tile<P, kRows, kRows>(s.shape, [&](auto t) {
+      e = with_tile<P, kRows, kRows>(s, a.C, a.H, [&](auto t) {
         typedef decltype(t) TL;
         return launch_tiles<class_dscores_kernel<TL>, TL>(tiles, stream, a, c.K, stats, g, dS,
                                                           w.ld);

@@ -152,9 +152,7 @@ __device__ __forceinline__ int col_swizzle(int k) {
     return R >= 128 ? (k & 3) * 4 : R == 64 ? ((k >> 1) & 1) * 4 : 0;
 }
 
-// One operand's way from memory to LDS: R rows (or columns) by T threads. ONCE: each value passes
-// one workgroup only, so that whole lines go past the caches (16384 x 10240 fp32 under 26 classes:
-// 121 us instead of 130; rows of 2000 bytes, whose lines two stages share, 73 instead of 59).
+// One operand's way from memory to LDS: R rows (or columns) by T threads. ONCE: past the caches.
 template <class P, int KIND, int R, int T, int RING, bool ONCE>
 struct Loader {
   static constexpr int kE = 16 / P::kEs;
@@ -168,14 +166,12 @@ struct Loader {
   const uint64_t* live;
   uint32_t off[KIND == kCols ? 1 : kPasses];
   int lds_at, row, cols;
-  bool back;   // kCols: the elements before a piece are the row's
-  bool lines;  // rows are whole cache lines
+  bool back;  // kCols: the elements before a piece are the row's
   u32x4 ring[RING][kPasses];  // stages on their way
 
   __device__ __forceinline__ Loader(const Operand& o, int64_t at, int tid) {
     ld = o.ld * P::kEs;
     live = o.live;
-    lines = ((uint64_t)o.p | (uint64_t)ld) % 128 == 0;
     row = tid / kAcross;
     const int piece = tid % kAcross;
     if constexpr (KIND == kImage) {
@@ -217,10 +213,16 @@ struct Loader {
     }
   }
   __device__ __forceinline__ u32x4 whole(const char* p) const {
-    const typename P::piece* at = reinterpret_cast<const typename P::piece*>(p);
-    if constexpr (ONCE)
-      if (lines) return __builtin_nontemporal_load(at);
-    return *at;
+    return *reinterpret_cast<const typename P::piece*>(p);
+  }
+  // reg[p] = piece(p) for every pass, past the caches where that pays.
+  template <class F>
+  __device__ __forceinline__ void pieces(u32x4 (&reg)[kPasses], F piece) const {
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p)
+      reg[p] = ONCE ? __builtin_nontemporal_load(
+                          reinterpret_cast<const typename P::piece*>(piece(p)))
+                    : whole(piece(p));
   }
 
   // Stage [k, min(k + kBk, end)) to a slot of the ring.
@@ -233,8 +235,7 @@ struct Loader {
     } else if constexpr (KIND == kRows) {
       const char* at = base + k * P::kEs;
       if (k + P::kBk <= end) {
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) reg[p] = whole(at + off[p]);
+        pieces(reg, [&](int p) { return at + off[p]; });
       } else {
         const int64_t left = end - k - cols;
 #pragma unroll
@@ -249,8 +250,7 @@ struct Loader {
         // (a piece across the row's end runs into the next rows, of which there are enough: what
         // it takes from there are columns that nobody looks at)
         const uint64_t mine = bits >> row;
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) reg[p] = whole(at + p * kStep * ld + off[0]);
+        pieces(reg, [&](int p) { return at + p * kStep * ld + off[0]; });
         if (live) {
 #pragma unroll
           for (int p = 0; p < kPasses; ++p)
@@ -351,7 +351,8 @@ __device__ __forceinline__ u32x4 fragment(const char* lds, int sub, int kk, int 
 
 // BM x BN by WM x WN waves. Of a wave's accumulators c[i][j], register r of lane l is
 //   m = 32 (wave row * MT + i) + 8 (r / 4) + 4 (l / 32) + r % 4,  n = 32 (...) + l % 32.
-template <class P_, int AK, int BK_, int BM_, int BN_, int WM_, int WN_>
+// ONCE: the wide operand of a narrow tile goes past the caches.
+template <class P_, int AK, int BK_, int BM_, int BN_, int WM_, int WN_, bool ONCE = false>
 struct Tile {
   typedef P_ P;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, T = 64 * WM * WN;
@@ -379,8 +380,8 @@ struct Tile {
 #pragma unroll
         for (int r = 0; r < 16; ++r) c[i][j][r] = 0;
     if (k0 >= k1) return;
-    Loader<P, AK, BM, T, kRing, (BN == 32)> la(a, m0, tid);
-    Loader<P, BK_, BN, T, kRing, (BM == 32)> lb(b, n0, tid);
+    Loader<P, AK, BM, T, kRing, (ONCE && BN == 32)> la(a, m0, tid);
+    Loader<P, BK_, BN, T, kRing, (ONCE && BM == 32)> lb(b, n0, tid);
     // (stages are counted in 32 bits: a reduction is far shorter)
     const int stages = (int)((k1 - k0 + P::kBk - 1) / P::kBk);
     auto load = [&](int s, int slot) {
@@ -518,6 +519,16 @@ struct Plan {
   int64_t splits;   // parts of the reduction
   int64_t each;     // values of k of a part (a multiple of 128)
 };
+
+// Whether the wide operand of a narrow tile goes past the caches: each of its values passes one
+// workgroup, but where lines hold parts of two rows or stages, those take it from the cache
+// (16384 x 10240 fp32 under 26 classes: 114 us instead of 130; 100003 rows of 2000 bytes: 66
+// instead of 55).
+inline bool once(const Plan& p, const Operand& a, const Operand& b, int es) {
+  if (p.shape != k32x256 && p.shape != k256x32) return false;
+  const Operand& wide = p.shape == k32x256 ? b : a;
+  return ((uintptr_t)wide.p | (uintptr_t)(wide.ld * es)) % 128 == 0;
+}
 
 // For [M][N] sums over K: the large tile where there is one for every compute unit, narrow
 // ones where a side is short, and parts of the reduction where that leaves the chip idle.
