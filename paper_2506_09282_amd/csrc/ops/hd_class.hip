@@ -507,18 +507,23 @@ __device__ __forceinline__ void put(const Out& o, int64_t at, f32x4 v, int64_t n
     store_four(reinterpret_cast<T*>(o.out), at, v, n);
 }
 
+struct Product {  // out = a b over K, tile by tile and part by part
+  Operand a, b;
+  int64_t K, each;
+  uint32_t mt, nt;
+  Out o;
+};
+
 template <class TL>
-__global__ __launch_bounds__(TL::T, 2) void class_product_kernel(
-    Operand a, Operand b, int64_t K, int64_t each, uint32_t mt, uint32_t nt, Out o) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const uint32_t tiles = mt * nt;
-  const uint32_t id = die_order(blockIdx.x, gridDim.x), part = id / tiles;
+__device__ __forceinline__ void product_tile(const Product& p, uint32_t id, char* lds) {
+  const uint32_t tiles = p.mt * p.nt, part = id / tiles;
   uint32_t mi, ni;
-  tile_at(id % tiles, mt, nt, mi, ni);
+  tile_at(id % tiles, p.mt, p.nt, mi, ni);
   const int64_t m0 = (int64_t)mi * TL::BM, n0 = (int64_t)ni * TL::BN;
-  const int64_t k0 = part * each, k1 = k0 + each < K ? k0 + each : K;
+  const int64_t k0 = part * p.each, k1 = k0 + p.each < p.K ? k0 + p.each : p.K;
   typename TL::Acc c[TL::MT][TL::NT];
-  TL::product(a, b, m0, n0, k0, k1, lds, c);
+  TL::product(p.a, p.b, m0, n0, k0, k1, lds, c);
+  const Out& o = p.o;
   float* to = o.parts ? o.parts + (int64_t)part * o.M * o.N : nullptr;
   TL::rows_out(c, lds, m0, n0, [&](int64_t m, int64_t n, const f32x4& v) {
     if (m >= o.M || n >= o.N) return;
@@ -529,13 +534,38 @@ __global__ __launch_bounds__(TL::T, 2) void class_product_kernel(
   });
 }
 
+template <class TL>
+__global__ __launch_bounds__(TL::T, 2) void class_product_kernel(Product p) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  product_tile<TL>(p, die_order(blockIdx.x, gridDim.x), lds);
+}
+
+// Two products in one launch: the first `blocks` workgroups take p's tiles, the others q's.
+template <class TL, class TQ>
+__global__ __launch_bounds__(TL::T, 2) void class_products_kernel(Product p, uint32_t blocks,
+                                                                  Product q) {
+  static_assert(TL::T == TQ::T, "");
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  if (blockIdx.x < blocks)
+    product_tile<TL>(p, blockIdx.x, lds);
+  else
+    product_tile<TQ>(q, blockIdx.x - blocks, lds);
+}
+
 // The parts' sum, four values to a thread, the parts shared by PG groups of threads.
 template <typename T, int PG>
-__global__ __launch_bounds__(kThreads) void class_sum_kernel(Out o, int count) {
+__global__ __launch_bounds__(kThreads) void class_sum_kernel(Out o, int count, uint32_t blocks,
+                                                             Out o2, int count2) {
   constexpr int kLanes = kThreads / PG;
   __shared__ f32x4 sums[PG > 1 ? kThreads : 1];
+  const bool second = blockIdx.x >= blocks;  // (another sum behind the first)
+  if (second) {
+    o = o2;
+    count = count2;
+  }
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  const int64_t each = o.M * o.N, at = ((int64_t)blockIdx.x * kLanes + lane) * 4;
+  const int64_t each = o.M * o.N;
+  const int64_t at = ((int64_t)(blockIdx.x - (second ? blocks : 0)) * kLanes + lane) * 4;
   f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
   if (at + 4 <= each) {
     const float* p = o.parts + group * each + at;
@@ -643,8 +673,8 @@ GradPlace grad_place(int64_t N, int64_t D, int64_t K, int64_t es) {
   size_t most = 0;
   for (int64_t k : {w.piece, K - (K - 1) / w.piece * w.piece}) {
     const Plan h = tile::plan(N, D, k), c = tile::plan(k, D, N);
-    if (h.splits > 1) most = std::max(most, (size_t)(h.splits * N * D) * 4);
-    if (c.splits > 1) most = std::max(most, (size_t)(c.splits * k * D) * 4);
+    most = std::max(most, (size_t)((h.splits > 1 ? h.splits * N * D : 0) +
+                                   (c.splits > 1 ? c.splits * k * D : 0)) * 4);
   }
   w.total = at + up(most);
   return w;
@@ -713,24 +743,83 @@ hipError_t run_loss(const ClassArgs& c, float* loss, float* stats, char* ws, hip
   return hipGetLastError();
 }
 
-template <class P, int AK, int BK>
-hipError_t run_product(const Operand& a, const Operand& b, int64_t K, Out o, float* parts,
-                       hipStream_t stream) {
+struct Job {
+  Plan plan;
+  Product p;
+  int64_t blocks() const { return plan.mt * plan.nt * plan.splits; }
+};
+Job job(const Operand& a, const Operand& b, int64_t K, Out o, float* parts) {
   const Plan p = tile::plan(o.M, o.N, K);
   if (p.splits > 1) o.parts = parts;
-  const hipError_t e = with_tile<P, AK, BK>(p, a, b, [&](auto t) {
-    typedef decltype(t) TL;
-    return launch_tiles<class_product_kernel<TL>, TL>(p.mt * p.nt * p.splits, stream, a, b, K,
-                                                      p.each, (uint32_t)p.mt, (uint32_t)p.nt, o);
-  });
-  if (e != hipSuccess || p.splits == 1) return e;
+  return {p, {a, b, K, p.each, (uint32_t)p.mt, (uint32_t)p.nt, o}};
+}
+
+template <class P>
+hipError_t sum_parts(const Job* x, const Job* y, hipStream_t stream) {
+  typedef typename P::elem T;
+  if (x && x->plan.splits == 1) x = nullptr;
+  if (y && y->plan.splits == 1) y = nullptr;
+  if (!x) std::swap(x, y);
+  if (!x) return hipSuccess;
+  const int count = (int)x->plan.splits, count2 = y ? (int)y->plan.splits : 0;
+  const Out o = x->p.o, o2 = y ? y->p.o : o;
   auto sum = [&](auto* kernel, int groups) {
-    kernel<<<dim3((uint32_t)cdiv(o.M * o.N, 4 * kThreads / groups)), dim3(kThreads), 0, stream>>>(
-        o, (int)p.splits);
+    const int64_t each = 4 * kThreads / groups;
+    const int64_t blocks = cdiv(o.M * o.N, each), more = y ? cdiv(o2.M * o2.N, each) : 0;
+    kernel<<<dim3((uint32_t)(blocks + more)), dim3(kThreads), 0, stream>>>(
+        o, count, (uint32_t)blocks, o2, count2);
     return hipGetLastError();
   };
-  typedef typename P::elem T;
-  return p.splits > 8 ? sum(class_sum_kernel<T, 8>, 8) : sum(class_sum_kernel<T, 1>, 1);
+  return std::max(count, count2) > 8 ? sum(class_sum_kernel<T, 8>, 8)
+                                     : sum(class_sum_kernel<T, 1>, 1);
+}
+
+template <class P, int AK, int BK>
+hipError_t run_product(const Job& w, hipStream_t stream) {
+  return with_tile<P, AK, BK>(w.plan, w.p.a, w.p.b, [&](auto t) {
+    typedef decltype(t) TL;
+    return launch_tiles<class_product_kernel<TL>, TL>(w.blocks(), stream, w.p);
+  });
+}
+
+// Both gradients' products. Short ones share a launch, in which neither waits for the other's last
+// tiles (300 rows by 20 classes, D = 512: 28 us a call instead of 33; the large tile
+// and long products gain nothing).
+constexpr int64_t kSharedBlocks = 1024;
+template <class P>
+hipError_t run_products(const Job* c, const Job* h, hipStream_t stream) {
+  hipError_t e;
+  if (c && h && c->blocks() + h->blocks() <= kSharedBlocks && c->plan.shape != tile::k256 &&
+      h->plan.shape != tile::k256 && c->plan.shape != tile::k256x32 &&
+      h->plan.shape != tile::k256x32) {
+    typedef std::conditional_t<std::is_same_v<P, F32>, tile::X3, P> Q;
+    typedef Tile<Q, kCols, kCols, 128, 128, 2, 2> C128;
+    typedef Tile<P, kCols, kCols, 32, 256, 1, 4> C32;
+    typedef Tile<Q, kRows, kCols, 128, 128, 2, 2> H128;
+    typedef Tile<P, kRows, kCols, 32, 256, 1, 4> H32;
+    auto both = [&](auto t, auto u) {
+      typedef decltype(t) TC;
+      typedef decltype(u) TH;
+      constexpr int kLds = TC::kLds > TH::kLds ? TC::kLds : TH::kLds;
+      const hipError_t err = allow_lds<class_products_kernel<TC, TH>>(kLds);
+      if (err != hipSuccess) return err;
+      class_products_kernel<TC, TH>
+          <<<dim3((uint32_t)(c->blocks() + h->blocks())), dim3(TC::T), kLds, stream>>>(
+              c->p, (uint32_t)c->blocks(), h->p);
+      return hipGetLastError();
+    };
+    const bool c32 = c->plan.shape == tile::k32x256, h32 = h->plan.shape == tile::k32x256;
+    e = c32 ? h32 ? both(C32(), H32()) : both(C32(), H128())
+            : h32 ? both(C128(), H32()) : both(C128(), H128());
+    return e != hipSuccess ? e : sum_parts<P>(c, h, stream);
+  }
+  if (c) {
+    if ((e = run_product<P, kCols, kCols>(*c, stream)) != hipSuccess) return e;
+    if ((e = sum_parts<P>(c, nullptr, stream)) != hipSuccess) return e;
+  }
+  if (!h) return hipSuccess;
+  e = run_product<P, kRows, kCols>(*h, stream);
+  return e != hipSuccess ? e : sum_parts<P>(h, nullptr, stream);
 }
 
 template <class P>
@@ -785,18 +874,13 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
                        : sum(class_dscores_parts_kernel<T, 1>, 1);
     }
     if (e != hipSuccess) return e;
-    if (dC) {
-      const Out o{reinterpret_cast<T*>(dC) + first * c.D, nullptr, nullptr, nullptr, K, c.D};
-      e = run_product<P, kCols, kCols>({dS, w.ld, K, nullptr}, {c.H, c.ldh, c.D, rows}, c.N, o,
-                                       parts, stream);
-      if (e != hipSuccess) return e;
-    }
-    if (dH) {
-      const Out o{dH, last ? nullptr : sums, nullptr, first ? sums : nullptr, c.N, c.D};
-      e = run_product<P, kRows, kCols>({dS, w.ld, c.N, nullptr}, {C, c.ldc, c.D, part_open}, K, o,
-                                       parts, stream);
-      if (e != hipSuccess) return e;
-    }
+    const Out oc{reinterpret_cast<T*>(dC) + first * c.D, nullptr, nullptr, nullptr, K, c.D};
+    const Out oh{dH, last ? nullptr : sums, nullptr, first ? sums : nullptr, c.N, c.D};
+    const Job jc = job({dS, w.ld, K, nullptr}, {c.H, c.ldh, c.D, rows}, c.N, oc, parts);
+    const Job jh = job({dS, w.ld, c.N, nullptr}, {C, c.ldc, c.D, part_open}, K, oh,
+                       parts + (jc.plan.splits > 1 ? jc.plan.splits * K * c.D : 0));
+    if ((e = run_products<P>(dC ? &jc : nullptr, dH ? &jh : nullptr, stream)) != hipSuccess)
+      return e;
   }
   return hipSuccess;
 }

@@ -530,8 +530,14 @@ inline bool once(const Plan& p, const Operand& a, const Operand& b, int es) {
   return ((uintptr_t)wide.p | (uintptr_t)(wide.ld * es)) % 128 == 0;
 }
 
-// For [M][N] sums over K: the large tile where there is one for every compute unit, narrow
-// ones where a side is short, and parts of the reduction where that leaves the chip idle.
+// Whether the large tile, one to a compute unit, finishes before the tile of a quarter of its size, two to
+// a unit, which takes 5/8 of the time (4096 x 4096 by 2048 bf16, one round and two: 67 us
+// instead of 83; 4096 x 5120, two and three: 118 instead of 103).
+inline bool large_pays(int64_t M, int64_t N) {
+  return 8 * cdiv(cdiv(M, 256) * cdiv(N, 256), 256) <= 5 * cdiv(cdiv(M, 128) * cdiv(N, 128), 512);
+}
+
+// For [M][N] sums over K: the large tile or the one of a quarter of its size, narrow ones where a side is short, and parts of the reduction where that leaves the chip idle.
 inline Plan plan(int64_t M, int64_t N, int64_t K) {
   Plan p;
   int64_t slots;  // workgroups that the chip holds at once
@@ -541,7 +547,7 @@ inline Plan plan(int64_t M, int64_t N, int64_t K) {
   } else if (N <= 32) {
     p = {k256x32, cdiv(M, 256), 1, 1, 0};
     slots = 512;
-  } else if (cdiv(M, 256) * cdiv(N, 256) >= 192) {
+  } else if (large_pays(M, N)) {
     p = {k256, cdiv(M, 256), cdiv(N, 256), 1, 0};
     slots = 256;
   } else {
