@@ -37,6 +37,8 @@ struct Operand {
   int64_t extent;        // rows of the tile's own dimension
   const uint64_t* live;  // kCols: a bit for each k that takes part (null: all do); the
                          // others' rows are not looked at and count as 0
+  int64_t rest = 0;      // a product's first operand: bytes from its values to what their type's
+                         // rounding left of them, which is multiplied too (0: nothing)
 };
 
 // Strides up to this keep a tile's offsets in 32 bits.
@@ -226,14 +228,14 @@ struct Loader {
   }
 
   // Stage [k, min(k + kBk, end)) to a slot of the ring.
-  __device__ __forceinline__ void load(int64_t k, int64_t end, int slot) {
+  __device__ __forceinline__ void load(int64_t k, int64_t end, int slot, int64_t more = 0) {
     u32x4(&reg)[kPasses] = ring[slot];
     if constexpr (KIND == kImage) {
 #pragma unroll
       for (int p = 0; p < kPasses; ++p)  // (an image's reduction is whole stages)
         reg[p] = *reinterpret_cast<const u32x4*>(base + k * 32 + off[p]);
     } else if constexpr (KIND == kRows) {
-      const char* at = base + k * P::kEs;
+      const char* at = base + k * P::kEs + more;
       if (k + P::kBk <= end) {
         pieces(reg, [&](int p) { return at + off[p]; });
       } else {
@@ -244,7 +246,7 @@ struct Loader {
                              : load_part<P, (RING > 1)>(at + off[p], (int)left, k + cols >= kE);
       }
     } else {
-      const char* at = base + k * ld;
+      const char* at = base + k * ld + more;
       const uint64_t bits = live ? live[k >> 6] >> (k & 63) : ~uint64_t(0);
       if (k + P::kBk + kE <= end) {
         // (a piece across the row's end runs into the next rows, of which there are enough: what
@@ -383,10 +385,14 @@ struct Tile {
     Loader<P, AK, BM, T, kRing, (ONCE && BN == 32)> la(a, m0, tid);
     Loader<P, BK_, BN, T, kRing, (ONCE && BM == 32)> lb(b, n0, tid);
     // (stages are counted in 32 bits: a reduction is far shorter)
-    const int stages = (int)((k1 - k0 + P::kBk - 1) / P::kBk);
+    // With a rest each stage comes twice, the second time with the rest of a's values (and b's
+    // again, from a cache).
+    const int twice = a.rest != 0;
+    const int stages = (int)((k1 - k0 + P::kBk - 1) / P::kBk) << twice;
     auto load = [&](int s, int slot) {
-      la.load(k0 + (int64_t)s * P::kBk, k1, slot);
-      lb.load(k0 + (int64_t)s * P::kBk, k1, slot);
+      const int64_t k = k0 + (int64_t)(s >> twice) * P::kBk;
+      la.load(k, k1, slot, s & twice ? a.rest : 0);
+      lb.load(k, k1, slot);
     };
     auto store = [&](char* to, int slot) {
       la.store(to, tid, slot);
