@@ -450,7 +450,6 @@ struct Tile {
           // (the next stage is there, and the rest of this one is in registers)
           if (kk == 3) __syncthreads();
           multiply(0, 0);
-          __builtin_amdgcn_sched_barrier(0);
         }
       }
     };
