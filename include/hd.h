@@ -476,7 +476,8 @@ hd_status hd_byte_product(const void *X, int64_t ldx, const float *row_scales, c
  * outputs) and class vectors C[K][D], without the scores S = H C^T being kept:
  *   s_k = sum_d H[n][d] C[k][d],  m = max_k s_k,  L = log sum_k exp(scale (s_k - m)),
  *   loss = L - scale (s_y - m),  stats = {m, L}          (loss = -logp of hd_logprobs)
- * H and C are of dt, loss and stats fp32, sums fp32 (an H or C of fp32 is used in full). mask, if not
+ * H and C are of dt, loss and stats fp32, sums fp32 (an H or C of fp32 is used in full, but for
+ * products of its lowest bits, within 2^-22 of the whole; an infinity in it may count as NaN). mask, if not
  * NULL, is K bytes: classes whose byte is 0 take no part, and what their vectors hold is not
  * looked at.
  *   - y[n] outside [0, K): no class is asked for, loss = 0. Such rows have no gradient and pass none
@@ -503,7 +504,8 @@ hd_status hd_class_loss(const void *H, int64_t ldh, const void *C, int64_t ldc,
  *   dH[n][d] = sum_k dS[n][k] C[k][d],   dC[k][d] = sum_n dS[n][k] H[n][d],
  * both of dt, contiguous [N][D] and [K][D]; either may be NULL (not both). dS is 0 in classes that
  * take no part and rows that ask for none, and those classes' vectors and rows' encodings count
- * as 0. For HD_BF16 dS is rounded to bf16 before the two products; sums are fp32. N == 0 clears dC.
+ * as 0. For HD_BF16 dS is rounded to bf16 before the two products (to two bf16 values where N <= 128);
+ * sums are fp32. N == 0 clears dC.
  */
 size_t hd_class_loss_grad_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
 hd_status hd_class_loss_grad(const void *H, int64_t ldh, const void *C, int64_t ldc,

@@ -11,9 +11,18 @@
 //
 // In LDS a kRows operand is [row][8 pieces of 16 bytes], piece j at j ^ (row / 2 % 8): a lane's
 // operand of the 32 x 32 instruction is one piece, and 16 lanes' pieces, of 16 rows, lie in all 64
-// banks (with j ^ (row % 8) two at a time share theirs: 37% of the LDS's cycles, measured). A kCols operand is [k][R values] as in memory; bf16 takes its operands with transposing
-// reads (16 lanes read 4 rows of 16 values and get 4 values of one column each), fp32, whose
-// instruction takes one k from a lane, with plain ones.
+// banks (with j ^ (row % 8) two at a time share theirs: 37% of the LDS's cycles). A kCols operand
+// is [k][R values] as in memory; bf16 takes its operands with transposing reads (16 lanes read 4
+// rows of 16 values and get 4 values of one column each), fp32, whose instruction takes one k
+// from a lane, with plain ones.
+//
+// What bounds the large tile (256 x 256, eight waves of 128 x 64): the matrix units are busy for half
+// of the cycles at 2.1 GHz. It is not memory (with every load from a cache's hot lines 4096 x
+// 131072 by 4096 bf16 took 3.73 ms instead of 3.87) and not the wait for operands (reading them a
+// quarter ahead changed nothing); a stage's 256 KB through LDS are half of its cycles. Measured: that
+// product with the epilogue of a cross entropy 3.7 ms (1.19 PFLOP/s, where a library product of
+// 8192^3 reaches 1.4 to 1.5), int8 8192 x 4096 x 16384 0.57 ms (1.9 POP/s), fp32 in three parts
+// 777 x 2047 x 32003 0.60 ms (170 TFLOP/s; fp32's own instruction 1.02 ms).
 #pragma once
 
 #include <type_traits>
@@ -108,8 +117,8 @@ struct I8 {
 };
 
 // The first `valid` elements at p, zeros behind them. With `back`, the elements before p are there
-// too, and one load takes those that end with the last valid one (BACK: not in the large tile, whose
-// registers are full).
+// too, and one load takes those that end with the last valid one (BACK: not in the large tile,
+// whose registers are full).
 template <class P, bool BACK>
 __device__ __forceinline__ u32x4 load_part(const char* p, int valid, bool back) {
   constexpr int kE = 16 / P::kEs;
@@ -128,7 +137,7 @@ __device__ __forceinline__ u32x4 load_part(const char* p, int valid, bool back) 
     hi >>= s;
     return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
   }
-  // (a loop, not 16 bytes' worth of straight code: it is rare, and short kernels wait for their code)
+  // (a loop, not 16 bytes' worth of straight code: it is rare, and short kernels wait for code)
   uint64_t lo = 0, hi = 0;
 #pragma unroll 1
   for (int e = valid - 1; e >= 0; --e) {
@@ -366,7 +375,9 @@ struct Tile {
   static constexpr int kSets = P::kParts;
   // Stages loaded ahead: as many as the registers hold. The large tile has the time of a whole
   // stage (over 2000 cycles) for each load; smaller ones, and short reductions, wait for memory.
-  static constexpr int kRing = BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128 && P::kParts == 3 ? 3 : 2;
+  static constexpr int kRing = BM * BN > 128 * 128                       ? 1
+                               : BM * BN == 128 * 128 && P::kParts == 3 ? 3
+                                                                        : 2;
   typedef typename P::acc Acc;
 
   // The sum over k in [k0, k1). All threads of the workgroup; ends with a barrier.
@@ -535,14 +546,15 @@ inline bool once(const Plan& p, const Operand& a, const Operand& b, int es) {
   return ((uintptr_t)wide.p | (uintptr_t)(wide.ld * es)) % 128 == 0;
 }
 
-// Whether the large tile, one to a compute unit, finishes before the tile of a quarter of its size, two to
-// a unit, which takes 5/8 of the time (4096 x 4096 by 2048 bf16, one round and two: 67 us
+// Whether the large tile, one to a compute unit, finishes before the tile of a quarter of its size,
+// two to a unit, which takes 5/8 of the time (4096 x 4096 by 2048 bf16, one round and two: 67 us
 // instead of 83; 4096 x 5120, two and three: 118 instead of 103).
 inline bool large_pays(int64_t M, int64_t N) {
   return 8 * cdiv(cdiv(M, 256) * cdiv(N, 256), 256) <= 5 * cdiv(cdiv(M, 128) * cdiv(N, 128), 512);
 }
 
-// For [M][N] sums over K: the large tile or the one of a quarter of its size, narrow ones where a side is short, and parts of the reduction where that leaves the chip idle.
+// For [M][N] sums over K: the large tile or the one of a quarter of its size, narrow ones where a
+// side is short, and parts of the reduction where that leaves the chip idle.
 inline Plan plan(int64_t M, int64_t N, int64_t K) {
   Plan p;
   int64_t slots;  // workgroups that the chip holds at once
