@@ -298,3 +298,23 @@ def test_other_stream_and_graph():
     torch.cuda.synchronize()
     for a, b in zip(got, want[0]):
         assert torch.equal(torch.nan_to_num(a, nan=9.0), torch.nan_to_num(b, nan=9.0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_far_apart(dtype):
+    """Strides at which offsets pass 32 bits: the bits of contiguous rows."""
+    hd = hd_gpu()
+    announce(f"class loss, rows far apart {dtype}")
+    N, K, D, ld = 1100, 60, 200, 1 << 20
+    H, C, y, m, up, scale = make(N, K, D, dtype, seed=13, mask=0.8)
+    wide = torch.empty(N, ld, dtype=dtype, device="cuda")  # 4.6 GB in fp32
+    wide[:, 7:7 + D] = H.cuda()
+    far = wide[:, 7:7 + D]
+    dev = (C.cuda(), y.cuda())
+    got, want = [], []
+    for x, out in ((far, got), (H.cuda(), want)):
+        cl = hd.class_loss(x, *dev, scale=scale, mask=m.cuda())
+        out += [cl.loss, cl.stats, *hd.class_loss_grad(x, *dev, cl, up.cuda(), scale=scale,
+                                                       mask=m.cuda())]
+    for a, b in zip(got, want):
+        assert torch.equal(torch.nan_to_num(a.float(), nan=9.0), torch.nan_to_num(b.float(), nan=9.0))
