@@ -489,7 +489,8 @@ hd_status hd_byte_product(const void *X, int64_t ldx, const float *row_scales, c
  *     for) and stats NaN.
  * workspace: hd_class_loss_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant before and
  * undefined after the call.
- * Limits: N, K <= 2^24, D <= 2^20, N * K, N * D and K * D <= 2^38, row strides up to 2^22.
+ * Limits: 0 < scale < 2^127, N, K <= 2^24, D <= 2^20, N * K, N * D and K * D <= 2^38, row strides
+ * up to 2^22.
  */
 size_t hd_class_loss_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
 hd_status hd_class_loss(const void *H, int64_t ldh, const void *C, int64_t ldc,

@@ -81,7 +81,8 @@ hd_status class_sizes(int64_t N, int64_t D, int64_t K, int dt) {
 hd_status class_args(const void* H, int64_t ldh, const void* C, int64_t ldc, const int32_t* y,
                      float scale, const float* stats, int64_t N, int64_t D, int64_t K, int dt) {
   const hd_status st = class_sizes(N, D, K, dt);
-  if (st == HD_ERR_ARG || !(scale > 0.0f) || !isfinite(scale) || ldh < D || ldc < D)
+  // (the kernels take scale log2(e), under 2 scale)
+  if (st == HD_ERR_ARG || !(scale > 0.0f) || !isfinite(2.0f * scale) || ldh < D || ldc < D)
     return HD_ERR_ARG;
   if (st != HD_OK || ldh > kMaxStride || ldc > kMaxStride) return HD_ERR_UNSUPPORTED;
   if (N == 0) return HD_OK;

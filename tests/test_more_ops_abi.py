@@ -37,7 +37,7 @@ def test_class_loss_refusals(L):
     assert f(st=None) == ARG and f(ws=None) == ARG and f(ws=FAKE + 8) == ARG
     assert f(N=-1) == ARG and f(D=0) == ARG and f(K=0) == ARG and f(dt=7) == ARG
     assert f(ldh=7) == ARG and f(ldc=7) == ARG
-    for scale in (0.0, -1.0, math.inf, math.nan):
+    for scale in (0.0, -1.0, math.inf, math.nan, 3e38):
         assert f(scale=scale) == ARG
     assert f(H=FAKE + 2) == ARG and f(C=FAKE + 1) == ARG and f(y=FAKE + 2) == ARG
     assert f(loss=FAKE + 2) == ARG and f(st=FAKE + 1) == ARG
