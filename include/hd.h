@@ -505,8 +505,8 @@ hd_status hd_class_loss(const void *H, int64_t ldh, const void *C, int64_t ldc,
  *   dH[n][d] = sum_k dS[n][k] C[k][d],   dC[k][d] = sum_n dS[n][k] H[n][d],
  * both of dt, contiguous [N][D] and [K][D]; either may be NULL (not both). dS is 0 in classes that
  * take no part and rows that ask for none, and those classes' vectors and rows' encodings count
- * as 0. For HD_BF16 dS is rounded to bf16 before the two products (to two bf16 values where N <= 128);
- * sums are fp32. N == 0 clears dC.
+ * as 0. For HD_BF16 the two products take dS as two bf16 values, within 2^-16 of it; sums are fp32
+ * and the result is rounded once. N == 0 clears dC.
  */
 size_t hd_class_loss_grad_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
 hd_status hd_class_loss_grad(const void *H, int64_t ldh, const void *C, int64_t ldc,

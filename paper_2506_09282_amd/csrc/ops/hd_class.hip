@@ -13,7 +13,8 @@
 // exchange between lanes.
 //
 // Many classes are bound by the matrix units: a forward pass of 4096 x 131072 by 4096 bf16 takes 3.7 ms,
-// a backward pass of 4096 x 65536 by 4096 6.3 ms (1.04 PFLOP/s, epilogues included). Few
+// a backward pass of 4096 x 65536 by 4096 10.2 ms (1.08 PFLOP/s of its five products, two of them
+// for the rest of dS). Few
 // classes are bound by reading H, once forward and twice backward: 16384 x 10240 fp32 under 26
 // classes 114 and 258 us (5.9 and 5.2 TB/s).
 //
@@ -45,11 +46,15 @@ constexpr int kThreads = 256;
 // that writes them and the two that read them.
 constexpr int64_t kPieceBytes = int64_t(128) << 20;
 
-// bf16 gradients of up to this many rows are kept as two bf16 values. The rounding of dS to one is
-// as large as that of the result; over many rows the two together are 1.41 times one of
-// them, but over a few the rows' own roundings may be 1.6 times. The second value costs the products
-// a second pass over each stage in LDS, hidden by memory while the rows are few.
-constexpr int64_t kTwoValueRows = 128;
+// bf16 values that hold one of dS: two for the bf16 products, within 2^-16 of it. One is not enough
+// at any size: while the class vectors are nearly equal (before the first refining step) every row's dS
+// is rounded alike, and the gradients cancel what the encodings, or the class vectors, have in
+// common, but not what was rounded off with it (4096 rows with a shared component under 10 equal
+// classes: errors of dC 31 times its own rounding). The second value costs the products a second
+// pass over each stage (4096 x 65536 by 4096 10.2 ms instead of 6.3; 16384 x 10240 under 26 classes,
+// their gradient alone, 150 us instead of 123).
+template <typename T>
+constexpr int kValues = sizeof(T) == 2 ? 2 : 1;
 
 struct Scores {  // of the classes [0, K) of a piece
   Operand H, C;
@@ -373,11 +378,11 @@ __device__ __forceinline__ float score_grad(const RowGrad& r, float s, int64_t k
   return r.on && open ? r.g * p : 0.0f;
 }
 
-// dS[n][class] of a piece, rows of ld elements.
+// dS[value][n][class] of a piece, rows of ld elements.
 template <class TL>
 __global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
     Scores a, int64_t K_all, const float* __restrict__ stats, const float* __restrict__ g,
-    typename TL::P::elem* __restrict__ dS, int64_t ld, int values) {
+    typename TL::P::elem* __restrict__ dS, int64_t ld) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   uint32_t mi, ni;
   tile_at(die_order(blockIdx.x, gridDim.x), a.mt, a.nt, mi, ni);
@@ -390,57 +395,60 @@ __global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
   const int wm = wave / TL::WN, wn = wave % TL::WN;
   const float scale2 = a.scale * kLog2e;
   typedef typename TL::P::elem T;
-  // [32 samples][up to 256 bytes of the wave's classes], so that the stores run along the rows
-  constexpr int kTiles = TL::MT * 32 * sizeof(T) > 256 ? 256 / (32 * sizeof(T)) : TL::MT;
-  constexpr int kAcross = kTiles * 32, kPitch = kAcross + 16 / sizeof(T);
-  static_assert(TL::WM * TL::WN * 32 * kPitch * sizeof(T) <= TL::kLds, "");
+  // [32 samples][up to 256 bytes of the wave's classes, first values before second], so that the
+  // stores run along the rows
+  constexpr int kV = kValues<T>, kMost = 256 / (32 * sizeof(T) * kV);
+  constexpr int kTiles = TL::MT > kMost ? kMost : TL::MT;
+  constexpr int kAcross = kTiles * 32, kPitch = kV * kAcross + 16 / sizeof(T);
+  static_assert(TL::MT % kTiles == 0 && TL::WM * TL::WN * 32 * kPitch * sizeof(T) <= TL::kLds, "");
   T* mine = reinterpret_cast<T*>(lds) + wave * 32 * kPitch;
-  // (the large tile is for more rows than kTwoValueRows)
-  constexpr bool kTwo = sizeof(T) == 2 && TL::BM * TL::BN <= 128 * 128;
-#pragma unroll 1
-  for (int value = 0; value < (kTwo ? values : 1); ++value, dS += a.N * ld) {
 #pragma unroll
-    for (int j = 0; j < TL::NT; ++j) {
-      const int64_t nw = n0 + (wn * TL::NT + j) * 32, n = nw + (lane & 31);
-      const RowGrad row = row_grad(a, stats, g, K_all, n < a.N ? n : a.N - 1);
+  for (int j = 0; j < TL::NT; ++j) {
+    const int64_t nw = n0 + (wn * TL::NT + j) * 32, n = nw + (lane & 31);
+    const RowGrad row = row_grad(a, stats, g, K_all, n < a.N ? n : a.N - 1);
 #pragma unroll
-      for (int i0 = 0; i0 < TL::MT; i0 += kTiles) {
-        const int64_t first = m0 + (wm * TL::MT + i0) * 32;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    for (int i0 = 0; i0 < TL::MT; i0 += kTiles) {
+      const int64_t first = m0 + (wm * TL::MT + i0) * 32;
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          uint32_t bits = open_bits(a, first + i * 32);
-          asm volatile("" : "+v"(bits));  // (worked out for each column again)
+      for (int i = 0; i < kTiles; ++i) {
+        uint32_t bits = open_bits(a, first + i * 32);
+        asm volatile("" : "+v"(bits));  // (worked out for each column again)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            f32x4 v;
+        for (int q = 0; q < 4; ++q) {
+          f32x4 v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int at = q * 8 + half * 4 + e;
-              v[e] = score_grad(row, c[i0 + i][j][4 * q + e], first + i * 32 + at, bits >> at & 1,
-                                scale2);
-              if (kTwo && value) v[e] -= bf16_to_f32(to_bf16(v[e]));
-            }
-            store_four(mine, (lane & 31) * kPitch + i * 32 + q * 8 + half * 4, v, 4);
-            __builtin_amdgcn_sched_barrier(0);  // (four at a time: the registers hold the sums)
+          for (int e = 0; e < 4; ++e) {
+            const int at = q * 8 + half * 4 + e;
+            v[e] = score_grad(row, c[i0 + i][j][4 * q + e], first + i * 32 + at, bits >> at & 1,
+                              scale2);
           }
+          const int at = (lane & 31) * kPitch + i * 32 + q * 8 + half * 4;
+          store_four(mine, at, v, 4);
+          if constexpr (kV > 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] -= bf16_to_f32(to_bf16(v[e]));
+            store_four(mine, at + kAcross, v, 4);
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (four at a time: the registers hold the sums)
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        // (ld is a multiple of 8: a piece of 16 bytes fits or begins past it)
-        constexpr int kE = 16 / sizeof(T), kPieces = kAcross / kE;
-        int q0 = threadIdx.x & 63;
-        asm volatile("" : "+v"(q0));
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      // (ld is a multiple of 8: a piece of 16 bytes fits or begins past it)
+      constexpr int kE = 16 / sizeof(T), kPieces = kAcross / kE;
+      int q0 = threadIdx.x & 63;
+      asm volatile("" : "+v"(q0));
 #pragma unroll 1
-        for (int q = q0; q < 32 * kPieces; q += 64) {
-          const int r = q / kPieces, k = q % kPieces * kE;
-          if (nw + r < a.N && first + k < ld)
-            *reinterpret_cast<u32x4*>(dS + (nw + r) * ld + first + k) =
-                *reinterpret_cast<const u32x4*>(mine + r * kPitch + k);
-        }
+      for (int q = q0; q < 32 * kV * kPieces; q += 64) {
+        const int r = q / (kV * kPieces), piece = q % (kV * kPieces);
+        const int value = piece / kPieces, k = piece % kPieces * kE;
+        if (nw + r < a.N && first + k < ld)
+          *reinterpret_cast<u32x4*>(dS + (value * a.N + nw + r) * ld + first + k) =
+              *reinterpret_cast<const u32x4*>(mine + r * kPitch + value * kAcross + k);
       }
     }
   }
@@ -477,8 +485,8 @@ __global__ __launch_bounds__(kThreads) void class_bits_kernel(const int32_t* __r
 template <typename T, int PG>
 __global__ __launch_bounds__(kThreads) void class_dscores_parts_kernel(
     Scores a, Parts sc, const float* __restrict__ stats, const float* __restrict__ g,
-    T* __restrict__ dS, int64_t ld, int values, const uint8_t* __restrict__ mask, uint32_t blocks,
-    uint64_t* rows, uint64_t* classes) {
+    T* __restrict__ dS, int64_t ld, const uint8_t* __restrict__ mask, uint32_t blocks, uint64_t* rows,
+    uint64_t* classes) {
   constexpr int kLanes = kThreads / PG;
   __shared__ f32x4 sums[PG > 1 ? kThreads : 1];
   if (blockIdx.x >= blocks) {
@@ -500,7 +508,7 @@ __global__ __launch_bounds__(kThreads) void class_dscores_parts_kernel(
   for (int e = 0; e < 4; ++e) {
     const float d = score_grad(row, v[e], k + e, bits >> e & 1, a.scale * kLog2e);
     store_elem(dS, n * ld + k + e, d);
-    if (sizeof(T) == 2 && values > 1)
+    if (kValues<T> > 1)
       store_elem(dS, (a.N + n) * ld + k + e, d - bf16_to_f32(to_bf16(d)));
   }
 }
@@ -646,8 +654,8 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 // How a call cuts its classes: one piece where the scores go through the workspace in
 // parts, else as many classes as kPieceBytes hold.
-int64_t piece_of(int64_t N, int64_t K, int64_t es) {
-  int64_t k = kPieceBytes / (N * es) / 256 * 256;
+int64_t piece_of(int64_t N, int64_t K, int64_t each) {
+  int64_t k = kPieceBytes / (N * each) / 256 * 256;
   if (k < 256) k = 256;
   return k < K ? k : K;
 }
@@ -674,19 +682,19 @@ LossPlace loss_place(int64_t N, int64_t D, int64_t K) {
 
 struct GradPlace {
   int64_t piece, ld;  // classes at a time, and of a row of dS
-  int values;         // that hold one of dS
   size_t rows, open, dS, scores, sums, parts, total;
 };
-GradPlace grad_place(int64_t N, int64_t D, int64_t K, int64_t es) {
+template <typename T>
+GradPlace grad_place(int64_t N, int64_t D, int64_t K) {
   GradPlace w;
+  constexpr int64_t kEach = kValues<T> * sizeof(T);  // bytes of one of dS
   const Plan s = tile::plan(K, N, D);
-  w.piece = s.splits > 1 ? K : piece_of(N, K, es);
+  w.piece = s.splits > 1 ? K : piece_of(N, K, kEach);
   w.ld = cdiv(w.piece, 8) * 8;
-  w.values = es == 2 && N <= kTwoValueRows ? 2 : 1;
   w.rows = 0;
   w.open = up((size_t)cdiv(N, 64) * 8);
   w.dS = w.open + up((size_t)cdiv(K, 64) * 8);
-  w.scores = w.dS + up((size_t)w.values * N * w.ld * es);
+  w.scores = w.dS + up((size_t)N * w.ld * kEach);
   size_t at = w.scores;
   if (s.splits > 1) at += up((size_t)s.splits * N * s.mt * tile_m(s) * 4);
   w.sums = at;
@@ -849,7 +857,7 @@ template <class P>
 hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void* dH, void* dC,
                     char* ws, hipStream_t stream) {
   typedef typename P::elem T;
-  const GradPlace w = grad_place(c.N, c.D, c.K, P::kEs);
+  const GradPlace w = grad_place<T>(c.N, c.D, c.K);
   uint64_t* rows = reinterpret_cast<uint64_t*>(ws + w.rows);
   uint64_t* open = reinterpret_cast<uint64_t*>(ws + w.open);
   if (!dC) rows = nullptr;
@@ -881,7 +889,7 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
       e = with_tile<P, kRows, kRows>(s, a.C, a.H, [&](auto t) {
         typedef decltype(t) TL;
         return launch_tiles<class_dscores_kernel<TL>, TL>(tiles, stream, a, c.K, stats, g, dS,
-                                                          w.ld, w.values);
+                                                          w.ld);
       });
     } else {
       float* scores = reinterpret_cast<float*>(ws + w.scores);
@@ -890,7 +898,7 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
       auto sum = [&](auto* kernel, int groups) {
         const uint32_t blocks = (uint32_t)cdiv(c.N * w.ld / 4, kThreads / groups);
         kernel<<<dim3(blocks + bit_blocks), dim3(kThreads), 0, stream>>>(
-            a, sc, stats, g, dS, w.ld, w.values, c.mask, blocks, rows, open);
+            a, sc, stats, g, dS, w.ld, c.mask, blocks, rows, open);
         return hipGetLastError();
       };
       e = sc.count > 8 ? sum(class_dscores_parts_kernel<T, 8>, 8)
@@ -899,7 +907,7 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
     if (e != hipSuccess) return e;
     const Out oc{reinterpret_cast<T*>(dC) + first * c.D, nullptr, nullptr, nullptr, K, c.D};
     const Out oh{dH, last ? nullptr : sums, nullptr, first ? sums : nullptr, c.N, c.D};
-    const int64_t rest = w.values > 1 ? c.N * w.ld * P::kEs : 0;
+    const int64_t rest = kValues<T> > 1 ? c.N * w.ld * P::kEs : 0;
     const Job jc = job({dS, w.ld, K, nullptr, rest}, {c.H, c.ldh, c.D, rows}, c.N, oc, parts);
     const Job jh = job({dS, w.ld, c.N, nullptr, rest}, {C, c.ldc, c.D, part_open}, K, oh,
                        parts + (jc.plan.splits > 1 ? jc.plan.splits * K * c.D : 0));
@@ -913,7 +921,7 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
 
 size_t class_loss_ws_bytes(int64_t N, int64_t D, int64_t K) { return loss_place(N, D, K).total; }
 size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt) {
-  return grad_place(N, D, K, dt == 0 ? 4 : 2).total;
+  return (dt == 0 ? grad_place<float>(N, D, K) : grad_place<bf16raw>(N, D, K)).total;
 }
 
 hipError_t launch_class_loss(const ClassArgs& a, float* loss, float* stats, void* workspace,

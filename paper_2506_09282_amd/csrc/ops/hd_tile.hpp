@@ -537,11 +537,12 @@ struct Plan {
 };
 
 // Whether the wide operand of a narrow tile goes past the caches: each of its values passes one
-// workgroup, but where lines hold parts of two rows or stages, those take it from the cache
+// workgroup, once (twice where the other operand has a rest: 16384 x 10240 bf16 under 26 classes 150
+// us instead of 166 through the caches), but where lines hold parts of two rows or stages, those take it from the cache
 // (16384 x 10240 fp32 under 26 classes: 114 us instead of 130; 100003 rows of 2000 bytes: 66
 // instead of 55).
 inline bool once(const Plan& p, const Operand& a, const Operand& b, int es) {
-  if (p.shape != k32x256 && p.shape != k256x32) return false;
+  if ((p.shape != k32x256 && p.shape != k256x32) || a.rest) return false;
   const Operand& wide = p.shape == k32x256 ? b : a;
   return ((uintptr_t)wide.p | (uintptr_t)(wide.ld * es)) % 128 == 0;
 }
