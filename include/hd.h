@@ -507,8 +507,14 @@ hd_status hd_class_loss(const void *H, int64_t ldh, const void *C, int64_t ldc,
  * take no part and rows that ask for none, and those classes' vectors and rows' encodings count
  * as 0. For HD_BF16 the two products take dS as two bf16 values, within 2^-16 of it; sums are fp32
  * and the result is rounded once. N == 0 clears dC.
+ * workspace: hd_class_loss_grad_workspace_bytes(...) bytes serve any call of these sizes,
+ * hd_class_loss_grad_workspace_bytes_of(...) one that gives the named gradients alone: dS of max(128
+ * MiB, N KiB) at most, fp32 sums of dH where the classes are taken in pieces, and parts of products
+ * with few tiles.
  */
 size_t hd_class_loss_grad_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt);
+size_t hd_class_loss_grad_workspace_bytes_of(int64_t N, int64_t D, int64_t K, hd_dtype dt,
+                                             int with_dH, int with_dC);
 hd_status hd_class_loss_grad(const void *H, int64_t ldh, const void *C, int64_t ldc,
                              const uint8_t *mask, const int32_t *y, float scale,
                              const float *stats, const float *g_loss, void *dH, void *dC,

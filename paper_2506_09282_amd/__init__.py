@@ -77,6 +77,7 @@ SYMBOLS = (
     "hd_class_loss_workspace_bytes",
     "hd_class_loss",
     "hd_class_loss_grad_workspace_bytes",
+    "hd_class_loss_grad_workspace_bytes_of",
     "hd_class_loss_grad",
     "hd_dropout",
 )
@@ -197,6 +198,8 @@ def lib():
         L.hd_class_loss.restype = i32
         L.hd_class_loss_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.hd_class_loss_grad_workspace_bytes.restype = sz
+        L.hd_class_loss_grad_workspace_bytes_of.argtypes = [i64, i64, i64, i32, i32, i32]
+        L.hd_class_loss_grad_workspace_bytes_of.restype = sz
         L.hd_class_loss_grad.argtypes = [vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, vp, i64, i64,
                                          i64, i32, vp, sz, vp]
         L.hd_class_loss_grad.restype = i32
@@ -1104,7 +1107,8 @@ def class_loss_grad(H, C, y, cl: ClassLoss, g_loss, scale: float = 1.0, mask=Non
         raise ValueError("stats must be float32 [N, 2] on the encodings' device")
     dH = torch.empty(N, D, dtype=H.dtype, device=H.device) if wrt != "classes" else None
     dC = torch.empty(K, D, dtype=H.dtype, device=H.device) if wrt != "encodings" else None
-    need = _need("hd_class_loss_grad_workspace_bytes", index, N, D, K, dt)
+    need = _need("hd_class_loss_grad_workspace_bytes_of", index, N, D, K, dt, dH is not None,
+                 dC is not None)
     ws = torch.empty(need, dtype=torch.uint8, device=H.device) if need else None
     st = lib().hd_class_loss_grad(H.data_ptr(), ldh, C.data_ptr(), ldc, mptr, yptr, scale,
                                   stats.data_ptr(), gptr, _ptr(dH), _ptr(dC), N, D, K, dt,

@@ -42,8 +42,9 @@ using tile::tile_at;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256;
 
-// Scores' gradients kept at a time. 128 MiB stay in the last cache (256 MB) between the launch
-// that writes them and the two that read them.
+// Scores' gradients kept at a time, in whole tiles of 256 classes (1 KiB a row at least, which is more
+// than this from 131072 rows on). 128 MiB stay in the last cache (256 MB) between the launch that
+// writes them and the two that read them.
 constexpr int64_t kPieceBytes = int64_t(128) << 20;
 
 // bf16 values that hold one of dS: two for the bf16 products, within 2^-16 of it. One is not enough
@@ -685,7 +686,7 @@ struct GradPlace {
   size_t rows, open, dS, scores, sums, parts, total;
 };
 template <typename T>
-GradPlace grad_place(int64_t N, int64_t D, int64_t K) {
+GradPlace grad_place(int64_t N, int64_t D, int64_t K, bool dH, bool dC) {
   GradPlace w;
   constexpr int64_t kEach = kValues<T> * sizeof(T);  // bytes of one of dS
   const Plan s = tile::plan(K, N, D);
@@ -698,14 +699,14 @@ GradPlace grad_place(int64_t N, int64_t D, int64_t K) {
   size_t at = w.scores;
   if (s.splits > 1) at += up((size_t)s.splits * N * s.mt * tile_m(s) * 4);
   w.sums = at;
-  if (w.piece < K) at += up((size_t)N * D * 4);
+  if (dH && w.piece < K) at += up((size_t)N * D * 4);
   w.parts = at;
   // (the last piece may be short, and its products split further)
   size_t most = 0;
   for (int64_t k : {w.piece, K - (K - 1) / w.piece * w.piece}) {
     const Plan h = tile::plan(N, D, k), c = tile::plan(k, D, N);
-    most = std::max(most, (size_t)((h.splits > 1 ? h.splits * N * D : 0) +
-                                   (c.splits > 1 ? c.splits * k * D : 0)) * 4);
+    most = std::max(most, (size_t)((dH && h.splits > 1 ? h.splits * N * D : 0) +
+                                   (dC && c.splits > 1 ? c.splits * k * D : 0)) * 4);
   }
   w.total = at + up(most);
   return w;
@@ -857,7 +858,7 @@ template <class P>
 hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void* dH, void* dC,
                     char* ws, hipStream_t stream) {
   typedef typename P::elem T;
-  const GradPlace w = grad_place<T>(c.N, c.D, c.K);
+  const GradPlace w = grad_place<T>(c.N, c.D, c.K, dH != nullptr, dC != nullptr);
   uint64_t* rows = reinterpret_cast<uint64_t*>(ws + w.rows);
   uint64_t* open = reinterpret_cast<uint64_t*>(ws + w.open);
   if (!dC) rows = nullptr;
@@ -910,7 +911,7 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
     const int64_t rest = kValues<T> > 1 ? c.N * w.ld * P::kEs : 0;
     const Job jc = job({dS, w.ld, K, nullptr, rest}, {c.H, c.ldh, c.D, rows}, c.N, oc, parts);
     const Job jh = job({dS, w.ld, c.N, nullptr, rest}, {C, c.ldc, c.D, part_open}, K, oh,
-                       parts + (jc.plan.splits > 1 ? jc.plan.splits * K * c.D : 0));
+                       parts + (dC && jc.plan.splits > 1 ? jc.plan.splits * K * c.D : 0));
     if ((e = run_products<P>(dC ? &jc : nullptr, dH ? &jh : nullptr, stream)) != hipSuccess)
       return e;
   }
@@ -920,8 +921,8 @@ hipError_t run_grad(const ClassArgs& c, const float* stats, const float* g, void
 }  // namespace
 
 size_t class_loss_ws_bytes(int64_t N, int64_t D, int64_t K) { return loss_place(N, D, K).total; }
-size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt) {
-  return (dt == 0 ? grad_place<float>(N, D, K) : grad_place<bf16raw>(N, D, K)).total;
+size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt, bool dH, bool dC) {
+  return (dt == 0 ? grad_place<float>(N, D, K, dH, dC) : grad_place<bf16raw>(N, D, K, dH, dC)).total;
 }
 
 hipError_t launch_class_loss(const ClassArgs& a, float* loss, float* stats, void* workspace,

@@ -142,7 +142,7 @@ struct ClassArgs {
 size_t class_loss_ws_bytes(int64_t N, int64_t D, int64_t K);
 hipError_t launch_class_loss(const ClassArgs& a, float* loss, float* stats, void* workspace,
                              hipStream_t stream);
-size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt);
+size_t class_grad_ws_bytes(int64_t N, int64_t D, int64_t K, int dt, bool dH, bool dC);
 hipError_t launch_class_loss_grad(const ClassArgs& a, const float* stats, const float* g_loss,
                                   void* dH, void* dC, void* workspace, hipStream_t stream);
 

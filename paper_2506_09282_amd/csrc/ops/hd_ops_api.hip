@@ -357,8 +357,12 @@ hd_status hd_class_loss(const void* H, int64_t ldh, const void* C, int64_t ldc,
 }
 
 size_t hd_class_loss_grad_workspace_bytes(int64_t N, int64_t D, int64_t K, hd_dtype dt) {
-  if (N < 1 || class_sizes(N, D, K, dt) != HD_OK) return 0;
-  return hd::ops::class_grad_ws_bytes(N, D, K, dt);
+  return hd_class_loss_grad_workspace_bytes_of(N, D, K, dt, 1, 1);
+}
+size_t hd_class_loss_grad_workspace_bytes_of(int64_t N, int64_t D, int64_t K, hd_dtype dt,
+                                             int with_dH, int with_dC) {
+  if (N < 1 || class_sizes(N, D, K, dt) != HD_OK || (!with_dH && !with_dC)) return 0;
+  return hd::ops::class_grad_ws_bytes(N, D, K, dt, with_dH != 0, with_dC != 0);
 }
 
 hd_status hd_class_loss_grad(const void* H, int64_t ldh, const void* C, int64_t ldc,
@@ -373,7 +377,8 @@ hd_status hd_class_loss_grad(const void* H, int64_t ldh, const void* C, int64_t 
   if (N == 0)  // an empty sum
     return dC ? from_hip(hd::launch_zero(dC, (size_t)(K * D) * esize(dt), stream)) : HD_OK;
   if (!g_loss || !aligned(g_loss, 4) || !workspace || !aligned(workspace, 256)) return HD_ERR_ARG;
-  if (workspace_bytes < hd::ops::class_grad_ws_bytes(N, D, K, dt)) return HD_ERR_WORKSPACE;
+  if (workspace_bytes < hd::ops::class_grad_ws_bytes(N, D, K, dt, dH != nullptr, dC != nullptr))
+    return HD_ERR_WORKSPACE;
   const hd::ops::ClassArgs a{H, ldh, C, ldc, mask, y, scale, N, D, K, dt};
   return from_hip(
       hd::ops::launch_class_loss_grad(a, stats, g_loss, dH, dC, workspace, stream));
