@@ -1078,7 +1078,7 @@ def class_loss(H, C, y, scale: float = 1.0, mask=None) -> ClassLoss:
     """Softmax cross entropy of the classes ``y`` [N] int32 (outside [0, K): none asked for, loss 0)
     under softmax(scale * H C^T), for encodings ``H`` [N, D] and class vectors ``C`` [K, D], both
     float32 or both bfloat16, without the scores being kept. ``mask`` [K]: classes that are False
-    take no part."""
+    take no part. Nothing here is recorded by autograd: gradients are ``class_loss_grad``'s."""
     torch = _torch()
     N, D, K, ldh, ldc, dt, index, yptr, mptr = _class_args(H, C, y, mask)
     buf = torch.empty(3 * N, dtype=torch.float32, device=H.device)
@@ -1120,8 +1120,9 @@ def class_loss_grad(H, C, y, cl: ClassLoss, g_loss, scale: float = 1.0, mask=Non
 def dropout(X, p: float, seed: int, step=0, out=None):
     """``X`` [N, D] (float32 or bfloat16) with values dropped with probability ``p`` and the others
     times 1 / (1 - p). Which ones is a function of ``seed`` and ``step`` (64 bits each) and a
-    value's place: the same call on the gradient is the backward pass. ``step`` may be an int64
-    tensor of one element on the GPU, which a graph's replays read. ``out`` may be X itself."""
+    value's place: the same call on the gradient is the backward pass (autograd records none).
+    ``step`` may be an int64 tensor of one element on the GPU, which a graph's replays read. ``out``
+    may be X itself."""
     torch = _torch()
     N, D, ldx, dt, index = _rows(X, "X")
     at = None

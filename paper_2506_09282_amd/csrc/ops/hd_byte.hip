@@ -11,9 +11,9 @@
 // l % 32. The blocks of 32 outputs follow each other along the inputs, filled up with zeros to
 // whole stages of 128 inputs; the outputs' scales follow the codes.
 //
-// Up to 64 rows are bound by reading the weights once (1 x 4096 x 14336 bf16 12 us a call, 32 rows 17
-// us, of which the product takes 13: 4.4 TB/s), more by the matrix units (8192 x 4096 x
-// 16384: 0.59 ms, 22 us of them the rows' codes).
+// Up to 64 rows are bound by reading the weights once (1 x 4096 x 14336 bf16 11 to 12 us a call, 32 rows
+// 16 to 17 us, of which the product takes 12 to 14: 4.4 TB/s), more by the tile's own pace (8192 x 4096
+// x 16384: 0.59 to 0.63 ms, 30 us of them the rows' codes).
 #include "hd_tile.hpp"
 
 namespace hd {
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void byte_sum_kernel(Result o, int count)
 // in LDS, which saves a launch.
 
 constexpr int kFewRows = 64;  // (64 x 4096 x 14336: 21 us instead of 36 by tiles)
-// (one row: 14 us instead of 17 by two launches; four: 22 instead of 17)
+// (4096 x 14336: one row 12 us instead of 16 by two launches, two 14 instead of 16; four 17 and 16)
 constexpr int64_t kOwnRows = 2, kOwnValues = 16384;  // of X, which a workgroup codes for itself
 
 struct Few {

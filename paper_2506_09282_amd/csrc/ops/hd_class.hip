@@ -12,9 +12,9 @@
 // that a lane holds 16 classes of one sample and most of a row's maximum and sum needs no
 // exchange between lanes.
 //
-// Many classes are bound by the matrix units: a forward pass of 4096 x 131072 by 4096 bf16 takes 3.7 ms,
-// a backward pass of 4096 x 65536 by 4096 10.2 ms (1.08 PFLOP/s of its five products, two of them
-// for the rest of dS). Few
+// Many classes are bound by the large tile's pace: a forward pass of 4096 x 131072 by 4096 bf16 takes 3.7 to
+// 3.9 ms, a backward pass of 4096 x 65536 by 4096 10.2 to 10.6 ms (1.04 to 1.08 PFLOP/s of its five
+// products, two of them for the rest of dS). Few
 // classes are bound by reading H, once forward and twice backward: 16384 x 10240 fp32 under 26
 // classes 114 and 258 us (5.9 and 5.2 TB/s).
 //

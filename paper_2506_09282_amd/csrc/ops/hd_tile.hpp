@@ -16,13 +16,15 @@
 // rows of 16 values and get 4 values of one column each), fp32, whose instruction takes one k
 // from a lane, with plain ones.
 //
-// What bounds the large tile (256 x 256, eight waves of 128 x 64): the matrix units are busy for half
-// of the cycles at 2.1 GHz. It is not memory (with every load from a cache's hot lines 4096 x
-// 131072 by 4096 bf16 took 3.73 ms instead of 3.87) and not the wait for operands (reading them a
-// quarter ahead changed nothing); a stage's 256 KB through LDS are half of its cycles. Measured: that
-// product with the epilogue of a cross entropy 3.7 ms (1.19 PFLOP/s, where a library product of
-// 8192^3 reaches 1.4 to 1.5), int8 8192 x 4096 x 16384 0.57 ms (1.9 POP/s), fp32 in three parts
-// 777 x 2047 x 32003 0.60 ms (170 TFLOP/s; fp32's own instruction 1.02 ms).
+// The large tile (256 x 256, eight waves of 128 x 64) keeps the matrix units busy for 57% of the
+// cycles in bf16 and 44% in int8, LDS for 35% in both, without bank conflicts in bf16. No unit is
+// full: its waves wait for 29 and 33% of their time, half of that for LDS, and meet at each stage's
+// barrier. It is not memory (with every load from a cache's hot lines 4096 x 131072 by 4096 bf16
+// took 3.73 ms instead of 3.87) and not the distance of the reads alone (reading operands a quarter
+// ahead changed nothing). Measured: that product with the epilogue of a cross entropy 3.7 to 3.9 ms
+// (1.12 to 1.19 PFLOP/s; a library product of 8192^3 1.22 to 1.26), int8 8192 x 4096 x 16384 0.57 to
+// 0.6 ms (1.8 to 1.9 POP/s), fp32 in three parts 777 x 2047 x 32003 0.60 to 0.63 ms (160 to 170
+// TFLOP/s; fp32's own instruction 1.02 ms). Ranges are those of several cards.
 #pragma once
 
 #include <type_traits>
