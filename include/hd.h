@@ -506,7 +506,8 @@ hd_status hd_class_loss(const void *H, int64_t ldh, const void *C, int64_t ldc,
  * both of dt, contiguous [N][D] and [K][D]; either may be NULL (not both). dS is 0 in classes that
  * take no part and rows that ask for none, and those classes' vectors and rows' encodings count
  * as 0. For HD_BF16 the two products take dS as two bf16 values, within 2^-16 of it; sums are fp32
- * and the result is rounded once. N == 0 clears dC.
+ * and the result is rounded once. An infinite g_loss gives infinities (for HD_F32 these may be
+ * NaN). N == 0 clears dC.
  * workspace: hd_class_loss_grad_workspace_bytes(...) bytes serve any call of these sizes,
  * hd_class_loss_grad_workspace_bytes_of(...) one that gives the named gradients alone: dS of max(128
  * MiB, N KiB) at most, fp32 sums of dH where the classes are taken in pieces, and parts of products

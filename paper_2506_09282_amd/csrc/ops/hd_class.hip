@@ -379,6 +379,12 @@ __device__ __forceinline__ float score_grad(const RowGrad& r, float s, int64_t k
   return r.on && open ? r.g * p : 0.0f;
 }
 
+// What a value's rounding to bf16 leaves of it (nothing of an infinity, which stays one).
+__device__ __forceinline__ float rest_of(float d) {
+  const float hi = bf16_to_f32(to_bf16(d));
+  return fabsf(hi) == INFINITY ? 0.0f : d - hi;
+}
+
 // dS[value][n][class] of a piece, rows of ld elements.
 template <class TL>
 __global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
@@ -430,7 +436,7 @@ __global__ __launch_bounds__(TL::T, 2) void class_dscores_kernel(
           store_four(mine, at, v, 4);
           if constexpr (kV > 1) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] -= bf16_to_f32(to_bf16(v[e]));
+            for (int e = 0; e < 4; ++e) v[e] = rest_of(v[e]);
             store_four(mine, at + kAcross, v, 4);
           }
           __builtin_amdgcn_sched_barrier(0);  // (four at a time: the registers hold the sums)
@@ -510,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void class_dscores_parts_kernel(
     const float d = score_grad(row, v[e], k + e, bits >> e & 1, a.scale * kLog2e);
     store_elem(dS, n * ld + k + e, d);
     if (kValues<T> > 1)
-      store_elem(dS, (a.N + n) * ld + k + e, d - bf16_to_f32(to_bf16(d)));
+      store_elem(dS, (a.N + n) * ld + k + e, rest_of(d));
   }
 }
 

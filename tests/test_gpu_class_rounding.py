@@ -52,3 +52,26 @@ def test_equal_classes(N, K, D, kind):
         off = (got.double() - ref).abs() - (e + 2.0 ** -8 * (ref.abs() + e))
         assert float(off.max()) <= 0, (float((got.double() - ref).norm() / ref.norm()),
                                        float(off.max()))
+
+
+@pytest.mark.parametrize("N,K,D", [(20, 30, 64), (200, 150, 100), (3601, 3600, 72)])
+def test_an_infinite_upstream_gradient(N, K, D):
+    """A row whose upstream gradient overflowed: infinities of the formula's signs in dC, and NaN only
+    where the formula has it (the row's own dH, a sum of both signs)."""
+    torch_or_skip()
+    import paper_2506_09282_amd as hd
+    announce(f"class gradient, infinite upstream, {N} rows, {K} classes, D {D}")
+    g = torch.Generator().manual_seed(N)
+    H, C = (torch.randn(n, D, generator=g).to(BF16) for n in (N, K))
+    H[H == 0] = 1.0
+    y = torch.arange(N, dtype=torch.int32) % K
+    up = torch.rand(N, generator=g)
+    up[5] = math.inf
+    scale = 0.3 / math.sqrt(D)
+    cl = hd.class_loss(H.cuda(), C.cuda(), y.cuda(), scale=scale)
+    dH, dC = hd.class_loss_grad(H.cuda(), C.cuda(), y.cuda(), cl, up.cuda(), scale=scale)
+    sign = -torch.sign(H[5].double()).repeat(K, 1)
+    sign[torch.arange(K) != y[5]] *= -1
+    assert torch.equal(dC.cpu().double(), sign * math.inf)
+    rest = torch.arange(N) != 5
+    assert bool(torch.isnan(dH.cpu()[5]).all()) and bool(torch.isfinite(dH.cpu()[rest]).all())
