@@ -13,9 +13,9 @@ from gpu_util import announce, torch_or_skip
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
 
-# N, K, D: narrow tiles on either side, 128 and 256 wide ones, classes in pieces
+# N, K, D: narrow tiles on either side, 128 and 256 wide ones, classes in pieces, of 256 at last
 SIZES = [(300, 3, 64), (31, 700, 130), (520, 26, 200), (1000, 100, 136), (129, 129, 129),
-         (3601, 3600, 72), (3601, 3600, 3599), (8200, 4900, 24)]
+         (3601, 3600, 72), (3601, 3600, 3599), (8200, 4900, 24), (140000, 600, 16)]
 
 
 def make(N, K, D, kind, seed):
